@@ -263,7 +263,7 @@ def _handles(st):
         st["out"] = torch.empty_like(q)
         st["lse"] = torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
         st["workspace"] = il.alloc_workspace_attention(q.shape[0], len(st["kv_len"]), case["Hq"], case["Hkv"], D, st["max_q"], st["max_kv"],
-                                                       dtype=il.ILRE_BF16 if case["dtype"] == "bf16" else il.ILRE_F32)
+                                                       total_kv=st["total_kv"], dtype=il.ILRE_BF16 if case["dtype"] == "bf16" else il.ILRE_F32)
 
 
 def _run_own(st):
