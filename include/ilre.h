@@ -211,6 +211,112 @@ int ilre_rerope_keys(const void *k_in, void *k_out, int64_t L, int32_t Hkv, int3
                      int32_t chunk_tokens, int32_t first_extra, double rope_base, const double *inv_freq,
                      int32_t pairing, const ilre_opts *opts);
 
+/* ---------------------------------------------------------------------------------------------------------
+   Around a recall: the operators that a context is streamed with, that fill and read a paged cache, and that a
+   compressed prompt is attended to with.  Inference only.  Tensors of new tokens are packed [T, heads, d]: the tokens
+   of sequence s are cu_q[s] .. cu_q[s+1] - 1.  Lengths and tables live on the device, so that a captured graph follows
+   what a later step writes there; they are taken modestly (clamped to the tensors they index), never trusted.
+   --------------------------------------------------------------------------------------------------------- */
+
+#define ILRE_MIN_PAGE_TOKENS 16
+#define ILRE_MAX_PAGE_TOKENS 32768
+
+/* Strides in elements of opts->dtype, multiples of 16 bytes; 0 = contiguous [T, heads, d].  (A fused projection's output is
+   three tensors with the token stride (Hq + 2 Hkv) * d.)  Which of them a call reads is said there. */
+typedef struct {
+    int64_t q_token, q_head;
+    int64_t out_token, out_head;
+    int64_t k_token, k_head;
+    int64_t v_token, v_head;
+} ilre_strides;
+
+/* A cache of pages, and the sequences of a call.  Token t of sequence s lies on page page_table[s * table_stride + t / page_tokens], at
+   place t % page_tokens of every kv head.  A table entry outside [0, num_pages) names no page: its tokens are absent (attention does not
+   see them, the append stores nothing there); entries past a sequence's length are not read. */
+typedef struct {
+    int32_t struct_size;     /* sizeof(ilre_paged_kv) */
+    int32_t page_tokens;     /* a power of two, ILRE_MIN_PAGE_TOKENS .. ILRE_MAX_PAGE_TOKENS */
+    int32_t num_pages;
+    int32_t Hkv;
+    int64_t stride_page, stride_head, stride_token; /* elements, the same for keys and values; 0 = contiguous [num_pages, Hkv, page_tokens, d] */
+    void *k_pages, *v_pages; /* dev, 16-byte aligned */
+    const int32_t *page_table; /* dev [n_seq] rows of table_width entries */
+    int64_t table_stride;    /* entries between rows; 0 = table_width */
+    const int32_t *kv_len;   /* dev [n_seq] tokens of each sequence, the new ones included */
+    const int32_t *cu_q;     /* dev [n_seq + 1] where each sequence's new tokens begin, ascending */
+    int32_t table_width;
+    int32_t n_seq;
+} ilre_paged_kv;
+
+/* Which tokens a row sees.  New token i of a sequence stands at p = kv_len - q_len + i and sees the tokens t < kv_len with t <= p (causal) and,
+   where window > 0, with t > p - window or t < sink (the sink part and sliding window of streaming chunked prefill). */
+typedef struct {
+    int32_t struct_size; /* sizeof(ilre_attn) */
+    int32_t causal;      /* 0: every row sees all tokens of its sequence (window must be 0) */
+    int32_t sink, window;
+    int32_t max_q;       /* the most new tokens of a sequence: decides how the work is cut up */
+    int32_t max_kv;      /* the most tokens of a sequence: likewise */
+    int64_t total_kv;    /* tokens of all sequences, 0 = n_seq * max_kv: likewise */
+} ilre_attn;
+
+/* Frequencies of rotary positions, pair j of `rotary` channels turning by inv_freq[j] radians a position.  f_j = base^(-2j/rotary).
+   ILRE_ROPE_PLAIN    f_j
+   ILRE_ROPE_LINEAR   f_j / factor
+   ILRE_ROPE_BANDS    by the turns n_j = original_len f_j / 2 pi a pair makes over the original length: f_j where n_j >= high, f_j / factor where
+                      n_j <= low, in between the two mixed with weight (n_j - low) / (high - low) of the first
+   ILRE_ROPE_PARTS    a ramp over the pairs' numbers between those that make `high` and `low` turns (rounded outwards, within [0, rotary - 1]):
+                      f_j (1 - r_j) + f_j / factor r_j; the turned channels are multiplied with 0.1 log(factor) + 1 */
+typedef enum { ILRE_ROPE_PLAIN = 0, ILRE_ROPE_LINEAR = 1, ILRE_ROPE_BANDS = 2, ILRE_ROPE_PARTS = 3 } ilre_rope_scaling;
+
+typedef struct {
+    int32_t struct_size; /* sizeof(ilre_rope_freqs) */
+    int32_t rotary;      /* channels of a head that are turned, the first ones: a multiple of 16, at most d */
+    double magnitude;    /* what the turned channels are multiplied with; 1 without scaling by parts */
+    double inv_freq[ILRE_HEAD_DIM / 2];
+} ilre_rope_freqs;
+
+/* Fills a frequency table (host computation only; a caller may as well fill it by itself).  out: host. */
+int ilre_rope_frequencies(int32_t rotary, double base, int32_t scaling, double factor, double low, double high, int32_t original_len,
+                          ilre_rope_freqs *out);
+
+/* Rotary positions: every head of token i turned by its position, pair (x, y) -> m (x cos a - y sin a, y cos a + x sin a), a = position * inv_freq[j],
+   m = magnitude, pairs by ilre_rope_pairing within the first `rotary` channels; the other channels are copied.  Angles are reduced in fp64, the rotation
+   runs in fp32, the result is rounded to opts->dtype (nearest even).
+   x          dev  [T, H, d] (strides->q_*); out dev likewise (strides->out_*), may be x itself, must not overlap it otherwise.  (Keys go straight
+                   into the recall's cache [Hkv, L, d] as out = k_cache + first token * d, out_token = d, out_head = L * d.)
+   positions  dev  T int32 of any sign, or NULL: first_position + i */
+int ilre_rope(const void *x, void *out, int32_t T, int32_t H, int32_t d, const int32_t *positions, int32_t first_position,
+              const ilre_rope_freqs *freqs, int32_t pairing, const ilre_strides *strides, const ilre_opts *opts);
+
+/* The new tokens' way into a paged cache: queries turned into q_out, keys turned and values copied to the cache, new token i of a sequence at place
+   kv_len - q_len + i.  (kv_len counts the new tokens already.)  Places outside the table, or on no page, are left out.
+   q, q_out   dev  [T, Hq, d] (strides->q_*, out_*); both NULL: keys and values only.  q_out may be q
+   k, v       dev  [T, Hkv, d] (strides->k_*, v_*); v NULL: keys only (the cache's v_pages may then be NULL)
+   positions  dev  T int32, or NULL: the tokens' places in the cache */
+int ilre_rope_append(const void *q, void *q_out, const void *k, const void *v, int32_t T, int32_t Hq, int32_t d, const int32_t *positions,
+                     const ilre_rope_freqs *freqs, int32_t pairing, const ilre_paged_kv *cache, const ilre_strides *strides, const ilre_opts *opts);
+
+/* Bytes of workspace the two attention calls can make use of (host computation only): partial results of sequences that are cut into several ranges of
+   tokens.  With less the calls cut less; without any they run all the same, slowly where few rows meet a long cache.  out_bytes: host. */
+int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_q, int32_t max_kv,
+                                   int64_t total_kv, int32_t dtype, size_t *out_bytes);
+
+/* Attention of the new tokens of n_seq sequences over a paged cache that holds them already: one token each, a chunk of a prompt, or any mixture.
+   out[i,h,:] = sum_t softmax_t(q[i,h,:] . K[g(h),t,:] * scale) V[g(h),t,:] over the tokens that ilre_attn lets row i see; consecutive query heads share a kv
+   head as in Eq. 4.  Rows that see nothing give zeros and lse = -inf.  Logits, softmax and sums are fp32, weights are rounded to opts->dtype for the
+   product with V.  Values and keys that some row of the call sees have to be finite; what no row sees may hold anything.
+   q, out     dev  [T, Hq, d] (strides->q_*, out_*); out must not overlap q
+   lse        dev  [T, Hq] float, the natural logarithm of each row's sum of exponentials; may be NULL
+   Tokens of no sequence (past cu_q[n_seq], before cu_q[0]) are left as they are. */
+int ilre_paged_attention(const void *q, void *out, float *lse, int32_t T, int32_t Hq, int32_t d, const ilre_attn *attn,
+                         const ilre_paged_kv *cache, const ilre_strides *strides, const ilre_opts *opts);
+
+/* The same over whole packed prompts: k, v dev [Tk, Hkv, d] (strides->k_*, v_*), the tokens of sequence s being cu_k[s] .. cu_k[s+1] - 1.
+   cu_q, cu_k dev n_seq + 1 int32 each, ascending; cu_k NULL: cu_q (then Tk = T). */
+int ilre_prompt_attention(const void *q, const void *k, const void *v, void *out, float *lse, int32_t T, int32_t Tk, int32_t Hq, int32_t Hkv,
+                          int32_t d, const int32_t *cu_q, const int32_t *cu_k, int32_t n_seq, const ilre_attn *attn, const ilre_strides *strides,
+                          const ilre_opts *opts);
+
 /* Measurement aid, not a step of the method: register-only loops with the instruction mix of the two scoring
    passes (Section 3.2, Eq. 4 / Eq. 5: 8 bf16 MFMAs per 32x32 block of logits; one fma, one exp2 and one add per
    logit), no LDS, no loads and no barriers inside the loop, one workgroup per compute unit.  The rate such a

@@ -20,6 +20,8 @@ ILRE_F32, ILRE_BF16 = 0, 1
 ILRE_SCORE_SUM, ILRE_SCORE_MAX = 0, 1
 ILRE_FLAG_EXACT_ROW_MAX = 1
 ILRE_ROPE_HALF, ILRE_ROPE_INTERLEAVED = 0, 1
+ILRE_ROPE_PLAIN, ILRE_ROPE_LINEAR, ILRE_ROPE_BANDS, ILRE_ROPE_PARTS = range(4)
+ILRE_MIN_PAGE_TOKENS, ILRE_MAX_PAGE_TOKENS = 16, 32768
 ILRE_MAX_BUDGET = 8192
 ILRE_MAX_POOL_KERNEL = 2047
 ILRE_MAX_POOL_KERNELS = 64
@@ -30,7 +32,8 @@ ILRE_STATIC_SCRATCH_BYTES = 4 << 20
 
 EXPORTS = ("ilre_workspace_bytes", "ilre_recall", "ilre_row_stats", "ilre_row_stats_static", "ilre_col_scores", "ilre_select",
            "ilre_select_max_avg", "ilre_recall_max_avg", "ilre_workspace_bytes_max_avg", "ilre_rerope_keys",
-           "ilre_gather_ids", "ilre_probe_mfma_ceiling", "ilre_probe_describe", "ilre_last_error")
+           "ilre_gather_ids", "ilre_rope_frequencies", "ilre_rope", "ilre_rope_append", "ilre_attention_workspace_bytes",
+           "ilre_paged_attention", "ilre_prompt_attention", "ilre_probe_mfma_ceiling", "ilre_probe_describe", "ilre_last_error")
 
 
 class IlreOpts(ctypes.Structure):
@@ -50,6 +53,52 @@ class IlreOpts(ctypes.Structure):
         ("stream", ctypes.c_void_p),
         ("sink", ctypes.c_int32),
         ("reserved", ctypes.c_int32),
+    ]
+
+
+class IlreStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q_token", "q_head", "out_token", "out_head", "k_token", "k_head", "v_token", "v_head")]
+
+
+class IlrePagedKv(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("Hkv", ctypes.c_int32),
+        ("stride_page", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("stride_token", ctypes.c_int64),
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+        ("table_stride", ctypes.c_int64),
+        ("kv_len", ctypes.c_void_p),
+        ("cu_q", ctypes.c_void_p),
+        ("table_width", ctypes.c_int32),
+        ("n_seq", ctypes.c_int32),
+    ]
+
+
+class IlreAttn(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+        ("sink", ctypes.c_int32),
+        ("window", ctypes.c_int32),
+        ("max_q", ctypes.c_int32),
+        ("max_kv", ctypes.c_int32),
+        ("total_kv", ctypes.c_int64),
+    ]
+
+
+class IlreRopeFreqs(ctypes.Structure):
+    """A table of rotary frequencies (ilre_rope_frequencies fills one; its fields may be set by hand as well)."""
+    _fields_ = [
+        ("struct_size", ctypes.c_int32),
+        ("rotary", ctypes.c_int32),
+        ("magnitude", ctypes.c_double),
+        ("inv_freq", ctypes.c_double * 64),
     ]
 
 
@@ -96,6 +145,20 @@ def load() -> ctypes.CDLL:
                                          i32, po]
         lib.ilre_gather_ids.restype = ctypes.c_int
         lib.ilre_gather_ids.argtypes = [vp, i64, vp, i32, vp, po]
+        ps, pf, pc, pa = (ctypes.POINTER(t) for t in (IlreStrides, IlreRopeFreqs, IlrePagedKv, IlreAttn))
+        f64 = ctypes.c_double
+        lib.ilre_rope_frequencies.restype = ctypes.c_int
+        lib.ilre_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, i32, pf]
+        lib.ilre_rope.restype = ctypes.c_int
+        lib.ilre_rope.argtypes = [vp, vp, i32, i32, i32, vp, i32, pf, i32, ps, po]
+        lib.ilre_rope_append.restype = ctypes.c_int
+        lib.ilre_rope_append.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, pf, i32, pc, ps, po]
+        lib.ilre_attention_workspace_bytes.restype = ctypes.c_int
+        lib.ilre_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+        lib.ilre_paged_attention.restype = ctypes.c_int
+        lib.ilre_paged_attention.argtypes = [vp, vp, vp, i32, i32, i32, pa, pc, ps, po]
+        lib.ilre_prompt_attention.restype = ctypes.c_int
+        lib.ilre_prompt_attention.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, i32, pa, ps, po]
         lib.ilre_probe_mfma_ceiling.restype = ctypes.c_int
         lib.ilre_probe_mfma_ceiling.argtypes = [i32, i32, vp, vp, ctypes.POINTER(ctypes.c_double), po]
         lib.ilre_probe_describe.restype = ctypes.c_char_p
@@ -362,6 +425,195 @@ def ilre_gather_ids(input_ids: torch.Tensor, idx: torch.Tensor, out: Optional[to
     _check(load().ilre_gather_ids(input_ids.data_ptr(), input_ids.numel(), idx.data_ptr(), idx.numel(), out.data_ptr(),
                                   ctypes.byref(o)))
     return out
+
+
+def _tokens_meta(name: str, t: torch.Tensor, heads: Optional[int] = None):
+    if t.dim() != 3 or not t.is_cuda or t.stride(2) != 1:
+        raise ValueError(f"{name} is a device tensor [tokens, heads, d] with the head dimension contiguous")
+    if heads is not None and t.shape[1] != heads:
+        raise ValueError(f"{name} has {t.shape[1]} heads, not {heads}")
+    return t.shape
+
+
+def _int32_vector(name: str, t: torch.Tensor, n: int) -> int:
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} is a contiguous int32 device vector of {n} entries")
+    return t.data_ptr()
+
+
+def _row_strides(t: torch.Tensor):
+    """Strides of [tokens, heads, d]; those of a single token or head say nothing (torch may hold anything there)."""
+    n, h, d = t.shape
+    return (t.stride(0) if n > 1 else 0), (t.stride(1) if h > 1 else 0)
+
+
+def _like(name: str, out: Optional[torch.Tensor], ref: torch.Tensor) -> torch.Tensor:
+    if out is None:
+        return torch.empty(ref.shape, dtype=ref.dtype, device=ref.device)
+    if out.shape != ref.shape or out.dtype != ref.dtype or not out.is_cuda or out.stride(2) != 1:
+        raise ValueError(f"{name} must have the shape and element type of its input, with the head dimension contiguous")
+    return out
+
+
+def ilre_rope_frequencies(rotary: int, base: float, *, scaling: int = ILRE_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                          original_len: int = 0) -> IlreRopeFreqs:
+    """Rotary frequencies (a host table that a program keeps): plain, divided by a factor, or scaled by bands or by parts; see include/ilre.h."""
+    f = IlreRopeFreqs()
+    _check(load().ilre_rope_frequencies(int(rotary), float(base), int(scaling), float(factor), float(low), float(high), int(original_len), ctypes.byref(f)))
+    return f
+
+
+def ilre_rope(x: torch.Tensor, freqs: IlreRopeFreqs, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
+              pairing: int = ILRE_ROPE_HALF, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotary positions of x [T, H, d]; `out` may be x itself, or a view of the recall's key cache: k_cache[:, a:a+T].transpose(0, 1)."""
+    T, H, d = _tokens_meta("x", x)
+    out = _like("out", out, x)
+    st = IlreStrides(*_row_strides(x), *_row_strides(out))
+    o = _opts(_dtype_code(x), 0, 0.0, ILRE_SCORE_SUM, None)
+    _check(load().ilre_rope(x.data_ptr(), out.data_ptr(), T, H, d, None if positions is None else _int32_vector("positions", positions, T),
+                            int(first_position), ctypes.byref(freqs), int(pairing), ctypes.byref(st), ctypes.byref(o)))
+    return out
+
+
+class PagedKV:
+    """A cache of pages and the sequences of a call, described once and kept: the tensors are referred to, not copied, and what a program
+    writes into page_table, kv_len and cu_q later counts in later calls.
+
+    k_pages, v_pages [num_pages, Hkv, page_tokens, d] in any layout with d contiguous (both the same; v_pages None: keys only),
+    page_table int32 [n_seq, pages a sequence], kv_len int32 [n_seq] (new tokens included), cu_q int32 [n_seq + 1]."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], page_table: torch.Tensor, kv_len: torch.Tensor, cu_q: torch.Tensor):
+        if k_pages.dim() != 4 or not k_pages.is_cuda or k_pages.stride(3) != 1:
+            raise ValueError("k_pages is a device tensor [num_pages, Hkv, page_tokens, d] with the head dimension contiguous")
+        if v_pages is not None and (v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype
+                                    or not v_pages.is_cuda):
+            raise ValueError("v_pages must have the shape, strides and element type of k_pages")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_cuda or page_table.stride(1) != 1:
+            raise ValueError("page_table is an int32 device tensor [n_seq, pages] with contiguous rows")
+        n_seq = page_table.shape[0]
+        num_pages, Hkv, P, d = k_pages.shape
+        if d != 128:
+            raise IlreError(ILRE_EUNSUPPORTED, f"head_dim {d} unsupported (only 128)")
+        self.k_pages, self.v_pages, self.page_table, self.kv_len, self.cu_q = k_pages, v_pages, page_table, kv_len, cu_q
+        self.dtype, self.n_seq, self.Hkv = _dtype_code(k_pages), n_seq, Hkv
+        c = self.c = IlrePagedKv()
+        c.struct_size = ctypes.sizeof(IlrePagedKv)
+        c.page_tokens, c.num_pages, c.Hkv = P, num_pages, Hkv
+        # the strides of a lone page or head say nothing
+        c.stride_token = k_pages.stride(2)
+        c.stride_head = k_pages.stride(1) if Hkv > 1 else max(k_pages.stride(1), d)
+        c.stride_page = k_pages.stride(0) if num_pages > 1 else max(k_pages.stride(0), d)
+        c.k_pages, c.v_pages = k_pages.data_ptr(), 0 if v_pages is None else v_pages.data_ptr()
+        c.page_table, c.table_width, c.n_seq = page_table.data_ptr(), page_table.shape[1], n_seq
+        c.table_stride = page_table.stride(0) if n_seq > 1 else page_table.shape[1]
+        c.kv_len, c.cu_q = _int32_vector("kv_len", kv_len, n_seq), _int32_vector("cu_q", cu_q, n_seq + 1)
+        self._ref = ctypes.byref(c)
+
+
+def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], cache: PagedKV, freqs: IlreRopeFreqs,
+                     positions: Optional[torch.Tensor] = None, *, pairing: int = ILRE_ROPE_HALF, q_out: Optional[torch.Tensor] = None
+                     ) -> Optional[torch.Tensor]:
+    """Turn queries (returned, or in q_out, which may be q) and keys to their positions (default: their places in the cache) and store keys and values in
+    the cache.  q [T, Hq, d], k and v [T, Hkv, d], any token and head strides; q None: keys and values only; v None: keys only."""
+    T, _, d = _tokens_meta("k", k, cache.Hkv)
+    dt = _dtype_code(k)
+    if dt != cache.dtype or any(t is not None and t.dtype != k.dtype for t in (q, v)):
+        raise TypeError("q, k, v and the cache must share an element type")
+    qs = os_ = vs = (0, 0)
+    Hq = cache.Hkv
+    if q is not None:
+        Tq, Hq, dq = _tokens_meta("q", q)
+        if Tq != T or dq != d:
+            raise ValueError("q and k differ in tokens or head dimension")
+        q_out = _like("q_out", q_out, q)
+        qs, os_ = _row_strides(q), _row_strides(q_out)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if v is not None:
+        if _tokens_meta("v", v, cache.Hkv) != k.shape:
+            raise ValueError("k and v differ in shape")
+        if cache.v_pages is None:
+            raise ValueError("the cache holds keys only")
+        vs = _row_strides(v)
+    st = IlreStrides(*qs, *os_, *_row_strides(k), *vs)
+    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    _check(load().ilre_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
+                                   None if v is None else v.data_ptr(), T, Hq, d,
+                                   None if positions is None else _int32_vector("positions", positions, T), ctypes.byref(freqs), int(pairing),
+                                   cache._ref, ctypes.byref(st), ctypes.byref(o)))
+    return q_out
+
+
+def ilre_attention_workspace_bytes(T: int, n_seq: int, Hq: int, Hkv: int, d: int, max_q: int, max_kv: int, total_kv: int, dtype: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().ilre_attention_workspace_bytes(int(T), int(n_seq), Hq, Hkv, d, int(max_q), int(max_kv), int(total_kv), dtype, ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_workspace_attention(T: int, n_seq: int, Hq: int, Hkv: int, d: int, max_q: int, max_kv: int, *, total_kv: int = 0, dtype: int = ILRE_BF16,
+                              device="cuda") -> torch.Tensor:
+    return torch.empty(ilre_attention_workspace_bytes(T, n_seq, Hq, Hkv, d, max_q, max_kv, total_kv, dtype), dtype=torch.uint8, device=device)
+
+
+def _attention_outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse: Optional[torch.Tensor], T: int, Hq: int):
+    out = _like("out", out, q)
+    if lse is None:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.shape != (T, Hq) or not lse.is_contiguous() or not lse.is_cuda:
+        raise ValueError("lse is a contiguous float32 device tensor [T, Hq]")
+    return out, lse
+
+
+def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv: int, total_kv: int = 0, causal: bool = True, sink: int = 0,
+                         window: int = 0, scale: float = 0.0, workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of new tokens q [T, Hq, d] over a paged cache that holds them already; returns (out [T, Hq, d], lse float32 [T, Hq]).
+    max_q, max_kv, total_kv: the most new tokens and tokens of a sequence, and all tokens together (0: not known); they decide how the work is
+    cut up, not what comes out."""
+    T, Hq, d = _tokens_meta("q", q)
+    dt = _dtype_code(q)
+    if dt != cache.dtype:
+        raise TypeError("q and the cache must share an element type")
+    if cache.v_pages is None:
+        raise ValueError("the cache holds keys only")
+    out, lse = _attention_outputs(q, out, lse, T, Hq)
+    if workspace is None:
+        workspace = alloc_workspace_attention(T, cache.n_seq, Hq, cache.Hkv, d, max_q, max_kv, total_kv=total_kv, dtype=dt, device=q.device)
+    at = IlreAttn(ctypes.sizeof(IlreAttn), 1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
+    st = IlreStrides(*_row_strides(q), *_row_strides(out))
+    o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
+    _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, ctypes.byref(at), cache._ref, ctypes.byref(st),
+                                       ctypes.byref(o)))
+    return out, lse
+
+
+def ilre_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, *, cu_k: Optional[torch.Tensor] = None, max_q: int,
+                          max_k: Optional[int] = None, causal: bool = True, sink: int = 0, window: int = 0, scale: float = 0.0,
+                          workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                          ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of packed sequences, q [T, Hq, d], k and v [Tk, Hkv, d], cut up by cu_q and cu_k (int32 [n_seq + 1]; cu_k None: cu_q); the last
+    queries of a sequence stand at its last keys.  Returns (out [T, Hq, d], lse float32 [T, Hq])."""
+    T, Hq, d = _tokens_meta("q", q)
+    Tk, Hkv, dk = _tokens_meta("k", k)
+    if v.shape != k.shape or dk != d:
+        raise ValueError("k and v differ in shape, or from q in the head dimension")
+    _tokens_meta("v", v)
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("q, k and v must share an element type")
+    n_seq = cu_q.numel() - 1
+    pq = _int32_vector("cu_q", cu_q, n_seq + 1)
+    pk = None if cu_k is None else _int32_vector("cu_k", cu_k, n_seq + 1)
+    max_k = max_q if max_k is None else max_k
+    dt = _dtype_code(q)
+    out, lse = _attention_outputs(q, out, lse, T, Hq)
+    if workspace is None:
+        workspace = alloc_workspace_attention(T, n_seq, Hq, Hkv, d, max_q, max_k, total_kv=Tk, dtype=dt, device=q.device)
+    at = IlreAttn(ctypes.sizeof(IlreAttn), 1 if causal else 0, int(sink), int(window), int(max_q), int(max_k), Tk)
+    st = IlreStrides(*_row_strides(q), *_row_strides(out), *_row_strides(k), *_row_strides(v))
+    o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
+    _check(load().ilre_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Tk, Hq, Hkv, d, pq, pk, n_seq,
+                                        ctypes.byref(at), ctypes.byref(st), ctypes.byref(o)))
+    return out, lse
 
 
 ILRE_PROBE_OPERAND_BYTES = 65536

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libilre.so")
-SOURCES = ["scoring.hip", "select.hip", "rerope.hip", "ceiling.hip", "api.hip"]
+SOURCES = ["scoring.hip", "select.hip", "rerope.hip", "ceiling.hip", "attention.hip", "rope.hip", "api.hip", "api_attention.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

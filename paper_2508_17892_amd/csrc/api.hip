@@ -19,7 +19,10 @@ namespace {
 
 thread_local char g_err[256] = "";
 
-int fail(int status, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+}  // namespace
+
+namespace ilre {
+
 int fail(int status, const char *fmt, ...)
 {
     va_list ap;
@@ -28,6 +31,33 @@ int fail(int status, const char *fmt, ...)
     va_end(ap);
     return status;
 }
+
+int hip_fail(hipError_t e, const char *what)
+{
+    return fail(ILRE_EHIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+int check_opts(const ilre_opts *o)
+{
+    if (!o) return fail(ILRE_EINVAL, "opts is null");
+    if (o->struct_size != (int32_t)sizeof(ilre_opts))
+        return fail(ILRE_EINVAL, "opts->struct_size %d != %zu", o->struct_size, sizeof(ilre_opts));
+    if (o->score_mode != ILRE_SCORE_SUM && o->score_mode != ILRE_SCORE_MAX)
+        return fail(ILRE_EUNSUPPORTED, "unknown score_mode %d", o->score_mode);
+    if (!(o->scale >= 0.f) || isinf(o->scale)) return fail(ILRE_EINVAL, "scale must be finite and >= 0 (0 = 1/sqrt(d))");
+    if (o->flags & ~ILRE_FLAG_EXACT_ROW_MAX) return fail(ILRE_EUNSUPPORTED, "unknown flag bits 0x%x", o->flags);
+    if (o->sink < 0) return fail(ILRE_EINVAL, "sink must be non-negative");
+    if (o->reserved != 0) return fail(ILRE_EINVAL, "opts->reserved must be 0");
+    return ILRE_OK;
+}
+
+}  // namespace ilre
+
+using ilre::check_opts;
+using ilre::fail;
+using ilre::hip_fail;
+
+namespace {
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -157,20 +187,6 @@ int check_max_avg(int64_t L, int32_t sink, int32_t budget, const int32_t *max_ke
     return ILRE_OK;
 }
 
-int check_opts(const ilre_opts *o)
-{
-    if (!o) return fail(ILRE_EINVAL, "opts is null");
-    if (o->struct_size != (int32_t)sizeof(ilre_opts))
-        return fail(ILRE_EINVAL, "opts->struct_size %d != %zu", o->struct_size, sizeof(ilre_opts));
-    if (o->score_mode != ILRE_SCORE_SUM && o->score_mode != ILRE_SCORE_MAX)
-        return fail(ILRE_EUNSUPPORTED, "unknown score_mode %d", o->score_mode);
-    if (!(o->scale >= 0.f) || isinf(o->scale)) return fail(ILRE_EINVAL, "scale must be finite and >= 0 (0 = 1/sqrt(d))");
-    if (o->flags & ~ILRE_FLAG_EXACT_ROW_MAX) return fail(ILRE_EUNSUPPORTED, "unknown flag bits 0x%x", o->flags);
-    if (o->sink < 0) return fail(ILRE_EINVAL, "sink must be non-negative");
-    if (o->reserved != 0) return fail(ILRE_EINVAL, "opts->reserved must be 0");
-    return ILRE_OK;
-}
-
 int check_workspace(const ilre_opts *o, size_t need)
 {
     if (!o->workspace) return fail(ILRE_ENOMEM, "workspace is null (%zu bytes needed)", need);
@@ -231,11 +247,6 @@ void fill_plan(ilre::ScoreArgs &a, const ilre::ScorePlan &p)
     a.ntiles = p.ntiles;
     a.tiles_per_split = p.tiles_per_split;
     a.table_tag = p.table_tag;
-}
-
-int hip_fail(hipError_t e, const char *what)
-{
-    return fail(ILRE_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
 // Device address of the static scratch array on the current device, looked up once per device.

@@ -1,0 +1,917 @@
+// Attention of new tokens over a cache of pages, and over whole packed prompts, for gfx950.
+//
+//   out[r] = sum_t p_rt V_t / sum_t p_rt,   p_rt = exp(q_r . K_t * scale - m_r),   log sum_t exp(q_r . K_t * scale)
+//
+// over the tokens t that row r sees: t < kv_len, t <= p (causal; p is the row's position in its sequence) and, with a window,
+// t > p - window or t < sink.  A row is a new token and a query head; the rows of a kv head's G query heads are taken together
+// (row = token * G + head of the group), so that a K tile that is in LDS serves all of them.
+//
+// Both products run with the tokens of the tile as matrix rows: S^T = K Q^T leaves lane l with the logits of query l % 32 and
+// tokens 8 (i / 4) + 4 (l / 32) + i % 4, i = 0..15, so that the softmax of a row is that lane's (and its partner's, l ^ 32) own
+// business, and the same registers, rounded to bf16 in pairs, are the right operand of O^T += V^T P^T: which token stands at
+// which place of the contraction is free as long as both operands agree, and V^T is read from LDS with the transposing
+// read (four tokens of one channel a lane) in that very order.  P never goes through LDS.
+//
+// Weights are taken relative to a reference m per row.  attend_rows follows the running maximum over a row's first tiles and then
+// keeps it: any m gives the same quotient as long as the exponentials stay in range, and the maximum, the rescaling and the branch in
+// front of it are a fifth of the vector work.  A row whose later logits exceed its reference by more than 2^60 shows in its
+// sum, and the workgroup walks its tiles again, following the maximum all the way.
+#include "ilre_internal.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <mutex>
+
+namespace ilre {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+
+namespace {
+
+constexpr float kFloor = -1.0e30f;            // reference of a row that has seen nothing, in base-2 units
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+__device__ __forceinline__ uint4 lds_read16(unsigned at) 
+{
+    return __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) u32x4 *)(size_t)at);
+}
+__device__ __forceinline__ float lds_read4(unsigned at) { return *(const __attribute__((address_space(3))) float *)(size_t)at; }
+// Four tokens of the lane's channel: the 16 lanes of a group point at 4 rows x 16 channels (8 bytes each), and each gets a column.
+__device__ __forceinline__ u32x2 lds_read_tr(unsigned at)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(size_t)at));
+}
+// Table entries and lengths: the same for the whole wavefront and not written while the kernel runs, so that they come through the
+// scalar cache, outside the count of vector loads that the tile copies are waited for by.
+__device__ __forceinline__ int scalar_i32(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b)  // nearest even
+{
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// ------------------------------------------------------------------------------------------------ which rows, which tiles
+
+// The rows of one workgroup, and the tokens they see.  All of it is the same for the whole wavefront.
+struct Block {
+    int seq, rows0, nrows;  // rows0: first row within the sequence; nrows: rows of the sequence
+    int q0, q_len;          // first new token in the packed order
+    int kv, kv0;            // tokens in the sequence; first one in the packed order (contiguous keys)
+    int lo, hi;             // tokens that a row of this block may see: [0, sink) and [lo, hi)
+    int sink;               // of the sink part, what lies before lo
+    int ns, w0, nt;         // tiles [0, ns) and [w0, w0 + nt - ns)
+    int all_lo, all_hi;     // tokens that every row of this block sees: [all_lo, all_hi)
+};
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+template <bool PAGED>
+__device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b)
+{
+    b.seq = seq;
+    b.q0 = clampi(scalar_i32(a.cu_q + seq), 0, a.T);
+    b.q_len = clampi(scalar_i32(a.cu_q + seq + 1), b.q0, a.T) - b.q0;
+    if (PAGED) {
+        b.kv0 = 0;
+        b.kv = (int)min((int64_t)max(scalar_i32(a.kv_len + seq), 0), a.kv_limit);
+    } else {
+        b.kv0 = clampi(scalar_i32(a.cu_k + seq), 0, a.Tk);
+        b.kv = clampi(scalar_i32(a.cu_k + seq + 1), b.kv0, a.Tk) - b.kv0;
+    }
+    b.nrows = b.q_len * a.G;
+}
+
+// Tiles of `tn` tokens that the rows rows0 .. rows0 + rows - 1 see something of.
+__device__ __forceinline__ void tiles_of(const AttnArgs &a, Block &b, int rows, int tn)
+{
+    const int first = b.rows0 / a.G, last = min(b.rows0 + rows, b.nrows) - 1;
+    const int64_t p0 = (int64_t)b.kv - b.q_len + first, p1 = (int64_t)b.kv - b.q_len + last / a.G;
+    b.hi = a.causal ? (int)min(max(p1 + 1, (int64_t)0), (int64_t)b.kv) : b.kv;
+    b.all_hi = a.causal ? (int)min(max(p0 + 1, (int64_t)0), (int64_t)b.kv) : b.kv;
+    b.lo = b.all_lo = b.sink = 0;
+    if (a.window > 0) {
+        b.lo = (int)min(max(p0 - a.window + 1, (int64_t)0), (int64_t)b.hi);
+        b.all_lo = (int)max(p1 - a.window + 1, (int64_t)0);
+        b.sink = min(a.sink, b.lo);
+    }
+    const int end = (b.hi + tn - 1) / tn;
+    b.ns = min((b.sink + tn - 1) / tn, end);
+    b.w0 = max(b.lo / tn, b.ns);
+    b.nt = b.hi > 0 ? b.ns + max(end - b.w0, 0) : 0;
+}
+
+// Workgroup w's block of `rows` rows: the blocks of all sequences one after the other, within a sequence the last one first (with a causal
+// mask it has most to do).  False where there are fewer blocks.
+template <bool PAGED>
+__device__ __forceinline__ bool find_block(const AttnArgs &a, int w, int rows, Block &b)
+{
+    int seq = 0, before = 0;
+    if (a.n_seq > 1) {
+        const int lane = threadIdx.x & 63;
+        bool found = false;
+        for (int base = 0; base < a.n_seq && !found; base += 64) {
+            const int s = base + lane;
+            int n = 0;
+            if (s < a.n_seq) {
+                const int from = clampi(a.cu_q[s], 0, a.T);
+                n = ((clampi(a.cu_q[s + 1], from, a.T) - from) * a.G + rows - 1) / rows;
+            }
+            int sum = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int x = __shfl_up(sum, o);
+                if (lane >= o) sum += x;
+            }
+            const unsigned long long past = __ballot(before + sum > w);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                seq = base + at;
+                before += __shfl(sum - n, at);
+                found = true;
+            } else {
+                before += __shfl(sum, 63);
+            }
+        }
+        if (!found) return false;
+    }
+    sequence_of<PAGED>(a, __builtin_amdgcn_readfirstlane(seq), b);
+    const int n = (b.nrows + rows - 1) / rows;
+    const int at = __builtin_amdgcn_readfirstlane(w - before);
+    if (at >= n) return false;
+    b.rows0 = (n - 1 - at) * rows;
+    return true;
+}
+
+// Into how many ranges of tiles a block's list is cut: the same answer here, in the merge and on the host.
+__device__ __forceinline__ int splits_of(const AttnArgs &a, int nt)
+{
+    return a.nsplit == 1 || nt <= a.split_tiles ? 1 : min(a.nsplit, (nt + a.split_tiles - 1) / a.split_tiles);
+}
+
+// ------------------------------------------------------------------------------------------------ tile copies
+
+// Where a kv head's keys (or values) lie, and the part of a tile that one wavefront copies: `rows` consecutive tokens, 16 at most and
+// aligned, so that they are on one page.
+struct Source {
+    uint64_t base;
+    int64_t page, token;  // bytes
+};
+
+// A page's number, clamped to the table; -1 where the entry names no page (its tokens count as absent).
+__device__ __forceinline__ int page_of(const AttnArgs &a, const Block &b, int tok)
+{
+    const int at = min(tok >> a.page_shift, a.table_width - 1);
+    const int id = scalar_i32(a.table + (int64_t)b.seq * a.table_stride + at);
+    return (unsigned)id < (unsigned)a.num_pages ? id : -1;
+}
+
+// One wavefront's share of a tile, from its first token `tok` on: ROWS rows of ROWB bytes to LDS address `to`, 16-byte chunk c of a row at place
+// c ^ swizzle(row).  Rows that no row of the block sees (past hi, between sink and lo, on no page) are written as zeros: what lies there may
+// be anything, and 0 * NaN is no 0.  Always the same number of copies, so that they can be waited for by count.
+template <int ROWS, int ROWB, bool VALUES, bool PAGED>
+__device__ __forceinline__ void copy_rows(const AttnArgs &a, const Block &b, const Source &src, int tok, int page, unsigned to, const int (&voff)[ROWS * ROWB / 1024],
+                                          int lane)
+{
+    constexpr int N = ROWS * ROWB / 1024, PER = 1024 / ROWB;
+    uint64_t at;
+    int n = clampi(b.hi - tok, 0, ROWS);
+    if (PAGED) {
+        at = src.base + (uint64_t)((int64_t)max(page, 0) * src.page + (int64_t)(tok & ((1 << a.page_shift) - 1)) * src.token);
+        if (page < 0) n = 0;
+    } else {
+        at = src.base + (uint64_t)((int64_t)(n > 0 ? tok : 0) * src.token);
+    }
+    i32x4 rsrc;
+    rsrc[0] = __builtin_amdgcn_readfirstlane((int)(unsigned)at);
+    rsrc[1] = __builtin_amdgcn_readfirstlane((int)((unsigned)(at >> 32) & 0xFFFFu));
+    rsrc[2] = __builtin_amdgcn_readfirstlane(n > 0 ? (int)((n - 1) * src.token) + ROWB : 0);
+    rsrc[3] = 0x00020000;
+    const bool gap = __builtin_amdgcn_readfirstlane(tok < b.lo && tok + ROWS > b.sink);
+    if (!gap) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) lds_dma16(rsrc, __builtin_amdgcn_readfirstlane(to + j * 1024), voff[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int t = tok + j * PER + lane / (64 / PER);
+            lds_dma16(rsrc, __builtin_amdgcn_readfirstlane(to + j * 1024), t < b.lo && t >= b.sink ? -1 : voff[j]);
+        }
+    }
+}
+
+// Byte offsets, within the copied rows, of the chunks that this lane moves.
+template <int ROWS, int ROWB, bool VALUES>
+__device__ __forceinline__ void copy_offsets(int (&voff)[ROWS * ROWB / 1024], int first_row, int64_t token_bytes, int lane)
+{
+    constexpr int N = ROWS * ROWB / 1024, CPR = ROWB / 16, PER = 1024 / ROWB;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int row = j * PER + lane / CPR, place = lane % CPR, r = first_row + row;
+        voff[j] = (int)(row * token_bytes) + (place ^ (VALUES ? (r & 3) << 2 : r & 15)) * 16;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ products
+
+template <int DT>
+struct Elem;
+
+template <>
+struct Elem<ILRE_BF16> {
+    static constexpr int ROWB = 256, QREGS = 8;  // QREGS: 16-byte pieces a lane holds of its query row
+    struct Weights {
+        uint4 p[2];
+    };
+    static __device__ __forceinline__ void mma(f32x16 &acc, const uint4 &x, const uint4 &y)
+    {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+    }
+    // lane-dependent parts of the LDS addresses: chunk 2 st + half of key row l32; the value rows' column block
+    struct Addr {
+        unsigned k[8], v[4];
+        __device__ __forceinline__ void init(int lane)
+        {
+            const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
+#pragma unroll
+            for (int st = 0; st < 8; ++st) k[st] = l32 * ROWB + (((2 * st + half) ^ (l32 & 15)) * 16);
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+                v[db] = (4 * half + (l16 >> 2)) * ROWB + ((db ^ (l16 >> 2)) * 64) + ((lane >> 4) & 1) * 32 + (l16 & 3) * 8;
+        }
+    };
+    template <int NB>
+    static __device__ __forceinline__ void logits(f32x16 (&s)[NB], const uint4 (&q)[NB][QREGS], const Addr &ad, unsigned kat)
+    {
+#pragma unroll
+        for (int st = 0; st < 8; ++st) {
+            const uint4 kf = lds_read16(ad.k[st] + kat);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                if (st == 0) s[b] = f32x16{};
+                mma(s[b], kf, q[b][st]);
+            }
+        }
+    }
+    // The weights are rounded to bf16 for the product with V, like V itself; their sum is taken before.
+    static __device__ __forceinline__ void pack(Weights &w, const float (&p)[16])
+    {
+        unsigned u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+        w.p[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        w.p[1] = make_uint4(u[4], u[5], u[6], u[7]);
+    }
+    template <int NB>
+    static __device__ __forceinline__ void values(f32x16 (&o)[NB][4], const Weights (&w)[NB], const Addr &ad, unsigned vat)
+    {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                const u32x2 x = lds_read_tr(ad.v[db] + vat + ks * 16 * ROWB), y = lds_read_tr(ad.v[db] + vat + (ks * 16 + 8) * ROWB);
+                const uint4 vf = make_uint4(x[0], x[1], y[0], y[1]);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) mma(o[b][db], vf, w[b].p[ks]);
+            }
+    }
+};
+
+// fp32 states: the fp32 matrix instructions (a sixteenth of the bf16 rate), nothing is rounded on the way.
+template <>
+struct Elem<ILRE_F32> {
+    static constexpr int ROWB = 512, QREGS = 16;
+    struct Weights {
+        float p[16];
+    };
+    struct Addr {
+        unsigned k[16], v[4];
+        __device__ __forceinline__ void init(int lane)
+        {
+            const int l32 = lane & 31, half = lane >> 5;
+#pragma unroll
+            for (int st = 0; st < 16; ++st) k[st] = l32 * ROWB + (((2 * st + half) ^ (l32 & 15)) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = 4 * half * ROWB + j * ROWB + (((l32 >> 2) ^ ((j & 1) << 2)) * 16) + (l32 & 3) * 4;
+        }
+    };
+    template <int NB>
+    static __device__ __forceinline__ void logits(f32x16 (&s)[NB], const uint4 (&q)[NB][QREGS], const Addr &ad, unsigned kat)
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+#pragma unroll
+        for (int st = 0; st < 16; ++st) {
+            const uint4 kf = lds_read16(ad.k[st] + kat);
+            const unsigned k[4] = {kf.x, kf.y, kf.z, kf.w};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const unsigned x[4] = {q[b][st].x, q[b][st].y, q[b][st].z, q[b][st].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(x[e]), s[b], 0, 0, 0);
+            }
+        }
+    }
+    static __device__ __forceinline__ void pack(Weights &w, const float (&p)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w.p[i] = p[i];
+    }
+    template <int NB>
+    static __device__ __forceinline__ void values(f32x16 (&o)[NB][4], const Weights (&w)[NB], const Addr &ad, unsigned vat)
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                // chunk (8 db + l32 / 4) ^ (i % 4 << 2): the upper bit of the XOR picks another channel block
+                const float v = lds_read4(ad.v[i & 3] + vat + (i >> 2) * 8 * ROWB + (db ^ ((i & 3) >> 1)) * 128);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) o[b][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[b].p[i], o[b][db], 0, 0, 0);
+            }
+    }
+};
+
+// One row of a lane and what it sees.
+struct Row {
+    int lo, hi;  // [0, sink) and [lo, hi)
+};
+
+// A wavefront's running state for NB x 32 rows.
+template <int DT, int NB>
+struct State {
+    uint4 q[NB][Elem<DT>::QREGS];
+    f32x16 o[NB][4];
+    float m[NB], z[NB][4];
+    Row row[NB];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int db = 0; db < 4; ++db) o[b][db] = f32x16{};
+            m[b] = kFloor;
+            z[b][0] = z[b][1] = z[b][2] = z[b][3] = 0.f;
+        }
+    }
+    // Query rows row0 + 32 b + l32 of the sequence; past the last one zeros, which see what the last one sees and are written nowhere.
+    __device__ __forceinline__ void load(const AttnArgs &a, const Block &blk, int head_kv, int row0, int l32, int half)
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int want = row0 + 32 * b + l32, r = min(want, blk.nrows - 1);
+            const int i = r / a.G, g = r - i * a.G;
+            const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head_kv * a.G + g) * a.q_head + half * 16;
+#pragma unroll
+            for (int st = 0; st < Elem<DT>::QREGS; ++st) q[b][st] = *(const uint4 *)(src + st * 32);
+            // waited for here, not in the loop over tiles, where that would be a wait for the tile copies as well
+#pragma unroll
+            for (int st = 0; st < Elem<DT>::QREGS; ++st) asm volatile("" : "+v"(q[b][st].x), "+v"(q[b][st].y), "+v"(q[b][st].z), "+v"(q[b][st].w));
+            if (want != r) {
+#pragma unroll
+                for (int st = 0; st < Elem<DT>::QREGS; ++st) q[b][st] = make_uint4(0, 0, 0, 0);
+            }
+            const int p = blk.kv - blk.q_len + i;
+            row[b].hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
+            row[b].lo = a.window > 0 ? p - a.window + 1 : 0;
+        }
+    }
+    // The logits of 32 tokens from `tok` on become weights; the running maximum is followed.  `absent`: bit 0 / 1: the first / last 16 are on no page.
+    template <bool MASKED>
+    __device__ __forceinline__ void weigh(f32x16 (&s)[NB], typename Elem<DT>::Weights (&w)[NB], float c, int tok, int sink, int half, int absent)
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if (MASKED) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int t = tok + 8 * (i >> 2) + 4 * half + (i & 3);
+                    const bool seen = t < row[b].hi && (t >= row[b].lo || t < sink) && !(absent >> (i >> 3) & 1);
+                    s[b][i] = seen ? s[b][i] : -INFINITY;
+                }
+            }
+            float top = s[b][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
+            top = fmaxf(top, other_half(top));
+            const float mnew = fmaxf(m[b], top * c);
+            if (__ballot(mnew != m[b])) {
+                const float f = exp2_fast(m[b] - mnew);
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[b][db][i] *= f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) z[b][k] *= f;
+                m[b] = mnew;
+            }
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = exp2_fast(fmaf(s[b][i], c, -m[b]));
+                z[b][i & 3] += p[i];
+            }
+            Elem<DT>::pack(w[b], p);
+        }
+    }
+    __device__ __forceinline__ float sum(int b) const
+    {
+        const float x = (z[b][0] + z[b][1]) + (z[b][2] + z[b][3]);
+        return x + other_half(x);
+    }
+};
+
+// Where a row's results go: where all of its tokens were in this workgroup's range, out and the logarithm of the sum; otherwise the quotient in
+// fp32 and the base-2 logarithm for the merge.
+struct Target {
+    bool real, direct;
+    int64_t row;          // token * Hq + head (in the range's part of the partial results)
+    unsigned char *out;
+    float f, e;           // 1 / sum, log2 of the sum of 2^logit
+};
+
+__device__ __forceinline__ Target target_of(const AttnArgs &a, const Block &blk, int head_kv, int want, bool direct, int split, float m, float sum)
+{
+    Target t;
+    t.real = want < blk.nrows;
+    t.direct = direct;
+    const int r = t.real ? want : 0, i = r / a.G, g = r - i * a.G;
+    const int token = blk.q0 + i, head = head_kv * a.G + g;
+    t.row = ((int64_t)(direct ? 0 : split) * a.T + token) * a.Hq + head;
+    t.out = a.out + (int64_t)token * a.out_token + (int64_t)head * a.out_head;
+    t.f = sum == 0.f ? 0.f : 1.f / sum;
+    t.e = sum == 0.f ? -INFINITY : m + __log2f(sum);
+    return t;
+}
+
+// x holds channels 32 db + 8 (i / 4) + 4 half + i % 4.
+template <int DT>
+__device__ __forceinline__ void store_channels(const AttnArgs &a, const Target &t, int db, const f32x16 &x, int half)
+{
+    float y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i] * t.f;
+    if (!t.direct || DT == ILRE_F32) {
+        float *to = t.direct ? (float *)t.out : a.part_o + t.row * kHeadDim;
+        if (t.real) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *(float4 *)(to + db * 32 + 8 * k + 4 * half) = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 16; k += 8) {
+        // the halves hold 4 channels each of two groups of 8: after the swap each has one group whole
+        const u32x2 u = __builtin_amdgcn_permlane32_swap(pack_bf16(y[k], y[k + 1]), pack_bf16(y[k + 4], y[k + 5]), false, false);
+        const u32x2 v = __builtin_amdgcn_permlane32_swap(pack_bf16(y[k + 2], y[k + 3]), pack_bf16(y[k + 6], y[k + 7]), false, false);
+        if (t.real) *(uint4 *)(t.out + (db * 32 + 2 * k + 8 * half) * 2) = make_uint4(u[0], v[0], u[1], v[1]);
+    }
+}
+
+__device__ __forceinline__ void store_sum(const AttnArgs &a, const Target &t, int half)
+{
+    if (!t.real || half != 0) return;
+    if (!t.direct)
+        a.part_e[t.row] = t.e;
+    else if (a.lse)
+        a.lse[t.row] = t.e * kLn2;
+}
+
+// Whether an entry of the page table between tokens `from` and `to` names no page.
+__device__ __forceinline__ bool pages_missing(const AttnArgs &a, const Block &b, int from, int to, int tid, int threads)
+{
+    bool missing = false;
+    if (from < to) {
+        const int32_t *t = a.table + (int64_t)b.seq * a.table_stride;
+        const int last = min((to - 1) >> a.page_shift, a.table_width - 1);
+        for (int i = (from >> a.page_shift) + tid; i <= last; i += threads) missing = missing || (unsigned)t[i] >= (unsigned)a.num_pages;
+    }
+    return missing;
+}
+
+// ------------------------------------------------------------------------------------------------ many rows
+
+// WAVES wavefronts of NB x 32 rows share the tiles of TN tokens.  Keys and values have four tile buffers each; while tile i is worked on, its values, the
+// keys of tile i + 1 and (in the pipelined loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.
+template <int DT, int WAVES, int NB, int TN, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void attend_rows(const AttnArgs a)
+{
+    using E = Elem<DT>;
+    constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, ROWS = WAVES * NB * 32, SUB = TN / 32;
+    constexpr int CROWS = TN / WAVES, COPIES = CROWS * ROWB / 1024;  // a wavefront's rows and copies of a tile
+    static_assert(CROWS <= 16 && CROWS * ROWB % 1024 == 0 && TN % 32 == 0, "a wavefront's rows lie on one page");
+    extern __shared__ __align__(16) unsigned char smem[];
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+    // kv heads run fastest: workgroups that share keys and values are a multiple of Hkv apart, on one XCD where Hkv is a multiple of 8
+    const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, split = rest / a.nblocks;
+    Block blk;
+    if (!find_block<PAGED>(a, rest - split * a.nblocks, ROWS, blk)) return;
+    tiles_of(a, blk, ROWS, TN);
+    const int nsp = splits_of(a, blk.nt);
+    if (split >= nsp) return;
+    const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
+    auto token_of = [&](int i) { return (first + i < blk.ns ? first + i : first + i - blk.ns + blk.w0) * TN; };
+
+    State<DT, NB> st;
+    const int row0 = blk.rows0 + wave * NB * 32;
+    const bool idle = row0 >= blk.nrows;
+    st.load(a, blk, head, row0, l32, half);
+    st.clear();
+
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    typename E::Addr ad;
+    ad.init(lane);
+    bool careful = false;
+    int *flag = (int *)(smem + 8 * SLOT);
+    if (tid == 0) *flag = 0;
+    __syncthreads();
+    if (PAGED && count > 0) {
+        const int from = token_of(0), to = min(token_of(count - 1) + TN, blk.hi);
+        bool missing;
+        if (first < blk.ns)
+            missing = pages_missing(a, blk, from, min(blk.sink, to), tid, WAVES * 64) || pages_missing(a, blk, blk.lo, to, tid, WAVES * 64);
+        else
+            missing = pages_missing(a, blk, max(from, blk.lo), to, tid, WAVES * 64);
+        if (missing) *flag = 1;
+        __syncthreads();
+        careful = __builtin_amdgcn_readfirstlane(*flag) != 0;
+        __syncthreads();
+        if (tid == 0) *flag = 0;
+    }
+
+    Source ks, vs;
+    ks.base = (uint64_t)a.k + (uint64_t)((int64_t)head * a.k_head + (int64_t)blk.kv0 * a.k_token);
+    vs.base = (uint64_t)a.v + (uint64_t)((int64_t)head * a.v_head + (int64_t)blk.kv0 * a.v_token);
+    ks.page = a.k_page, vs.page = a.v_page, ks.token = a.k_token, vs.token = a.v_token;
+    int kvoff[COPIES], vvoff[COPIES];
+    copy_offsets<CROWS, ROWB, false>(kvoff, wave * CROWS, a.k_token, lane);
+    copy_offsets<CROWS, ROWB, true>(vvoff, wave * CROWS, a.v_token, lane);
+    int pages[2];  // of this wavefront's rows: of the last tile whose keys were asked for, and the next one
+    auto own_token = [&](int i) { return i < count ? token_of(i) + wave * CROWS : blk.hi; };
+    auto lookup = [&](int i) { return PAGED ? page_of(a, blk, min(own_token(i), blk.hi - 1)) : 0; };
+    auto copy_keys = [&](int i, int page) {
+        copy_rows<CROWS, ROWB, false, PAGED>(a, blk, ks, own_token(i), page, lds0 + (i & 3) * SLOT + wave * CROWS * ROWB, kvoff, lane);
+    };
+    auto copy_values = [&](int i, int page) {
+        copy_rows<CROWS, ROWB, true, PAGED>(a, blk, vs, own_token(i), page, lds0 + (4 + (i & 3)) * SLOT + wave * CROWS * ROWB, vvoff, lane);
+    };
+    auto begin = [&]() {
+        const int p0 = lookup(0), p1 = lookup(1), p2 = lookup(2);
+        copy_keys(0, p0);
+        copy_keys(1, p1);
+        copy_values(0, p0);
+        copy_keys(2, p2);
+        copy_values(1, p1);
+        pages[0] = p2;
+        pages[1] = lookup(3);
+    };
+    // Tile i's values and tile i + 1's keys are there, everybody is done with tile i - 1, and the next copies are on their way.
+    auto advance = [&](int i) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * COPIES) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        copy_keys(i + 3, pages[1]);
+        copy_values(i + 2, pages[0]);
+        pages[0] = pages[1];
+        pages[1] = lookup(i + 4);
+    };
+    auto follow_tile = [&](int i) {
+        advance(i);
+        if (idle) return;
+        const int tok = token_of(i);
+        const bool whole = !careful && tok + TN <= blk.all_hi && tok >= blk.all_lo;
+#pragma unroll 1
+        for (int sub = 0; sub < SUB; ++sub) {
+            const unsigned kat = lds0 + (i & 3) * SLOT + sub * 32 * ROWB, vat = lds0 + (4 + (i & 3)) * SLOT + sub * 32 * ROWB;
+            const int t = tok + sub * 32;
+            f32x16 s[NB];
+            typename E::Weights w[NB];
+            E::template logits<NB>(s, st.q, ad, kat);
+            if (whole) {
+                st.template weigh<false>(s, w, a.c, t, a.sink, half, 0);
+            } else {
+                int absent = 0;
+                if (PAGED && careful) absent = (page_of(a, blk, t) < 0 ? 1 : 0) | (page_of(a, blk, t + 16) < 0 ? 2 : 0);
+                st.template weigh<true>(s, w, a.c, t, a.sink, half, absent);
+            }
+            E::template values<NB>(st.o, w, ad, vat);
+        }
+    };
+
+    if (count > 0) {
+        begin();
+        for (int i = 0; i < count; ++i) follow_tile(i);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    if (idle) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const Target t = target_of(a, blk, head, row0 + 32 * b + l32, nsp == 1, split, st.m[b], st.sum(b));
+#pragma unroll
+        for (int db = 0; db < 4; ++db) store_channels<DT>(a, t, db, st.o[b][db], half);
+        store_sum(a, t, half);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+
+// Up to 32 rows: each of WAVES wavefronts takes 32 of a tile's 32 * WAVES tokens, with tile buffers of its own and no barrier on the way; what they have is
+// added up at the end.
+template <int DT, int WAVES, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
+{
+    using E = Elem<DT>;
+    constexpr int ROWB = E::ROWB, SLOT = 32 * ROWB, STAGES = DT == ILRE_BF16 ? 2 : 1, TN = 32 * WAVES;
+    constexpr int HALF = 16 * ROWB / 1024, COPIES = 2 * HALF;  // copies of 16 rows, of 32
+    extern __shared__ __align__(16) unsigned char smem[];
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+    const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, split = rest / a.nblocks;
+    Block blk;
+    if (!find_block<PAGED>(a, rest - split * a.nblocks, 32, blk)) return;
+    tiles_of(a, blk, 32, TN);
+    const int nsp = splits_of(a, blk.nt);
+    if (split >= nsp) return;
+    const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
+    auto token_of = [&](int i) { return (first + i < blk.ns ? first + i : first + i - blk.ns + blk.w0) * TN + wave * 32; };
+
+    State<DT, 1> st;
+    st.load(a, blk, head, blk.rows0, l32, half);
+    st.clear();
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * 2 * STAGES * SLOT;
+    typename E::Addr ad;
+    ad.init(lane);
+
+    Source ks, vs;
+    ks.base = (uint64_t)a.k + (uint64_t)((int64_t)head * a.k_head + (int64_t)blk.kv0 * a.k_token);
+    vs.base = (uint64_t)a.v + (uint64_t)((int64_t)head * a.v_head + (int64_t)blk.kv0 * a.v_token);
+    ks.page = a.k_page, vs.page = a.v_page, ks.token = a.k_token, vs.token = a.v_token;
+    int kvoff[HALF], vvoff[HALF];
+    copy_offsets<16, ROWB, false>(kvoff, 0, a.k_token, lane);
+    copy_offsets<16, ROWB, true>(vvoff, 0, a.v_token, lane);
+    struct Pages {
+        int id[2];
+    };
+    auto own_token = [&](int i) { return i < count ? token_of(i) : blk.hi; };
+    auto lookup = [&](int i) {
+        Pages p{};
+        if (PAGED) {
+            const int t = own_token(i);
+            p.id[0] = page_of(a, blk, min(t, blk.hi - 1));
+            p.id[1] = page_of(a, blk, min(t + 16, blk.hi - 1));
+        }
+        return p;
+    };
+    auto copy_keys = [&](int i, const Pages &p) {
+        const unsigned to = lds0 + (i % STAGES) * SLOT;
+        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, own_token(i), p.id[0], to, kvoff, lane);
+        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, own_token(i) + 16, p.id[1], to + 16 * ROWB, kvoff, lane);
+    };
+    auto copy_values = [&](int i, const Pages &p) {
+        const unsigned to = lds0 + (STAGES + i % STAGES) * SLOT;
+        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, own_token(i), p.id[0], to, vvoff, lane);
+        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, own_token(i) + 16, p.id[1], to + 16 * ROWB, vvoff, lane);
+    };
+
+    if (count > 0) {
+        Pages pg[STAGES + 1];
+#pragma unroll
+        for (int s = 0; s <= STAGES; ++s) pg[s] = lookup(s);
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) {
+            copy_keys(s, pg[s]);
+            copy_values(s, pg[s]);
+        }
+        for (int i = 0; i < count; ++i) {
+            const int tok = token_of(i);
+            const int absent = PAGED ? (pg[0].id[0] < 0 ? 1 : 0) | (pg[0].id[1] < 0 ? 2 : 0) : 0;
+            const Pages next = pg[STAGES];
+            // still on their way: this step's values, and both of the steps behind it
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * STAGES - 1) * COPIES) : "memory");
+            f32x16 s[1];
+            typename E::Weights w[1];
+            E::template logits<1>(s, st.q, ad, lds0 + (i % STAGES) * SLOT);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
+            copy_keys(i + STAGES, next);
+            if (tok + 32 <= blk.all_hi && tok >= blk.all_lo && absent == 0)
+                st.template weigh<false>(s, w, a.c, tok, a.sink, half, 0);
+            else
+                st.template weigh<true>(s, w, a.c, tok, a.sink, half, absent);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * STAGES - 1) * COPIES) : "memory");
+            E::template values<1>(st.o, w, ad, lds0 + (STAGES + i % STAGES) * SLOT);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            copy_values(i + STAGES, next);
+#pragma unroll
+            for (int k = 0; k < STAGES; ++k) pg[k] = pg[k + 1];
+            pg[STAGES] = lookup(i + STAGES + 1);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    // What the wavefronts have: sums in `mine` (rows 33 pieces of 16 bytes apart), references and sums of weights behind all of them.
+    constexpr int PITCH = 132;
+    static_assert(32 * PITCH * 4 <= 2 * STAGES * SLOT, "a wavefront's sums fit where its tiles were");
+    float *mine = (float *)(smem + wave * 2 * STAGES * SLOT);
+    float2 *stats = (float2 *)(smem + WAVES * 2 * STAGES * SLOT);  // [WAVES][32]
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *(float4 *)&mine[l32 * PITCH + db * 32 + 8 * k + 4 * half] =
+                make_float4(st.o[0][db][4 * k], st.o[0][db][4 * k + 1], st.o[0][db][4 * k + 2], st.o[0][db][4 * k + 3]);
+    const float z = st.sum(0);
+    if (half == 0) stats[wave * 32 + l32] = make_float2(st.m[0], z);
+    __syncthreads();
+    float2 ms[WAVES];
+    float top = kFloor, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        ms[w] = stats[w * 32 + l32];
+        top = fmaxf(top, ms[w].x);
+    }
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        ms[w].x = exp2_fast(ms[w].x - top);
+        sum = fmaf(ms[w].y, ms[w].x, sum);
+    }
+    const Target t = target_of(a, blk, head, blk.rows0 + l32, nsp == 1, split, top, sum);
+    static_assert(4 % WAVES == 0, "a wavefront's share of the four channel blocks");
+#pragma unroll
+    for (int db = wave; db < 4; db += WAVES) {
+        f32x16 x = f32x16{};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float *from = (const float *)(smem + w * 2 * STAGES * SLOT) + l32 * PITCH + db * 32 + 4 * half;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 y = *(const float4 *)(from + 8 * k);
+                x[4 * k] = fmaf(y.x, ms[w].x, x[4 * k]);
+                x[4 * k + 1] = fmaf(y.y, ms[w].x, x[4 * k + 1]);
+                x[4 * k + 2] = fmaf(y.z, ms[w].x, x[4 * k + 2]);
+                x[4 * k + 3] = fmaf(y.w, ms[w].x, x[4 * k + 3]);
+            }
+        }
+        store_channels<DT>(a, t, db, x, half);
+    }
+    if (wave == 0) store_sum(a, t, half);
+}
+
+// ------------------------------------------------------------------------------------------------ merge of the ranges
+
+// A wavefront a row (token, head): out = sum_s 2^(e_s - E) o_s / sum_s 2^(e_s - E), E the largest e_s, in the order of the ranges.
+template <int DT, bool PAGED>
+__global__ __launch_bounds__(256) void merge_ranges(const AttnArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (row >= (int64_t)a.T * a.Hq) return;
+    const int token = (int)(row / a.Hq), head = (int)(row - (int64_t)token * a.Hq);
+    int seq = 0;
+    for (int base = 0; base < a.n_seq; base += 64) {
+        const int s = base + lane;
+        const unsigned long long past = __ballot(s < a.n_seq && clampi(a.cu_q[s + 1], 0, a.T) > token);
+        if (past) {
+            seq = base + __builtin_ctzll(past);
+            break;
+        }
+    }
+    Block blk;
+    sequence_of<PAGED>(a, __builtin_amdgcn_readfirstlane(seq), blk);
+    if (token < blk.q0 || token >= blk.q0 + blk.q_len) return;  // a token of no sequence
+    const int r = (token - blk.q0) * a.G + head % a.G;
+    blk.rows0 = r / a.rows * a.rows;
+    tiles_of(a, blk, a.rows, a.tile);
+    const int nsp = splits_of(a, blk.nt);
+    if (nsp == 1) return;  // written already
+    const int64_t pitch = (int64_t)a.T * a.Hq;
+    float top = -INFINITY;
+    for (int s = lane; s < nsp; s += 64) top = fmaxf(top, a.part_e[s * pitch + row]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float sum = 0.f;
+    float2 x = make_float2(0.f, 0.f);
+    const float ref = top == -INFINITY ? 0.f : top;  // no range has a token that the row sees
+#pragma unroll 8
+    for (int s = 0; s < nsp; ++s) {
+        const float2 y = *(const float2 *)(a.part_o + (s * pitch + row) * kHeadDim + 2 * lane);
+        const float w = exp2_fast(a.part_e[s * pitch + row] - ref);
+        sum += w;
+        x.x = fmaf(w, y.x, x.x);
+        x.y = fmaf(w, y.y, x.y);
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    unsigned char *to = a.out + (int64_t)token * a.out_token + (int64_t)head * a.out_head;
+    if (DT == ILRE_F32)
+        *(float2 *)(to + 8 * lane) = make_float2(x.x * f, x.y * f);
+    else
+        *(unsigned *)(to + 4 * lane) = pack_bf16(x.x * f, x.y * f);
+    if (lane == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+}
+
+constexpr int kMaxLds = 136 * 1024;
+hipError_t raise_lds_limit_once(const void *kernel)
+{
+    static std::mutex mutex;
+    static const void *done[32];
+    static int ndone = 0;
+    std::lock_guard<std::mutex> lock(mutex);
+    for (int i = 0; i < ndone; ++i)
+        if (done[i] == kernel) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+    if (e == hipSuccess && ndone < 32) done[ndone++] = kernel;
+    return e;
+}
+
+template <typename K>
+hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const AttnArgs &a, hipStream_t s)
+{
+    const hipError_t e = raise_lds_limit_once((const void *)kernel);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.nsplit * p.nblocks * a.Hkv), dim3(threads), lds, s, a);
+    return hipGetLastError();
+}
+
+template <int DT, int WAVES, int NB, int TN, bool PAGED>
+hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
+{
+    return launch(attend_rows<DT, WAVES, NB, TN, PAGED>, p, WAVES * 64, 8 * TN * Elem<DT>::ROWB + 16, a, s);
+}
+
+template <bool PAGED>
+hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
+{
+    hipError_t e;
+    if (p.dtype == ILRE_BF16) {
+        if (p.rows == 32)
+            e = launch(attend_tokens<ILRE_BF16, 4, PAGED>, p, 256, 4 * 4 * 32 * 256 + 4 * 32 * sizeof(float2), a, s);
+        else if (p.rows == 128)
+            e = launch_rows<ILRE_BF16, 4, 1, 32, PAGED>(p, a, s);
+        else
+            e = launch_rows<ILRE_BF16, 8, 1, 64, PAGED>(p, a, s);
+    } else {
+        if (p.rows == 32)
+            e = launch(attend_tokens<ILRE_F32, 4, PAGED>, p, 256, 4 * 2 * 32 * 512 + 4 * 32 * sizeof(float2), a, s);
+        else
+            e = launch_rows<ILRE_F32, 4, 1, 32, PAGED>(p, a, s);
+    }
+    if (e != hipSuccess || p.nsplit == 1) return e;
+    const unsigned grid = (unsigned)(((int64_t)a.T * a.Hq + 3) / 4);
+    if (p.dtype == ILRE_BF16)
+        hipLaunchKernelGGL((merge_ranges<ILRE_BF16, PAGED>), dim3(grid), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((merge_ranges<ILRE_F32, PAGED>), dim3(grid), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
+{
+    AttnPlan p{};
+    p.dtype = dtype;
+    const int64_t G = Hq / Hkv, rows = (int64_t)max_q * G;
+    p.rows = rows <= 32 ? 32 : dtype == ILRE_F32 || rows <= 128 ? 128 : 256;
+    p.tile = p.rows == 32 ? 128 : p.rows == 128 ? 32 : 64;
+    // at most so many blocks, whatever the sequences' lengths
+    p.nblocks = (int)std::min(((int64_t)T * G + (int64_t)n_seq * (p.rows - 1)) / p.rows, (int64_t)T * G);
+    if (total_kv <= 0) total_kv = (int64_t)n_seq * max_kv;
+    auto tiles = [&](int64_t kv) {
+        const int64_t all = (kv + p.tile - 1) / p.tile;
+        if (window <= 0) return all;
+        return std::min(all, (std::min((int64_t)sink, kv) + p.tile - 1) / p.tile + (window + (p.rows + G - 1) / G) / p.tile + 2);
+    };
+    const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
+    const int64_t work = std::max<int64_t>((int64_t)p.nblocks * Hkv * tiles(total_kv / n_seq), 1);
+    const int64_t places = p.rows == 128 && dtype == ILRE_BF16 ? 2 * kNumCU : kNumCU;
+    int64_t per = std::max<int64_t>((work + places - 1) / places, p.rows == 32 ? 1 : 4);
+    int64_t n = (most + per - 1) / per;
+    const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);
+    n = std::max<int64_t>(1, std::min({n, (int64_t)256, (int64_t)(workspace / (size_t)row_bytes), (int64_t)0x7FFFFFFF / ((int64_t)p.nblocks * Hkv)}));
+    p.nsplit = (int)n;
+    p.split_tiles = (int)((most + n - 1) / n);
+    p.bytes = n == 1 ? 0 : (size_t)(n * row_bytes);
+    return p;
+}
+
+hipError_t launch_attention(const AttnPlan &p, AttnArgs a, void *workspace, hipStream_t s)
+{
+    a.nsplit = p.nsplit;
+    a.split_tiles = p.split_tiles;
+    a.nblocks = p.nblocks;
+    a.rows = p.rows;
+    a.tile = p.tile;
+    a.part_o = (float *)workspace;
+    a.part_e = a.part_o + (int64_t)p.nsplit * a.T * a.Hq * kHeadDim;
+    return a.table ? launch_kernels<true>(p, a, s) : launch_kernels<false>(p, a, s);
+}
+
+}  // namespace ilre

@@ -210,6 +210,61 @@ struct RopeArgs {
 
 hipError_t launch_rerope(const RopeArgs &a, int dtype, int pairing, hipStream_t s);
 
+// ---------------------------------------------------------------- rotary positions, fill of a paged cache
+
+struct TurnArgs {
+    const unsigned char *q, *k, *v;  // [T, heads, d]; each may be null
+    unsigned char *q_out;
+    int64_t q_token, q_head, out_token, out_head, k_token, k_head, v_token, v_head;  // bytes
+    const int32_t *positions;        // null: first_position + token, or the place in the cache
+    int T, Hq, Hkv, rotary, first_position;
+    float magnitude;
+    // the cache
+    unsigned char *k_pages, *v_pages;
+    int64_t page_bytes, head_bytes, token_bytes;
+    const int32_t *table, *kv_len, *cu_q;
+    int64_t table_stride, kv_limit;
+    int n_seq, num_pages, page_shift;
+    double turns[ILRE_HEAD_DIM / 2];  // of pair j, a position
+};
+
+hipError_t launch_turn(const TurnArgs &a, int dtype, int pairing, hipStream_t s);
+
+// ---------------------------------------------------------------- attention over a paged cache or packed keys and values
+
+struct AttnArgs {
+    const unsigned char *q, *k, *v;
+    unsigned char *out;
+    float *lse;
+    int64_t q_token, q_head, out_token, out_head, k_page, k_head, k_token, v_page, v_head, v_token;  // bytes
+    const int32_t *table, *kv_len;  // null: contiguous keys and values, cut up by cu_k
+    const int32_t *cu_q, *cu_k;
+    int64_t table_stride, kv_limit;
+    int table_width, page_shift, num_pages;
+    int T, Tk, n_seq, Hq, Hkv, G;
+    int causal, sink, window;
+    float c;  // scale * log2(e)
+    // the plan
+    int nsplit, split_tiles, nblocks, rows, tile;
+    float *part_o, *part_e;  // [nsplit][T * Hq][d], [nsplit][T * Hq]
+};
+
+// How a call is cut up: blocks of `rows` query rows a kv head (32: attend_tokens, otherwise attend_rows), tiles of `tile` tokens, up to nsplit ranges of
+// split_tiles tiles a block.
+struct AttnPlan {
+    int dtype, rows, tile, nblocks, nsplit, split_tiles;
+    size_t bytes;  // of workspace
+};
+
+AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
+hipError_t launch_attention(const AttnPlan &p, AttnArgs a, void *workspace, hipStream_t s);
+
+// ---------------------------------------------------------------- of api.hip, for the other entry points
+
+int fail(int status, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+int hip_fail(hipError_t e, const char *what);
+int check_opts(const ilre_opts *o);
+
 // ---------------------------------------------------------------- measurement aid: MFMA ceiling probes
 
 int probe_variants();
