@@ -16,6 +16,7 @@
 // keeps it: any m gives the same quotient as long as the exponentials stay in range, and the maximum, the rescaling and the branch in
 // front of it are a fifth of the vector work.  A row whose later logits exceed its reference by more than 2^60 shows in its
 // sum, and the workgroup walks its tiles again, following the maximum all the way.
+#include "attn_blocks.h"
 #include "ilre_internal.h"
 
 #include <math.h>
@@ -62,52 +63,23 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b)  // nearest even
 
 // ------------------------------------------------------------------------------------------------ which rows, which tiles
 
-// The rows of one workgroup, and the tokens they see.  All of it is the same for the whole wavefront.
-struct Block {
-    int seq, rows0, nrows;  // rows0: first row within the sequence; nrows: rows of the sequence
-    int q0, q_len;          // first new token in the packed order
-    int kv, kv0;            // tokens in the sequence; first one in the packed order (contiguous keys)
-    int lo, hi;             // tokens that a row of this block may see: [0, sink) and [lo, hi)
-    int sink;               // of the sink part, what lies before lo
-    int ns, w0, nt;         // tiles [0, ns) and [w0, w0 + nt - ns)
-    int all_lo, all_hi;     // tokens that every row of this block sees: [all_lo, all_hi)
-};
-
-__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+// All of a Block is the same for the whole wavefront.
+__device__ __forceinline__ Mask mask_of(const AttnArgs &a) { return Mask{a.causal, a.sink, a.window}; }
 
 template <bool PAGED>
 __device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b)
 {
     b.seq = seq;
-    b.q0 = clampi(scalar_i32(a.cu_q + seq), 0, a.T);
-    b.q_len = clampi(scalar_i32(a.cu_q + seq + 1), b.q0, a.T) - b.q0;
+    b.q0 = clamp_to(scalar_i32(a.cu_q + seq), 0, a.T);
+    b.q_len = clamp_to(scalar_i32(a.cu_q + seq + 1), b.q0, a.T) - b.q0;
     if (PAGED) {
         b.kv0 = 0;
         b.kv = (int)min((int64_t)max(scalar_i32(a.kv_len + seq), 0), a.kv_limit);
     } else {
-        b.kv0 = clampi(scalar_i32(a.cu_k + seq), 0, a.Tk);
-        b.kv = clampi(scalar_i32(a.cu_k + seq + 1), b.kv0, a.Tk) - b.kv0;
+        b.kv0 = clamp_to(scalar_i32(a.cu_k + seq), 0, a.Tk);
+        b.kv = clamp_to(scalar_i32(a.cu_k + seq + 1), b.kv0, a.Tk) - b.kv0;
     }
     b.nrows = b.q_len * a.G;
-}
-
-// Tiles of `tn` tokens that the rows rows0 .. rows0 + rows - 1 see something of.
-__device__ __forceinline__ void tiles_of(const AttnArgs &a, Block &b, int rows, int tn)
-{
-    const int first = b.rows0 / a.G, last = min(b.rows0 + rows, b.nrows) - 1;
-    const int64_t p0 = (int64_t)b.kv - b.q_len + first, p1 = (int64_t)b.kv - b.q_len + last / a.G;
-    b.hi = a.causal ? (int)min(max(p1 + 1, (int64_t)0), (int64_t)b.kv) : b.kv;
-    b.all_hi = a.causal ? (int)min(max(p0 + 1, (int64_t)0), (int64_t)b.kv) : b.kv;
-    b.lo = b.all_lo = b.sink = 0;
-    if (a.window > 0) {
-        b.lo = (int)min(max(p0 - a.window + 1, (int64_t)0), (int64_t)b.hi);
-        b.all_lo = (int)max(p1 - a.window + 1, (int64_t)0);
-        b.sink = min(a.sink, b.lo);
-    }
-    const int end = (b.hi + tn - 1) / tn;
-    b.ns = min((b.sink + tn - 1) / tn, end);
-    b.w0 = max(b.lo / tn, b.ns);
-    b.nt = b.hi > 0 ? b.ns + max(end - b.w0, 0) : 0;
 }
 
 // Workgroup w's block of `rows` rows: the blocks of all sequences one after the other, within a sequence the last one first (with a causal
@@ -123,8 +95,8 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int w, int rows, B
             const int s = base + lane;
             int n = 0;
             if (s < a.n_seq) {
-                const int from = clampi(a.cu_q[s], 0, a.T);
-                n = ((clampi(a.cu_q[s + 1], from, a.T) - from) * a.G + rows - 1) / rows;
+                const int from = clamp_to(a.cu_q[s], 0, a.T);
+                n = ((clamp_to(a.cu_q[s + 1], from, a.T) - from) * a.G + rows - 1) / rows;
             }
             int sum = n;
 #pragma unroll
@@ -152,12 +124,6 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int w, int rows, B
     return true;
 }
 
-// Into how many ranges of tiles a block's list is cut: the same answer here, in the merge and on the host.
-__device__ __forceinline__ int splits_of(const AttnArgs &a, int nt)
-{
-    return a.nsplit == 1 || nt <= a.split_tiles ? 1 : min(a.nsplit, (nt + a.split_tiles - 1) / a.split_tiles);
-}
-
 // ------------------------------------------------------------------------------------------------ tile copies
 
 // Where a kv head's keys (or values) lie, and the part of a tile that one wavefront copies: `rows` consecutive tokens, 16 at most and
@@ -170,8 +136,7 @@ struct Source {
 // A page's number, clamped to the table; -1 where the entry names no page (its tokens count as absent).
 __device__ __forceinline__ int page_of(const AttnArgs &a, const Block &b, int tok)
 {
-    const int at = min(tok >> a.page_shift, a.table_width - 1);
-    const int id = scalar_i32(a.table + (int64_t)b.seq * a.table_stride + at);
+    const int id = scalar_i32(a.table + (int64_t)b.seq * a.table_stride + page_column(tok, a.page_shift, a.table_width));
     return (unsigned)id < (unsigned)a.num_pages ? id : -1;
 }
 
@@ -184,7 +149,7 @@ __device__ __forceinline__ void copy_rows(const AttnArgs &a, const Block &b, con
 {
     constexpr int N = ROWS * ROWB / 1024, PER = 1024 / ROWB;
     uint64_t at;
-    int n = clampi(b.hi - tok, 0, ROWS);
+    int n = clamp_to(b.hi - tok, 0, ROWS);
     if (PAGED) {
         at = src.base + (uint64_t)((int64_t)max(page, 0) * src.page + (int64_t)(tok & ((1 << a.page_shift) - 1)) * src.token);
         if (page < 0) n = 0;
@@ -492,7 +457,7 @@ __device__ __forceinline__ bool pages_missing(const AttnArgs &a, const Block &b,
     bool missing = false;
     if (from < to) {
         const int32_t *t = a.table + (int64_t)b.seq * a.table_stride;
-        const int last = min((to - 1) >> a.page_shift, a.table_width - 1);
+        const int last = page_column(to - 1, a.page_shift, a.table_width);
         for (int i = (from >> a.page_shift) + tid; i <= last; i += threads) missing = missing || (unsigned)t[i] >= (unsigned)a.num_pages;
     }
     return missing;
@@ -516,11 +481,11 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
     const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, split = rest / a.nblocks;
     Block blk;
     if (!find_block<PAGED>(a, rest - split * a.nblocks, ROWS, blk)) return;
-    tiles_of(a, blk, ROWS, TN);
-    const int nsp = splits_of(a, blk.nt);
+    tiles_of(blk, mask_of(a), a.G, ROWS, TN);
+    const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     if (split >= nsp) return;
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
-    auto token_of = [&](int i) { return (first + i < blk.ns ? first + i : first + i - blk.ns + blk.w0) * TN; };
+    auto token_of = [&](int i) { return tile_token(blk, first + i, TN); };
 
     State<DT, NB> st;
     const int row0 = blk.rows0 + wave * NB * 32;
@@ -639,11 +604,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
     const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, split = rest / a.nblocks;
     Block blk;
     if (!find_block<PAGED>(a, rest - split * a.nblocks, 32, blk)) return;
-    tiles_of(a, blk, 32, TN);
-    const int nsp = splits_of(a, blk.nt);
+    tiles_of(blk, mask_of(a), a.G, 32, TN);
+    const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     if (split >= nsp) return;
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
-    auto token_of = [&](int i) { return (first + i < blk.ns ? first + i : first + i - blk.ns + blk.w0) * TN + wave * 32; };
+    auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
 
     State<DT, 1> st;
     st.load(a, blk, head, blk.rows0, l32, half);
@@ -778,7 +743,7 @@ __global__ __launch_bounds__(256) void merge_ranges(const AttnArgs a)
     int seq = 0;
     for (int base = 0; base < a.n_seq; base += 64) {
         const int s = base + lane;
-        const unsigned long long past = __ballot(s < a.n_seq && clampi(a.cu_q[s + 1], 0, a.T) > token);
+        const unsigned long long past = __ballot(s < a.n_seq && clamp_to(a.cu_q[s + 1], 0, a.T) > token);
         if (past) {
             seq = base + __builtin_ctzll(past);
             break;
@@ -789,8 +754,8 @@ __global__ __launch_bounds__(256) void merge_ranges(const AttnArgs a)
     if (token < blk.q0 || token >= blk.q0 + blk.q_len) return;  // a token of no sequence
     const int r = (token - blk.q0) * a.G + head % a.G;
     blk.rows0 = r / a.rows * a.rows;
-    tiles_of(a, blk, a.rows, a.tile);
-    const int nsp = splits_of(a, blk.nt);
+    tiles_of(blk, mask_of(a), a.G, a.rows, a.tile);
+    const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     if (nsp == 1) return;  // written already
     const int64_t pitch = (int64_t)a.T * a.Hq;
     float top = -INFINITY;
