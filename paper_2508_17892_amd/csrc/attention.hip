@@ -37,6 +37,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 namespace {
 
 constexpr float kFloor = -1.0e30f;            // reference of a row that has seen nothing, in base-2 units
+constexpr float kSumLimit = 1.152921504606847e18f;  // 2^60: a sum against a kept reference beyond this is made again
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -388,6 +389,20 @@ struct State {
             Elem<DT>::pack(w[b], p);
         }
     }
+    // The same against the references as they are, all tokens seen.
+    __device__ __forceinline__ void weigh_kept(const f32x16 (&s)[NB], typename Elem<DT>::Weights (&w)[NB], float c)
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = exp2_fast(fmaf(s[b][i], c, -m[b]));
+                z[b][i & 3] += p[i];
+            }
+            Elem<DT>::pack(w[b], p);
+        }
+    }
     __device__ __forceinline__ float sum(int b) const
     {
         const float x = (z[b][0] + z[b][1]) + (z[b][2] + z[b][3]);
@@ -573,10 +588,93 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
         }
     };
 
+    // Tiles g1 .. g2 - 1, which all rows see whole, against the references that the tiles before have left.  32 tokens are a step, and a step holds three
+    // stages that do not wait for each other: the logits of the next 32 tokens, these ones' weights, the product of the weights before with their values.
+    auto kept_step = [&](f32x16 (&now)[NB], f32x16 (&next)[NB], typename E::Weights (&w)[NB], unsigned kat, unsigned vat) {
+        typename E::Weights wn[NB];
+        E::template logits<NB>(next, st.q, ad, kat);
+        E::template values<NB>(st.o, w, ad, vat);
+        st.weigh_kept(now, wn, a.c);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) w[b] = wn[b];
+        if (DT == ILRE_BF16) {
+#pragma unroll
+            for (int k = 0; k < 16 * NB; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            }
+        }
+    };
+    auto keys_at = [&](int i, int sub) { return lds0 + (i & 3) * SLOT + sub * 32 * ROWB; };
+    auto values_at = [&](int i, int sub) { return lds0 + (4 + (i & 3)) * SLOT + sub * 32 * ROWB; };
+    auto kept_tiles = [&](int g1, int g2) {
+        if (idle) {
+            for (int i = g1; i < g2; ++i) advance(i);
+            return;
+        }
+        f32x16 s[2][NB];
+        typename E::Weights w[NB];
+        E::template logits<NB>(s[0], st.q, ad, keys_at(g1, 0));
+        advance(g1);
+        // the first step has no weights before it
+        if (SUB == 2) {
+            E::template logits<NB>(s[1], st.q, ad, keys_at(g1, 1));
+            st.weigh_kept(s[0], w, a.c);
+            kept_step(s[1], s[0], w, keys_at(g1 + 1, 0), values_at(g1, 0));
+            for (int i = g1 + 1; i < g2; ++i) {
+                advance(i);
+                kept_step(s[0], s[1], w, keys_at(i, 1), values_at(i - 1, 1));
+                kept_step(s[1], s[0], w, keys_at(i + 1, 0), values_at(i, 0));
+            }
+        } else {
+            E::template logits<NB>(s[1], st.q, ad, keys_at(g1 + 1, 0));
+            st.weigh_kept(s[0], w, a.c);
+            int i = g1 + 1;
+            for (; i + 1 < g2; i += 2) {
+                advance(i);
+                kept_step(s[1], s[0], w, keys_at(i + 1, 0), values_at(i - 1, 0));
+                advance(i + 1);
+                kept_step(s[0], s[1], w, keys_at(i + 2, 0), values_at(i, 0));
+            }
+            if (i < g2) {
+                advance(i);
+                kept_step(s[1], s[0], w, keys_at(i + 1, 0), values_at(i - 1, 0));
+            }
+        }
+        E::template values<NB>(st.o, w, ad, values_at(g2 - 1, SUB - 1));
+    };
+
     if (count > 0) {
+        // behind the first tile that all rows see whole, as far as they do
+        int g1 = count, g2 = count;
+        if (DT == ILRE_BF16 && !careful) {
+            const int from = a.window > 0 ? max((blk.all_lo + TN - 1) / TN, blk.w0) - blk.w0 + blk.ns : 0;
+            const int to = a.window > 0 ? blk.all_hi / TN - blk.w0 + blk.ns : blk.all_hi / TN;
+            g1 = max(from - first, 0) + 1;
+            g2 = min(to - first, count);
+            if (g2 - g1 < 2) g1 = g2 = count;
+        }
         begin();
-        for (int i = 0; i < count; ++i) follow_tile(i);
+        for (int i = 0; i < g1; ++i) follow_tile(i);
+        if (g1 < g2) kept_tiles(g1, g2);
+        for (int i = g2; i < count; ++i) follow_tile(i);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (g1 < g2) {
+            bool far = false;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) far = far || !(st.z[b][k] <= kSumLimit);
+            if (!idle && far) *flag = 1;
+            __syncthreads();
+            if (__builtin_amdgcn_readfirstlane(*flag)) {
+                st.clear();
+                begin();
+                for (int i = 0; i < count; ++i) follow_tile(i);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+        }
     }
     if (idle) return;
 #pragma unroll
