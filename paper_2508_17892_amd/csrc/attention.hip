@@ -53,9 +53,9 @@ __device__ __forceinline__ u32x2 lds_read_tr(unsigned at)
 {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(size_t)at));
 }
-// Table entries and lengths: the same for the whole wavefront and not written while the kernel runs, so that they come through the
-// scalar cache, outside the count of vector loads that the tile copies are waited for by.
-__device__ __forceinline__ int scalar_i32(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
+// Table entries and lengths: not written while the kernel runs.  Where the address is the same for the whole wavefront they come through the scalar cache,
+// outside the count of vector loads that the tile copies are waited for by.
+__device__ __forceinline__ int read_i32(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
 
 __device__ __forceinline__ unsigned pack_bf16(float a, float b)  // nearest even
 {
@@ -71,14 +71,14 @@ template <bool PAGED>
 __device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b)
 {
     b.seq = seq;
-    b.q0 = clamp_to(scalar_i32(a.cu_q + seq), 0, a.T);
-    b.q_len = clamp_to(scalar_i32(a.cu_q + seq + 1), b.q0, a.T) - b.q0;
+    b.q0 = clamp_to(read_i32(a.cu_q + seq), 0, a.T);
+    b.q_len = clamp_to(read_i32(a.cu_q + seq + 1), b.q0, a.T) - b.q0;
     if (PAGED) {
         b.kv0 = 0;
-        b.kv = (int)min((int64_t)max(scalar_i32(a.kv_len + seq), 0), a.kv_limit);
+        b.kv = (int)min((int64_t)max(read_i32(a.kv_len + seq), 0), a.kv_limit);
     } else {
-        b.kv0 = clamp_to(scalar_i32(a.cu_k + seq), 0, a.Tk);
-        b.kv = clamp_to(scalar_i32(a.cu_k + seq + 1), b.kv0, a.Tk) - b.kv0;
+        b.kv0 = clamp_to(read_i32(a.cu_k + seq), 0, a.Tk);
+        b.kv = clamp_to(read_i32(a.cu_k + seq + 1), b.kv0, a.Tk) - b.kv0;
     }
     b.nrows = b.q_len * a.G;
 }
@@ -137,7 +137,7 @@ struct Source {
 // A page's number, clamped to the table; -1 where the entry names no page (its tokens count as absent).
 __device__ __forceinline__ int page_of(const AttnArgs &a, const Block &b, int tok)
 {
-    const int id = scalar_i32(a.table + (int64_t)b.seq * a.table_stride + page_column(tok, a.page_shift, a.table_width));
+    const int id = read_i32(a.table + (int64_t)b.seq * a.table_stride + page_column(tok, a.page_shift, a.table_width));
     return (unsigned)id < (unsigned)a.num_pages ? id : -1;
 }
 
@@ -215,18 +215,11 @@ struct Elem<ILRE_BF16> {
                 v[db] = (4 * half + (l16 >> 2)) * ROWB + ((db ^ (l16 >> 2)) * 64) + ((lane >> 4) & 1) * 32 + (l16 & 3) * 8;
         }
     };
-    template <int NB>
-    static __device__ __forceinline__ void logits(f32x16 (&s)[NB], const uint4 (&q)[NB][QREGS], const Addr &ad, unsigned kat)
+    static __device__ __forceinline__ void logits(f32x16 &s, const uint4 (&q)[QREGS], const Addr &ad, unsigned kat)
     {
+        s = f32x16{};
 #pragma unroll
-        for (int st = 0; st < 8; ++st) {
-            const uint4 kf = lds_read16(ad.k[st] + kat);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                if (st == 0) s[b] = f32x16{};
-                mma(s[b], kf, q[b][st]);
-            }
-        }
+        for (int st = 0; st < 8; ++st) mma(s, lds_read16(ad.k[st] + kat), q[st]);
     }
     // The weights are rounded to bf16 for the product with V, like V itself; their sum is taken before.
     static __device__ __forceinline__ void pack(Weights &w, const float (&p)[16])
@@ -237,17 +230,14 @@ struct Elem<ILRE_BF16> {
         w.p[0] = make_uint4(u[0], u[1], u[2], u[3]);
         w.p[1] = make_uint4(u[4], u[5], u[6], u[7]);
     }
-    template <int NB>
-    static __device__ __forceinline__ void values(f32x16 (&o)[NB][4], const Weights (&w)[NB], const Addr &ad, unsigned vat)
+    static __device__ __forceinline__ void values(f32x16 (&o)[4], const Weights &w, const Addr &ad, unsigned vat)
     {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
                 const u32x2 x = lds_read_tr(ad.v[db] + vat + ks * 16 * ROWB), y = lds_read_tr(ad.v[db] + vat + (ks * 16 + 8) * ROWB);
-                const uint4 vf = make_uint4(x[0], x[1], y[0], y[1]);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) mma(o[b][db], vf, w[b].p[ks]);
+                mma(o[db], make_uint4(x[0], x[1], y[0], y[1]), w.p[ks]);
             }
     }
 };
@@ -270,21 +260,15 @@ struct Elem<ILRE_F32> {
             for (int j = 0; j < 4; ++j) v[j] = 4 * half * ROWB + j * ROWB + (((l32 >> 2) ^ ((j & 1) << 2)) * 16) + (l32 & 3) * 4;
         }
     };
-    template <int NB>
-    static __device__ __forceinline__ void logits(f32x16 (&s)[NB], const uint4 (&q)[NB][QREGS], const Addr &ad, unsigned kat)
+    static __device__ __forceinline__ void logits(f32x16 &s, const uint4 (&q)[QREGS], const Addr &ad, unsigned kat)
     {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+        s = f32x16{};
 #pragma unroll
         for (int st = 0; st < 16; ++st) {
             const uint4 kf = lds_read16(ad.k[st] + kat);
-            const unsigned k[4] = {kf.x, kf.y, kf.z, kf.w};
+            const unsigned k[4] = {kf.x, kf.y, kf.z, kf.w}, x[4] = {q[st].x, q[st].y, q[st].z, q[st].w};
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const unsigned x[4] = {q[b][st].x, q[b][st].y, q[b][st].z, q[b][st].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(x[e]), s[b], 0, 0, 0);
-            }
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(x[e]), s, 0, 0, 0);
         }
     }
     static __device__ __forceinline__ void pack(Weights &w, const float (&p)[16])
@@ -292,8 +276,7 @@ struct Elem<ILRE_F32> {
 #pragma unroll
         for (int i = 0; i < 16; ++i) w.p[i] = p[i];
     }
-    template <int NB>
-    static __device__ __forceinline__ void values(f32x16 (&o)[NB][4], const Weights (&w)[NB], const Addr &ad, unsigned vat)
+    static __device__ __forceinline__ void values(f32x16 (&o)[4], const Weights &w, const Addr &ad, unsigned vat)
     {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -301,111 +284,92 @@ struct Elem<ILRE_F32> {
             for (int db = 0; db < 4; ++db) {
                 // chunk (8 db + l32 / 4) ^ (i % 4 << 2): the upper bit of the XOR picks another channel block
                 const float v = lds_read4(ad.v[i & 3] + vat + (i >> 2) * 8 * ROWB + (db ^ ((i & 3) >> 1)) * 128);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) o[b][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[b].p[i], o[b][db], 0, 0, 0);
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.p[i], o[db], 0, 0, 0);
             }
     }
 };
 
-// One row of a lane and what it sees.
-struct Row {
-    int lo, hi;  // [0, sink) and [lo, hi)
-};
-
-// A wavefront's running state for NB x 32 rows.
-template <int DT, int NB>
+// A wavefront's running state for 32 rows; a lane and its partner 32 lanes on have row l32, the tokens of each 32 between them.
+template <int DT>
 struct State {
-    uint4 q[NB][Elem<DT>::QREGS];
-    f32x16 o[NB][4];
-    float m[NB], z[NB][4];
-    Row row[NB];
+    using E = Elem<DT>;
+    uint4 q[E::QREGS];
+    f32x16 o[4];
+    float m, z[4];
+    int lo, hi;  // the row sees [0, sink) and [lo, hi)
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-#pragma unroll
-            for (int db = 0; db < 4; ++db) o[b][db] = f32x16{};
-            m[b] = kFloor;
-            z[b][0] = z[b][1] = z[b][2] = z[b][3] = 0.f;
-        }
+        for (int db = 0; db < 4; ++db) o[db] = f32x16{};
+        m = kFloor;
+        z[0] = z[1] = z[2] = z[3] = 0.f;
     }
-    // Query rows row0 + 32 b + l32 of the sequence; past the last one zeros, which see what the last one sees and are written nowhere.
+    // Query row row0 + l32 of the sequence; past the last one zeros, which see what the last one sees and are written nowhere.
     __device__ __forceinline__ void load(const AttnArgs &a, const Block &blk, int head_kv, int row0, int l32, int half)
     {
+        const int want = row0 + l32, r = min(want, blk.nrows - 1);
+        const int i = r / a.G, g = r - i * a.G;
+        const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head_kv * a.G + g) * a.q_head + half * 16;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int want = row0 + 32 * b + l32, r = min(want, blk.nrows - 1);
-            const int i = r / a.G, g = r - i * a.G;
-            const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head_kv * a.G + g) * a.q_head + half * 16;
+        for (int st = 0; st < E::QREGS; ++st) q[st] = *(const uint4 *)(src + st * 32);
+        // waited for here, not in the loop over tiles, where that would be a wait for the tile copies as well
 #pragma unroll
-            for (int st = 0; st < Elem<DT>::QREGS; ++st) q[b][st] = *(const uint4 *)(src + st * 32);
-            // waited for here, not in the loop over tiles, where that would be a wait for the tile copies as well
+        for (int st = 0; st < E::QREGS; ++st) asm volatile("" : "+v"(q[st].x), "+v"(q[st].y), "+v"(q[st].z), "+v"(q[st].w));
+        if (want != r) {
 #pragma unroll
-            for (int st = 0; st < Elem<DT>::QREGS; ++st) asm volatile("" : "+v"(q[b][st].x), "+v"(q[b][st].y), "+v"(q[b][st].z), "+v"(q[b][st].w));
-            if (want != r) {
-#pragma unroll
-                for (int st = 0; st < Elem<DT>::QREGS; ++st) q[b][st] = make_uint4(0, 0, 0, 0);
-            }
-            const int p = blk.kv - blk.q_len + i;
-            row[b].hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
-            row[b].lo = a.window > 0 ? p - a.window + 1 : 0;
+            for (int st = 0; st < E::QREGS; ++st) q[st] = make_uint4(0, 0, 0, 0);
         }
+        const int p = blk.kv - blk.q_len + i;
+        hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
+        lo = a.window > 0 ? p - a.window + 1 : 0;
     }
-    // The logits of 32 tokens from `tok` on become weights; the running maximum is followed.  `absent`: bit 0 / 1: the first / last 16 are on no page.
-    template <bool MASKED>
-    __device__ __forceinline__ void weigh(f32x16 (&s)[NB], typename Elem<DT>::Weights (&w)[NB], float c, int tok, int sink, int half, int absent)
+    // The logits of SUB x 32 tokens from `tok` on become weights; the running maximum is followed.  `absent`: bit k: tokens 16 k .. 16 k + 15 are on no page.
+    template <bool MASKED, int SUB>
+    __device__ __forceinline__ void weigh(f32x16 (&s)[SUB], typename E::Weights (&w)[SUB], float c, int tok, int sink, int half, int absent)
     {
+        float top = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
+        for (int u = 0; u < SUB; ++u) {
             if (MASKED) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int t = tok + 8 * (i >> 2) + 4 * half + (i & 3);
-                    const bool seen = t < row[b].hi && (t >= row[b].lo || t < sink) && !(absent >> (i >> 3) & 1);
-                    s[b][i] = seen ? s[b][i] : -INFINITY;
+                    const int t = tok + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3);
+                    const bool seen = t < hi && (t >= lo || t < sink) && !(absent >> (2 * u + (i >> 3)) & 1);
+                    s[u][i] = seen ? s[u][i] : -INFINITY;
                 }
             }
-            float top = s[b][0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
-            top = fmaxf(top, other_half(top));
-            const float mnew = fmaxf(m[b], top * c);
-            if (__ballot(mnew != m[b])) {
-                const float f = exp2_fast(m[b] - mnew);
-#pragma unroll
-                for (int db = 0; db < 4; ++db)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[b][db][i] *= f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) z[b][k] *= f;
-                m[b] = mnew;
-            }
-            float p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = exp2_fast(fmaf(s[b][i], c, -m[b]));
-                z[b][i & 3] += p[i];
-            }
-            Elem<DT>::pack(w[b], p);
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
         }
-    }
-    // The same against the references as they are, all tokens seen.
-    __device__ __forceinline__ void weigh_kept(const f32x16 (&s)[NB], typename Elem<DT>::Weights (&w)[NB], float c)
-    {
+        top = fmaxf(top, other_half(top));
+        const float mnew = fmaxf(m, top * c);
+        if (__ballot(mnew != m)) {
+            const float f = exp2_fast(m - mnew);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            float p[16];
+            for (int db = 0; db < 4; ++db)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = exp2_fast(fmaf(s[b][i], c, -m[b]));
-                z[b][i & 3] += p[i];
-            }
-            Elem<DT>::pack(w[b], p);
+                for (int i = 0; i < 16; ++i) o[db][i] *= f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] *= f;
+            m = mnew;
         }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) weigh_kept(s[u], w[u], c);
     }
-    __device__ __forceinline__ float sum(int b) const
+    // The same against the reference as it is, all tokens seen.
+    __device__ __forceinline__ void weigh_kept(const f32x16 &s, typename E::Weights &w, float c)
     {
-        const float x = (z[b][0] + z[b][1]) + (z[b][2] + z[b][3]);
+        float p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = exp2_fast(fmaf(s[i], c, -m));
+            z[i & 3] += p[i];
+        }
+        E::pack(w, p);
+    }
+    __device__ __forceinline__ float sum() const
+    {
+        const float x = (z[0] + z[1]) + (z[2] + z[3]);
         return x + other_half(x);
     }
 };
@@ -466,27 +430,16 @@ __device__ __forceinline__ void store_sum(const AttnArgs &a, const Target &t, in
         a.lse[t.row] = t.e * kLn2;
 }
 
-// Whether an entry of the page table between tokens `from` and `to` names no page.
-__device__ __forceinline__ bool pages_missing(const AttnArgs &a, const Block &b, int from, int to, int tid, int threads)
-{
-    bool missing = false;
-    if (from < to) {
-        const int32_t *t = a.table + (int64_t)b.seq * a.table_stride;
-        const int last = page_column(to - 1, a.page_shift, a.table_width);
-        for (int i = (from >> a.page_shift) + tid; i <= last; i += threads) missing = missing || (unsigned)t[i] >= (unsigned)a.num_pages;
-    }
-    return missing;
-}
-
 // ------------------------------------------------------------------------------------------------ many rows
 
-// WAVES wavefronts of NB x 32 rows share the tiles of TN tokens.  Keys and values have four tile buffers each; while tile i is worked on, its values, the
-// keys of tile i + 1 and (in the pipelined loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.
-template <int DT, int WAVES, int NB, int TN, bool PAGED>
-__global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void attend_rows(const AttnArgs a)
+// WAVES / TS groups of 32 rows share the tiles of TN tokens; with TS = 2 two wavefronts have the same rows and a half of each tile's tokens, and add up what
+// they have at the end.  Keys and values have four tile buffers each; while tile i is worked on, its values, the keys of tile i + 1 and (in the pipelined
+// loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.
+template <int DT, int WAVES, int TS, int TN, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_rows(const AttnArgs a)
 {
     using E = Elem<DT>;
-    constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, ROWS = WAVES * NB * 32, SUB = TN / 32;
+    constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, GROUPS = WAVES / TS, ROWS = GROUPS * 32, SUB = TN / 32 / TS;
     constexpr int CROWS = TN / WAVES, COPIES = CROWS * ROWB / 1024;  // a wavefront's rows and copies of a tile
     static_assert(CROWS <= 16 && CROWS * ROWB % 1024 == 0 && TN % 32 == 0, "a wavefront's rows lie on one page");
     extern __shared__ __align__(16) unsigned char smem[];
@@ -502,32 +455,17 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN); };
 
-    State<DT, NB> st;
-    const int row0 = blk.rows0 + wave * NB * 32;
+    State<DT> st;
+    const int row0 = blk.rows0 + wave % GROUPS * 32, part = wave / GROUPS * SUB * 32;  // its rows, and where its part of a tile begins
     const bool idle = row0 >= blk.nrows;
-    st.load(a, blk, head, row0, l32, half);
-    st.clear();
 
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem;
     typename E::Addr ad;
     ad.init(lane);
-    bool careful = false;
+    // Set where a kept reference turns out too low, or an entry of the table names no page: then the tiles are walked again, with care.
     int *flag = (int *)(smem + 8 * SLOT);
     if (tid == 0) *flag = 0;
     __syncthreads();
-    if (PAGED && count > 0) {
-        const int from = token_of(0), to = min(token_of(count - 1) + TN, blk.hi);
-        bool missing;
-        if (first < blk.ns)
-            missing = pages_missing(a, blk, from, min(blk.sink, to), tid, WAVES * 64) || pages_missing(a, blk, blk.lo, to, tid, WAVES * 64);
-        else
-            missing = pages_missing(a, blk, max(from, blk.lo), to, tid, WAVES * 64);
-        if (missing) *flag = 1;
-        __syncthreads();
-        careful = __builtin_amdgcn_readfirstlane(*flag) != 0;
-        __syncthreads();
-        if (tid == 0) *flag = 0;
-    }
 
     Source ks, vs;
     ks.base = (uint64_t)a.k + (uint64_t)((int64_t)head * a.k_head + (int64_t)blk.kv0 * a.k_token);
@@ -538,7 +476,12 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
     copy_offsets<CROWS, ROWB, true>(vvoff, wave * CROWS, a.v_token, lane);
     int pages[2];  // of this wavefront's rows: of the last tile whose keys were asked for, and the next one
     auto own_token = [&](int i) { return i < count ? token_of(i) + wave * CROWS : blk.hi; };
-    auto lookup = [&](int i) { return PAGED ? page_of(a, blk, min(own_token(i), blk.hi - 1)) : 0; };
+    auto lookup = [&](int i) {
+        if (!PAGED) return 0;
+        const int t = min(own_token(i), blk.hi - 1), page = page_of(a, blk, t);
+        if (page < 0 && (t + CROWS > blk.lo || t < blk.sink)) *flag = 1;
+        return page;
+    };
     auto copy_keys = [&](int i, int page) {
         copy_rows<CROWS, ROWB, false, PAGED>(a, blk, ks, own_token(i), page, lds0 + (i & 3) * SLOT + wave * CROWS * ROWB, kvoff, lane);
     };
@@ -565,61 +508,58 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
         pages[0] = pages[1];
         pages[1] = lookup(i + 4);
     };
-    auto follow_tile = [&](int i) {
+    auto keys_at = [&](int i, int sub) { return lds0 + (i & 3) * SLOT + (part + sub * 32) * ROWB; };
+    auto values_at = [&](int i, int sub) { return lds0 + (4 + (i & 3)) * SLOT + (part + sub * 32) * ROWB; };
+    auto follow_tile = [&](int i, bool careful) {
         advance(i);
         if (idle) return;
-        const int tok = token_of(i);
-        const bool whole = !careful && tok + TN <= blk.all_hi && tok >= blk.all_lo;
-#pragma unroll 1
-        for (int sub = 0; sub < SUB; ++sub) {
-            const unsigned kat = lds0 + (i & 3) * SLOT + sub * 32 * ROWB, vat = lds0 + (4 + (i & 3)) * SLOT + sub * 32 * ROWB;
-            const int t = tok + sub * 32;
-            f32x16 s[NB];
-            typename E::Weights w[NB];
-            E::template logits<NB>(s, st.q, ad, kat);
-            if (whole) {
-                st.template weigh<false>(s, w, a.c, t, a.sink, half, 0);
-            } else {
-                int absent = 0;
-                if (PAGED && careful) absent = (page_of(a, blk, t) < 0 ? 1 : 0) | (page_of(a, blk, t + 16) < 0 ? 2 : 0);
-                st.template weigh<true>(s, w, a.c, t, a.sink, half, absent);
+        const int tok = token_of(i) + part;
+        f32x16 s[SUB];
+        typename E::Weights w[SUB];
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub) E::logits(s[sub], st.q, ad, keys_at(i, sub));
+        if (!careful && tok + SUB * 32 <= blk.all_hi && tok >= blk.all_lo) {
+            st.template weigh<false, SUB>(s, w, a.c, tok, a.sink, half, 0);
+        } else {
+            int absent = 0;
+            if (PAGED && careful) {
+                for (int k = 0; k < SUB * 2; ++k) absent |= (page_of(a, blk, tok + 16 * k) < 0 ? 1 : 0) << k;
             }
-            E::template values<NB>(st.o, w, ad, vat);
+            st.template weigh<true, SUB>(s, w, a.c, tok, a.sink, half, absent);
         }
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub) E::values(st.o, w[sub], ad, values_at(i, sub));
     };
 
     // Tiles g1 .. g2 - 1, which all rows see whole, against the references that the tiles before have left.  32 tokens are a step, and a step holds three
     // stages that do not wait for each other: the logits of the next 32 tokens, these ones' weights, the product of the weights before with their values.
-    auto kept_step = [&](f32x16 (&now)[NB], f32x16 (&next)[NB], typename E::Weights (&w)[NB], unsigned kat, unsigned vat) {
-        typename E::Weights wn[NB];
-        E::template logits<NB>(next, st.q, ad, kat);
-        E::template values<NB>(st.o, w, ad, vat);
+    auto kept_step = [&](f32x16 &now, f32x16 &next, typename E::Weights &w, unsigned kat, unsigned vat) {
+        typename E::Weights wn;
+        E::logits(next, st.q, ad, kat);
+        E::values(st.o, w, ad, vat);
         st.weigh_kept(now, wn, a.c);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) w[b] = wn[b];
+        w = wn;
         if (DT == ILRE_BF16) {
 #pragma unroll
-            for (int k = 0; k < 16 * NB; ++k) {
+            for (int k = 0; k < 16; ++k) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
             }
         }
     };
-    auto keys_at = [&](int i, int sub) { return lds0 + (i & 3) * SLOT + sub * 32 * ROWB; };
-    auto values_at = [&](int i, int sub) { return lds0 + (4 + (i & 3)) * SLOT + sub * 32 * ROWB; };
     auto kept_tiles = [&](int g1, int g2) {
         if (idle) {
             for (int i = g1; i < g2; ++i) advance(i);
             return;
         }
-        f32x16 s[2][NB];
-        typename E::Weights w[NB];
-        E::template logits<NB>(s[0], st.q, ad, keys_at(g1, 0));
+        f32x16 s[2];
+        typename E::Weights w;
+        E::logits(s[0], st.q, ad, keys_at(g1, 0));
         advance(g1);
         // the first step has no weights before it
         if (SUB == 2) {
-            E::template logits<NB>(s[1], st.q, ad, keys_at(g1, 1));
+            E::logits(s[1], st.q, ad, keys_at(g1, 1));
             st.weigh_kept(s[0], w, a.c);
             kept_step(s[1], s[0], w, keys_at(g1 + 1, 0), values_at(g1, 0));
             for (int i = g1 + 1; i < g2; ++i) {
@@ -628,7 +568,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
                 kept_step(s[1], s[0], w, keys_at(i + 1, 0), values_at(i, 0));
             }
         } else {
-            E::template logits<NB>(s[1], st.q, ad, keys_at(g1 + 1, 0));
+            E::logits(s[1], st.q, ad, keys_at(g1 + 1, 0));
             st.weigh_kept(s[0], w, a.c);
             int i = g1 + 1;
             for (; i + 1 < g2; i += 2) {
@@ -642,59 +582,97 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 || NB == 2 ? 1 : 2) void
                 kept_step(s[1], s[0], w, keys_at(i + 1, 0), values_at(i - 1, 0));
             }
         }
-        E::template values<NB>(st.o, w, ad, values_at(g2 - 1, SUB - 1));
+        E::values(st.o, w, ad, values_at(g2 - 1, SUB - 1));
     };
 
+    if (count > 0) begin();
+    st.load(a, blk, head, row0, l32, half);  // behind the copies: they are on their way together
+    st.clear();
     if (count > 0) {
         // behind the first tile that all rows see whole, as far as they do
         int g1 = count, g2 = count;
-        if (DT == ILRE_BF16 && !careful) {
+        if (DT == ILRE_BF16) {
             const int from = a.window > 0 ? max((blk.all_lo + TN - 1) / TN, blk.w0) - blk.w0 + blk.ns : 0;
             const int to = a.window > 0 ? blk.all_hi / TN - blk.w0 + blk.ns : blk.all_hi / TN;
             g1 = max(from - first, 0) + 1;
             g2 = min(to - first, count);
             if (g2 - g1 < 2) g1 = g2 = count;
         }
-        begin();
-        for (int i = 0; i < g1; ++i) follow_tile(i);
+        for (int i = 0; i < g1; ++i) follow_tile(i, false);
         if (g1 < g2) kept_tiles(g1, g2);
-        for (int i = g2; i < count; ++i) follow_tile(i);
+        for (int i = g2; i < count; ++i) follow_tile(i, false);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (g1 < g2) {
+        if (PAGED || g1 < g2) {
             bool far = false;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) far = far || !(st.z[b][k] <= kSumLimit);
-            if (!idle && far) *flag = 1;
+            for (int k = 0; k < 4; ++k) far = far || !(st.z[k] <= kSumLimit);
+            if (!idle && far && g1 < g2) *flag = 1;
             __syncthreads();
             if (__builtin_amdgcn_readfirstlane(*flag)) {
                 st.clear();
                 begin();
-                for (int i = 0; i < count; ++i) follow_tile(i);
+                for (int i = 0; i < count; ++i) follow_tile(i, PAGED);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             }
         }
     }
-    if (idle) return;
+    float m = st.m, sum = st.sum();
+    if (TS == 2) {
+        // Each of the two keeps two of the four channel blocks and hands the other two to its partner, 16-byte pieces of row l32 at place piece ^ l32 % 16.
+        static_assert(TS == 1 || WAVES * 32 * 256 <= 8 * SLOT, "half the sums of every wavefront fit where the tiles were");
+        __syncthreads();  // everybody is done with the tiles
+        const int mine = wave / GROUPS;
+        auto piece = [&](int w, int at) { return (float4 *)(smem + w * 32 * 256 + l32 * 256 + (at ^ (l32 & 15)) * 16); };
+        float2 *stats = (float2 *)(smem + 8 * SLOT + 16);  // [WAVES][32]
+        const int other = wave < GROUPS ? wave + GROUPS : wave - GROUPS;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const Target t = target_of(a, blk, head, row0 + 32 * b + l32, nsp == 1, split, st.m[b], st.sum(b));
+        for (int d = 0; d < 2; ++d)
 #pragma unroll
-        for (int db = 0; db < 4; ++db) store_channels<DT>(a, t, db, st.o[b][db], half);
-        store_sum(a, t, half);
+            for (int k = 0; k < 4; ++k) {
+                const f32x16 &x = mine == 0 ? st.o[2 + d] : st.o[d];
+                *piece(wave, d * 8 + 2 * k + half) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+            }
+        if (half == 0) stats[wave * 32 + l32] = make_float2(m, sum);
+        __syncthreads();
+        if (idle) return;
+        const float2 theirs = stats[other * 32 + l32];
+        const float top = fmaxf(m, theirs.x), f = exp2_fast(m - top), g = exp2_fast(theirs.x - top);
+        // the same order on both sides: the first half's sum and then the second's
+        sum = mine == 0 ? fmaf(theirs.y, g, sum * f) : fmaf(sum, f, theirs.y * g);
+        m = top;
+        const Target t = target_of(a, blk, head, row0 + l32, nsp == 1, split, m, sum);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            f32x16 x = mine == 0 ? st.o[d] : st.o[2 + d];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 y = *piece(other, d * 8 + 2 * k + half);
+                x[4 * k] = fmaf(x[4 * k], f, y.x * g);
+                x[4 * k + 1] = fmaf(x[4 * k + 1], f, y.y * g);
+                x[4 * k + 2] = fmaf(x[4 * k + 2], f, y.z * g);
+                x[4 * k + 3] = fmaf(x[4 * k + 3], f, y.w * g);
+            }
+            store_channels<DT>(a, t, 2 * mine + d, x, half);
+        }
+        if (mine == 0) store_sum(a, t, half);
+        return;
     }
+    if (idle) return;
+    const Target t = target_of(a, blk, head, row0 + l32, nsp == 1, split, m, sum);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) store_channels<DT>(a, t, db, st.o[db], half);
+    store_sum(a, t, half);
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
 
 // Up to 32 rows: each of WAVES wavefronts takes 32 of a tile's 32 * WAVES tokens, with tile buffers of its own and no barrier on the way; what they have is
 // added up at the end.
-template <int DT, int WAVES, bool PAGED>
-__global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
+template <int DT, int WAVES, int STAGES, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 && STAGES == 1 ? 2 : 1) void attend_tokens(const AttnArgs a)
 {
     using E = Elem<DT>;
-    constexpr int ROWB = E::ROWB, SLOT = 32 * ROWB, STAGES = DT == ILRE_BF16 ? 2 : 1, TN = 32 * WAVES;
+    constexpr int ROWB = E::ROWB, SLOT = 32 * ROWB, TN = 32 * WAVES;
     constexpr int HALF = 16 * ROWB / 1024, COPIES = 2 * HALF;  // copies of 16 rows, of 32
     extern __shared__ __align__(16) unsigned char smem[];
 
@@ -708,9 +686,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
 
-    State<DT, 1> st;
-    st.load(a, blk, head, blk.rows0, l32, half);
-    st.clear();
+    State<DT> st;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * 2 * STAGES * SLOT;
     typename E::Addr ad;
     ad.init(lane);
@@ -746,8 +722,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
         copy_rows<16, ROWB, true, PAGED>(a, blk, vs, own_token(i) + 16, p.id[1], to + 16 * ROWB, vvoff, lane);
     };
 
+    Pages pg[STAGES + 1];
     if (count > 0) {
-        Pages pg[STAGES + 1];
 #pragma unroll
         for (int s = 0; s <= STAGES; ++s) pg[s] = lookup(s);
 #pragma unroll
@@ -755,6 +731,10 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
             copy_keys(s, pg[s]);
             copy_values(s, pg[s]);
         }
+    }
+    st.load(a, blk, head, blk.rows0, l32, half);  // behind the copies: they are on their way together
+    st.clear();
+    if (count > 0) {
         for (int i = 0; i < count; ++i) {
             const int tok = token_of(i);
             const int absent = PAGED ? (pg[0].id[0] < 0 ? 1 : 0) | (pg[0].id[1] < 0 ? 2 : 0) : 0;
@@ -763,15 +743,12 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * STAGES - 1) * COPIES) : "memory");
             f32x16 s[1];
             typename E::Weights w[1];
-            E::template logits<1>(s, st.q, ad, lds0 + (i % STAGES) * SLOT);
+            E::logits(s[0], st.q, ad, lds0 + (i % STAGES) * SLOT);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
             copy_keys(i + STAGES, next);
-            if (tok + 32 <= blk.all_hi && tok >= blk.all_lo && absent == 0)
-                st.template weigh<false>(s, w, a.c, tok, a.sink, half, 0);
-            else
-                st.template weigh<true>(s, w, a.c, tok, a.sink, half, absent);
+            st.template weigh<true, 1>(s, w, a.c, tok, a.sink, half, absent);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * STAGES - 1) * COPIES) : "memory");
-            E::template values<1>(st.o, w, ad, lds0 + (STAGES + i % STAGES) * SLOT);
+            E::values(st.o, w[0], ad, lds0 + (STAGES + i % STAGES) * SLOT);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             copy_values(i + STAGES, next);
 #pragma unroll
@@ -780,19 +757,18 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    // What the wavefronts have: sums in `mine` (rows 33 pieces of 16 bytes apart), references and sums of weights behind all of them.
-    constexpr int PITCH = 132;
-    static_assert(32 * PITCH * 4 <= 2 * STAGES * SLOT, "a wavefront's sums fit where its tiles were");
-    float *mine = (float *)(smem + wave * 2 * STAGES * SLOT);
+    // What the wavefronts have: sums where their tiles were, the 16-byte pieces of row l32 at place piece ^ l32 % 16, references and sums of weights
+    // behind all of them.
+    static_assert(32 * kHeadDim * 4 <= 2 * STAGES * SLOT, "a wavefront's sums fit where its tiles were");
+    auto piece = [&](int w, int at) { return (float4 *)(smem + w * 2 * STAGES * SLOT + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
     float2 *stats = (float2 *)(smem + WAVES * 2 * STAGES * SLOT);  // [WAVES][32]
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            *(float4 *)&mine[l32 * PITCH + db * 32 + 8 * k + 4 * half] =
-                make_float4(st.o[0][db][4 * k], st.o[0][db][4 * k + 1], st.o[0][db][4 * k + 2], st.o[0][db][4 * k + 3]);
-    const float z = st.sum(0);
-    if (half == 0) stats[wave * 32 + l32] = make_float2(st.m[0], z);
+            *piece(wave, db * 8 + 2 * k + half) = make_float4(st.o[db][4 * k], st.o[db][4 * k + 1], st.o[db][4 * k + 2], st.o[db][4 * k + 3]);
+    const float z = st.sum();
+    if (half == 0) stats[wave * 32 + l32] = make_float2(st.m, z);
     __syncthreads();
     float2 ms[WAVES];
     float top = kFloor, sum = 0.f;
@@ -813,10 +789,9 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
         f32x16 x = f32x16{};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float *from = (const float *)(smem + w * 2 * STAGES * SLOT) + l32 * PITCH + db * 32 + 4 * half;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float4 y = *(const float4 *)(from + 8 * k);
+                const float4 y = *piece(w, db * 8 + 2 * k + half);
                 x[4 * k] = fmaf(y.x, ms[w].x, x[4 * k]);
                 x[4 * k + 1] = fmaf(y.y, ms[w].x, x[4 * k + 1]);
                 x[4 * k + 2] = fmaf(y.z, ms[w].x, x[4 * k + 2]);
@@ -830,54 +805,105 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_tokens(const AttnArgs a)
 
 // ------------------------------------------------------------------------------------------------ merge of the ranges
 
-// A wavefront a row (token, head): out = sum_s 2^(e_s - E) o_s / sum_s 2^(e_s - E), E the largest e_s, in the order of the ranges.
-template <int DT, bool PAGED>
+// 16 lanes a row (token, head), 8 channels each: out = sum_s 2^(e_s - E) o_s / sum_s 2^(e_s - E), E the largest e_s.  WIDE: a workgroup a row, its 16 groups
+// of 16 lanes take every 16th range and are added up in their order: with few rows there is nothing else to have loads under way from.  Logarithms and
+// results are asked for before it is known how many ranges there are (all of them lie in the workspace), so that one latency passes, not three.
+template <int DT, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(256) void merge_ranges(const AttnArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (row >= (int64_t)a.T * a.Hq) return;
-    const int token = (int)(row / a.Hq), head = (int)(row - (int64_t)token * a.Hq);
+    constexpr int STEP = WIDE ? 16 : 1, EARLY = 2;
+    __shared__ float4 parts[WIDE ? 16 : 1][16][2];
+    __shared__ float sums[16];
+    const int lane = threadIdx.x & 63, l16 = threadIdx.x & 15, group = threadIdx.x >> 4, mine = WIDE ? group : 0;
+    const int64_t rows = (int64_t)a.T * a.Hq, row = WIDE ? blockIdx.x : (int64_t)blockIdx.x * 16 + group;
+    // the row's sequence: the wavefront looks for the one of its first row's token, the others follow it
+    const int64_t first_row = WIDE ? row : (int64_t)blockIdx.x * 16 + (threadIdx.x >> 6) * 4;
+    if (first_row >= rows) return;
+    const float *e = a.part_e + min(row, rows - 1), *o = a.part_o + min(row, rows - 1) * kHeadDim + 8 * l16;
+    float ee = l16 < a.nsplit ? e[l16 * rows] : 0.f;
+    float4 y[EARLY], z[EARLY];
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k) {
+        const int64_t s = min(mine + k * STEP, a.nsplit - 1);
+        y[k] = *(const float4 *)(o + s * rows * kHeadDim);
+        z[k] = *(const float4 *)(o + s * rows * kHeadDim + 4);
+    }
+    const int token = (int)(row / a.Hq), head = (int)(row - (int64_t)token * a.Hq), first = (int)(first_row / a.Hq);
     int seq = 0;
-    for (int base = 0; base < a.n_seq; base += 64) {
-        const int s = base + lane;
-        const unsigned long long past = __ballot(s < a.n_seq && clamp_to(a.cu_q[s + 1], 0, a.T) > token);
-        if (past) {
-            seq = base + __builtin_ctzll(past);
-            break;
+    if (a.n_seq > 1) {
+        for (int base = 0; base < a.n_seq; base += 64) {
+            const int s = base + lane;
+            const unsigned long long past = __ballot(s < a.n_seq && clamp_to(a.cu_q[s + 1], 0, a.T) > first);
+            if (past) {
+                seq = base + __builtin_ctzll(past);
+                break;
+            }
         }
     }
+    if (row >= rows) return;
+    while (seq < a.n_seq - 1 && clamp_to(a.cu_q[seq + 1], 0, a.T) <= token) ++seq;
     Block blk;
-    sequence_of<PAGED>(a, __builtin_amdgcn_readfirstlane(seq), blk);
+    sequence_of<PAGED>(a, seq, blk);
     if (token < blk.q0 || token >= blk.q0 + blk.q_len) return;  // a token of no sequence
     const int r = (token - blk.q0) * a.G + head % a.G;
     blk.rows0 = r / a.rows * a.rows;
     tiles_of(blk, mask_of(a), a.G, a.rows, a.tile);
     const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     if (nsp == 1) return;  // written already
-    const int64_t pitch = (int64_t)a.T * a.Hq;
-    float top = -INFINITY;
-    for (int s = lane; s < nsp; s += 64) top = fmaxf(top, a.part_e[s * pitch + row]);
+    float top = l16 < nsp ? ee : -INFINITY;
+    for (int s = l16 + 16; s < nsp; s += 16) top = fmaxf(top, e[s * rows]);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    float sum = 0.f;
-    float2 x = make_float2(0.f, 0.f);
+    for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
     const float ref = top == -INFINITY ? 0.f : top;  // no range has a token that the row sees
-#pragma unroll 8
-    for (int s = 0; s < nsp; ++s) {
-        const float2 y = *(const float2 *)(a.part_o + (s * pitch + row) * kHeadDim + 2 * lane);
-        const float w = exp2_fast(a.part_e[s * pitch + row] - ref);
+    float sum = 0.f, x[8] = {};
+    auto take = [&](int s, const float4 &u, const float4 &v) {
+        const float w = exp2_fast(e[s * rows] - ref);
         sum += w;
-        x.x = fmaf(w, y.x, x.x);
-        x.y = fmaf(w, y.y, x.y);
+        x[0] = fmaf(w, u.x, x[0]), x[1] = fmaf(w, u.y, x[1]), x[2] = fmaf(w, u.z, x[2]), x[3] = fmaf(w, u.w, x[3]);
+        x[4] = fmaf(w, v.x, x[4]), x[5] = fmaf(w, v.y, x[5]), x[6] = fmaf(w, v.z, x[6]), x[7] = fmaf(w, v.w, x[7]);
+    };
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k)
+        if (mine + k * STEP < nsp) take(mine + k * STEP, y[k], z[k]);
+#pragma unroll 4
+    for (int s = mine + EARLY * STEP; s < nsp; s += STEP)
+        take(s, *(const float4 *)(o + s * rows * kHeadDim), *(const float4 *)(o + s * rows * kHeadDim + 4));
+    if (WIDE) {
+        parts[group][l16][0] = make_float4(x[0], x[1], x[2], x[3]);
+        parts[group][l16][1] = make_float4(x[4], x[5], x[6], x[7]);
+        if (l16 == 0) sums[group] = sum;
+        __syncthreads();
+        if (group != 0) return;
+        const int n = min(nsp, 16);
+        for (int g = 1; g < n; ++g) {
+            const float4 u = parts[g][l16][0], v = parts[g][l16][1];
+            x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w;
+            x[4] += v.x, x[5] += v.y, x[6] += v.z, x[7] += v.w;
+            sum += sums[g];
+        }
     }
     const float f = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] *= f;
     unsigned char *to = a.out + (int64_t)token * a.out_token + (int64_t)head * a.out_head;
-    if (DT == ILRE_F32)
-        *(float2 *)(to + 8 * lane) = make_float2(x.x * f, x.y * f);
+    if (DT == ILRE_F32) {
+        *(float4 *)(to + 32 * l16) = make_float4(x[0], x[1], x[2], x[3]);
+        *(float4 *)(to + 32 * l16 + 16) = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        *(uint4 *)(to + 16 * l16) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+    if (l16 == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+}
+
+template <int DT, bool PAGED>
+hipError_t launch_merge(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
+{
+    const int64_t rows = (int64_t)a.T * a.Hq;
+    if (rows <= 512 && p.nsplit > 4)
+        hipLaunchKernelGGL((merge_ranges<DT, PAGED, true>), dim3((unsigned)rows), dim3(256), 0, s, a);
     else
-        *(unsigned *)(to + 4 * lane) = pack_bf16(x.x * f, x.y * f);
-    if (lane == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+        hipLaunchKernelGGL((merge_ranges<DT, PAGED, false>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 constexpr int kMaxLds = 136 * 1024;
@@ -903,10 +929,16 @@ hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const At
     return hipGetLastError();
 }
 
-template <int DT, int WAVES, int NB, int TN, bool PAGED>
+template <int DT, int WAVES, int TS, int TN, bool PAGED>
 hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(attend_rows<DT, WAVES, NB, TN, PAGED>, p, WAVES * 64, 8 * TN * Elem<DT>::ROWB + 16, a, s);
+    return launch(attend_rows<DT, WAVES, TS, TN, PAGED>, p, WAVES * 64, 8 * TN * Elem<DT>::ROWB + 16 + (TS == 2 ? WAVES * 32 * sizeof(float2) : 0), a, s);
+}
+
+template <int DT, int WAVES, int STAGES, bool PAGED>
+hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
+{
+    return launch(attend_tokens<DT, WAVES, STAGES, PAGED>, p, WAVES * 64, WAVES * (2 * STAGES * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
 template <bool PAGED>
@@ -915,24 +947,19 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
     hipError_t e;
     if (p.dtype == ILRE_BF16) {
         if (p.rows == 32)
-            e = launch(attend_tokens<ILRE_BF16, 4, PAGED>, p, 256, 4 * 4 * 32 * 256 + 4 * 32 * sizeof(float2), a, s);
+            e = launch_tokens<ILRE_BF16, 4, 1, PAGED>(p, a, s);
         else if (p.rows == 128)
-            e = launch_rows<ILRE_BF16, 4, 1, 32, PAGED>(p, a, s);
+            e = launch_rows<ILRE_BF16, 8, 2, 64, PAGED>(p, a, s);
         else
             e = launch_rows<ILRE_BF16, 8, 1, 64, PAGED>(p, a, s);
     } else {
         if (p.rows == 32)
-            e = launch(attend_tokens<ILRE_F32, 4, PAGED>, p, 256, 4 * 2 * 32 * 512 + 4 * 32 * sizeof(float2), a, s);
+            e = launch_tokens<ILRE_F32, 4, 1, PAGED>(p, a, s);
         else
             e = launch_rows<ILRE_F32, 4, 1, 32, PAGED>(p, a, s);
     }
     if (e != hipSuccess || p.nsplit == 1) return e;
-    const unsigned grid = (unsigned)(((int64_t)a.T * a.Hq + 3) / 4);
-    if (p.dtype == ILRE_BF16)
-        hipLaunchKernelGGL((merge_ranges<ILRE_BF16, PAGED>), dim3(grid), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((merge_ranges<ILRE_F32, PAGED>), dim3(grid), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return p.dtype == ILRE_BF16 ? launch_merge<ILRE_BF16, PAGED>(p, a, s) : launch_merge<ILRE_F32, PAGED>(p, a, s);
 }
 
 }  // namespace
@@ -942,25 +969,37 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
     AttnPlan p{};
     p.dtype = dtype;
     const int64_t G = Hq / Hkv, rows = (int64_t)max_q * G;
-    p.rows = rows <= 32 ? 32 : dtype == ILRE_F32 || rows <= 128 ? 128 : 256;
-    p.tile = p.rows == 32 ? 128 : p.rows == 128 ? 32 : 64;
-    // at most so many blocks, whatever the sequences' lengths
-    p.nblocks = (int)std::min(((int64_t)T * G + (int64_t)n_seq * (p.rows - 1)) / p.rows, (int64_t)T * G);
     if (total_kv <= 0) total_kv = (int64_t)n_seq * max_kv;
+    auto cut = [&](int block, int tile) {
+        p.rows = block;
+        p.tile = tile;
+        // at most so many blocks, whatever the sequences' lengths
+        p.nblocks = (int)std::min(((int64_t)T * G + (int64_t)n_seq * (block - 1)) / block, (int64_t)T * G);
+    };
     auto tiles = [&](int64_t kv) {
         const int64_t all = (kv + p.tile - 1) / p.tile;
         if (window <= 0) return all;
         return std::min(all, (std::min((int64_t)sink, kv) + p.tile - 1) / p.tile + (window + (p.rows + G - 1) / G) / p.tile + 2);
     };
+    if (rows <= 32) {
+        cut(32, 128);
+    } else if (dtype == ILRE_F32) {
+        cut(128, 32);
+    } else {
+        cut(256, 64);
+        if (rows <= 128 || ((int64_t)p.nblocks * Hkv < kNumCU && tiles(max_kv) <= 24)) cut(128, 64);
+    }
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
-    const int64_t work = std::max<int64_t>((int64_t)p.nblocks * Hkv * tiles(total_kv / n_seq), 1);
-    const int64_t places = p.rows == 128 && dtype == ILRE_BF16 ? 2 * kNumCU : kNumCU;
-    int64_t per = std::max<int64_t>((work + places - 1) / places, p.rows == 32 ? 1 : 4);
+    const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
+    const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);
+    const int64_t places = p.rows == 32 && dtype == ILRE_BF16 ? 2 * kNumCU : kNumCU;
+    const int64_t least = p.rows == 32 ? 2 : dtype == ILRE_F32 ? 2 : 12;
+    const int64_t per = std::max<int64_t>((work + places - 1) / places, least);
     int64_t n = (most + per - 1) / per;
     const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);
     n = std::max<int64_t>(1, std::min({n, (int64_t)256, (int64_t)(workspace / (size_t)row_bytes), (int64_t)0x7FFFFFFF / ((int64_t)p.nblocks * Hkv)}));
     p.nsplit = (int)n;
-    p.split_tiles = (int)((most + n - 1) / n);
+    p.split_tiles = (int)(n == 1 ? most : std::max(per, (most + n - 1) / n));
     p.bytes = n == 1 ? 0 : (size_t)(n * row_bytes);
     return p;
 }
