@@ -7,6 +7,7 @@ if the shared library is missing, loading fails loudly.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -218,23 +219,18 @@ def _qk_meta(q: torch.Tensor, k: torch.Tensor):
 
 def _opts(dtype: int, n_pool_kernels: int, scale: float, score_mode: int, workspace: Optional[torch.Tensor],
           q: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None, flags: int = 0, sink: int = 0) -> IlreOpts:
-    o = IlreOpts()
-    o.struct_size = ctypes.sizeof(IlreOpts)
-    o.dtype = dtype
-    o.n_pool_kernels = n_pool_kernels
-    o.score_mode = score_mode
-    o.scale = float(scale)
-    o.flags = int(flags)
-    o.sink = int(sink)
-    if q is not None:
-        o.q_stride_head, o.q_stride_token = q.stride(0), q.stride(1)
-    if k is not None:
-        o.k_stride_head, o.k_stride_token = k.stride(0), k.stride(1)
-    if workspace is not None:
-        o.workspace = workspace.data_ptr()
-        o.workspace_bytes = workspace.numel() * workspace.element_size()
-    o.stream = torch.cuda.current_stream().cuda_stream
-    return o
+    ks = (0, 0) if k is None else (k.stride(0), k.stride(1))
+    qs = (0, 0) if q is None else (q.stride(0), q.stride(1))
+    ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return IlreOpts(_OPTS_SIZE, dtype, n_pool_kernels, score_mode, float(scale), int(flags), *ks, *qs, *ws, _current_stream(), int(sink), 0)
+
+
+_OPTS_SIZE = ctypes.sizeof(IlreOpts)
+
+
+def _current_stream() -> int:
+    """Handle of the current stream of the current device (what torch.cuda.current_stream().cuda_stream is, without the stream object)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def alloc_workspace(L: int, Lq: int, Hq: int, Hkv: int, d: int, n_pool_kernels: int, dtype: int,
@@ -447,6 +443,17 @@ def _row_strides(t: torch.Tensor):
     return (t.stride(0) if n > 1 else 0), (t.stride(1) if h > 1 else 0)
 
 
+@functools.lru_cache(maxsize=4096)
+def _strides_ref(*values: int):
+    """An ilre_strides of these values to pass on (the library only reads it)."""
+    return ctypes.byref(IlreStrides(*values))
+
+
+@functools.lru_cache(maxsize=4096)
+def _attn_ref(causal: int, sink: int, window: int, max_q: int, max_kv: int, total_kv: int):
+    return ctypes.byref(IlreAttn(ctypes.sizeof(IlreAttn), causal, sink, window, max_q, max_kv, total_kv))
+
+
 def _like(name: str, out: Optional[torch.Tensor], ref: torch.Tensor) -> torch.Tensor:
     if out is None:
         return torch.empty(ref.shape, dtype=ref.dtype, device=ref.device)
@@ -468,10 +475,10 @@ def ilre_rope(x: torch.Tensor, freqs: IlreRopeFreqs, positions: Optional[torch.T
     """Rotary positions of x [T, H, d]; `out` may be x itself, or a view of the recall's key cache: k_cache[:, a:a+T].transpose(0, 1)."""
     T, H, d = _tokens_meta("x", x)
     out = _like("out", out, x)
-    st = IlreStrides(*_row_strides(x), *_row_strides(out))
+    st = _strides_ref(*_row_strides(x), *_row_strides(out))
     o = _opts(_dtype_code(x), 0, 0.0, ILRE_SCORE_SUM, None)
     _check(load().ilre_rope(x.data_ptr(), out.data_ptr(), T, H, d, None if positions is None else _int32_vector("positions", positions, T),
-                            int(first_position), ctypes.byref(freqs), int(pairing), ctypes.byref(st), ctypes.byref(o)))
+                            int(first_position), ctypes.byref(freqs), int(pairing), st, ctypes.byref(o)))
     return out
 
 
@@ -535,12 +542,12 @@ def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[tor
         if cache.v_pages is None:
             raise ValueError("the cache holds keys only")
         vs = _row_strides(v)
-    st = IlreStrides(*qs, *os_, *_row_strides(k), *vs)
+    st = _strides_ref(*qs, *os_, *_row_strides(k), *vs)
     o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
     _check(load().ilre_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
                                    None if v is None else v.data_ptr(), T, Hq, d,
                                    None if positions is None else _int32_vector("positions", positions, T), ctypes.byref(freqs), int(pairing),
-                                   cache._ref, ctypes.byref(st), ctypes.byref(o)))
+                                   cache._ref, st, ctypes.byref(o)))
     return q_out
 
 
@@ -579,11 +586,10 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
     out, lse = _attention_outputs(q, out, lse, T, Hq)
     if workspace is None:
         workspace = alloc_workspace_attention(T, cache.n_seq, Hq, cache.Hkv, d, max_q, max_kv, total_kv=total_kv, dtype=dt, device=q.device)
-    at = IlreAttn(ctypes.sizeof(IlreAttn), 1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
-    st = IlreStrides(*_row_strides(q), *_row_strides(out))
+    at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
+    st = _strides_ref(*_row_strides(q), *_row_strides(out))
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
-    _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, ctypes.byref(at), cache._ref, ctypes.byref(st),
-                                       ctypes.byref(o)))
+    _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, at, cache._ref, st, ctypes.byref(o)))
     return out, lse
 
 
@@ -608,11 +614,10 @@ def ilre_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_
     out, lse = _attention_outputs(q, out, lse, T, Hq)
     if workspace is None:
         workspace = alloc_workspace_attention(T, n_seq, Hq, Hkv, d, max_q, max_k, total_kv=Tk, dtype=dt, device=q.device)
-    at = IlreAttn(ctypes.sizeof(IlreAttn), 1 if causal else 0, int(sink), int(window), int(max_q), int(max_k), Tk)
-    st = IlreStrides(*_row_strides(q), *_row_strides(out), *_row_strides(k), *_row_strides(v))
+    at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_k), Tk)
+    st = _strides_ref(*_row_strides(q), *_row_strides(out), *_row_strides(k), *_row_strides(v))
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
-    _check(load().ilre_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Tk, Hq, Hkv, d, pq, pk, n_seq,
-                                        ctypes.byref(at), ctypes.byref(st), ctypes.byref(o)))
+    _check(load().ilre_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Tk, Hq, Hkv, d, pq, pk, n_seq, at, st, ctypes.byref(o)))
     return out, lse
 
 

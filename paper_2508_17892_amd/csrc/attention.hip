@@ -83,10 +83,11 @@ __device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b
     b.nrows = b.q_len * a.G;
 }
 
-// Workgroup w's block of `rows` rows: the blocks of all sequences one after the other, within a sequence the last one first (with a causal
-// mask it has most to do).  False where there are fewer blocks.
+// Unit w: a block of `rows` rows and one range of its tiles.  The units of all sequences come one after the other, a sequence's first ranges before its second
+// ones and, within them, the last block first (with a causal mask it has most to do); what is left of the grid has none and ends at once, behind all that
+// work (between them, 48 requests with contexts of 1 to 16384 tokens, it cost 10 of 85 us).  False where there is none.
 template <bool PAGED>
-__device__ __forceinline__ bool find_block(const AttnArgs &a, int w, int rows, Block &b)
+__device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, int tile, Block &b, int &split)
 {
     int seq = 0, before = 0;
     if (a.n_seq > 1) {
@@ -96,8 +97,14 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int w, int rows, B
             const int s = base + lane;
             int n = 0;
             if (s < a.n_seq) {
-                const int from = clamp_to(a.cu_q[s], 0, a.T);
-                n = ((clamp_to(a.cu_q[s + 1], from, a.T) - from) * a.G + rows - 1) / rows;
+                Block x;
+                sequence_of<PAGED>(a, s, x);
+                n = (x.nrows + rows - 1) / rows;
+                if (a.nsplit > 1 && n > 0) {
+                    x.rows0 = (n - 1) * rows;
+                    tiles_of(x, mask_of(a), a.G, rows, tile);
+                    n *= ranges_of(x.nt + (a.window > 0), a.split_tiles, a.nsplit);  // (with a window another block may have one tile more)
+                }
             }
             int sum = n;
 #pragma unroll
@@ -119,10 +126,12 @@ __device__ __forceinline__ bool find_block(const AttnArgs &a, int w, int rows, B
     }
     sequence_of<PAGED>(a, __builtin_amdgcn_readfirstlane(seq), b);
     const int n = (b.nrows + rows - 1) / rows;
+    if (n == 0) return false;
     const int at = __builtin_amdgcn_readfirstlane(w - before);
-    if (at >= n) return false;
-    b.rows0 = (n - 1 - at) * rows;
-    return true;
+    split = at / n;
+    b.rows0 = (n - 1 - (at - split * n)) * rows;
+    tiles_of(b, mask_of(a), a.G, rows, tile);
+    return split < ranges_of(b.nt, a.split_tiles, a.nsplit);
 }
 
 // ------------------------------------------------------------------------------------------------ tile copies
@@ -194,7 +203,7 @@ struct Elem;
 
 template <>
 struct Elem<ILRE_BF16> {
-    static constexpr int ROWB = 256, QREGS = 8;  // QREGS: 16-byte pieces a lane holds of its query row
+    static constexpr int ROWB = 256, QREGS = 8, RING = 4;  // QREGS: 16-byte pieces a lane holds of its query row
     struct Weights {
         uint4 p[2];
     };
@@ -245,7 +254,7 @@ struct Elem<ILRE_BF16> {
 // fp32 states: the fp32 matrix instructions (a sixteenth of the bf16 rate), nothing is rounded on the way.
 template <>
 struct Elem<ILRE_F32> {
-    static constexpr int ROWB = 512, QREGS = 16;
+    static constexpr int ROWB = 512, QREGS = 16, RING = 2;
     struct Weights {
         float p[16];
     };
@@ -289,6 +298,9 @@ struct Elem<ILRE_F32> {
     }
 };
 
+// A word with the lowest n bits set, all for n >= 32, none for n <= 0.
+__device__ __forceinline__ unsigned first_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+
 // A wavefront's running state for 32 rows; a lane and its partner 32 lanes on have row l32, the tokens of each 32 between them.
 template <int DT>
 struct State {
@@ -319,27 +331,29 @@ struct State {
 #pragma unroll
             for (int st = 0; st < E::QREGS; ++st) q[st] = make_uint4(0, 0, 0, 0);
         }
-        const int p = blk.kv - blk.q_len + i;
+        const int p = max(blk.kv - blk.q_len + i, -1);  // a row in front of its sequence sees nothing
         hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
-        lo = a.window > 0 ? p - a.window + 1 : 0;
+        lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
     }
     // The logits of SUB x 32 tokens from `tok` on become weights; the running maximum is followed.  `absent`: bit k: tokens 16 k .. 16 k + 15 are on no page.
-    template <bool MASKED, int SUB>
+    // What the row sees of 32 tokens is a word of bits, two instructions a logit: nearly every tile that comes here has an edge in it, and code that
+    // is not there need not be fetched.
+    template <int SUB>
     __device__ __forceinline__ void weigh(f32x16 (&s)[SUB], typename E::Weights (&w)[SUB], float c, int tok, int sink, int half, int absent)
     {
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            if (MASKED) {
+            const int at = tok + 32 * u;
+            unsigned bits = first_bits(hi - at) & (~first_bits(lo - at) | first_bits(sink - at));
+            bits &= ~((absent >> (2 * u) & 1 ? 0xFFFFu : 0u) | (absent >> (2 * u + 1) & 1 ? 0xFFFF0000u : 0u));
+            bits >>= 4 * half;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int t = tok + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3);
-                    const bool seen = t < hi && (t >= lo || t < sink) && !(absent >> (2 * u + (i >> 3)) & 1);
-                    s[u][i] = seen ? s[u][i] : -INFINITY;
-                }
+            for (int i = 0; i < 16; ++i) {
+                const int seen = (int)(bits << (31 - (8 * (i >> 2) + (i & 3)))) >> 31;
+                s[u][i] = __int_as_float((__float_as_int(s[u][i]) & seen) | (__float_as_int(-INFINITY) & ~seen));
+                top = fmaxf(top, s[u][i]);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
         }
         top = fmaxf(top, other_half(top));
         const float mnew = fmaxf(m, top * c);
@@ -434,24 +448,24 @@ __device__ __forceinline__ void store_sum(const AttnArgs &a, const Target &t, in
 
 // WAVES / TS groups of 32 rows share the tiles of TN tokens; with TS = 2 two wavefronts have the same rows and a half of each tile's tokens, and add up what
 // they have at the end.  Keys and values have four tile buffers each; while tile i is worked on, its values, the keys of tile i + 1 and (in the pipelined
-// loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.
+// loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.  fp32 tiles have two buffers
+// each, so that two workgroups of four wavefronts fit a compute unit: with one wavefront a SIMD every wait for LDS is a hole between matrix instructions.
 template <int DT, int WAVES, int TS, int TN, bool PAGED>
-__global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_rows(const AttnArgs a)
+__global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
 {
     using E = Elem<DT>;
-    constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, GROUPS = WAVES / TS, ROWS = GROUPS * 32, SUB = TN / 32 / TS;
+    constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, GROUPS = WAVES / TS, ROWS = GROUPS * 32, SUB = TN / 32 / TS, RING = E::RING;
     constexpr int CROWS = TN / WAVES, COPIES = CROWS * ROWB / 1024;  // a wavefront's rows and copies of a tile
     static_assert(CROWS <= 16 && CROWS * ROWB % 1024 == 0 && TN % 32 == 0, "a wavefront's rows lie on one page");
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
     // kv heads run fastest: workgroups that share keys and values are a multiple of Hkv apart, on one XCD where Hkv is a multiple of 8
-    const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, split = rest / a.nblocks;
+    const int head = blockIdx.x % a.Hkv;
     Block blk;
-    if (!find_block<PAGED>(a, rest - split * a.nblocks, ROWS, blk)) return;
-    tiles_of(blk, mask_of(a), a.G, ROWS, TN);
+    int split;
+    if (!find_unit<PAGED>(a, blockIdx.x / a.Hkv, ROWS, TN, blk, split)) return;
     const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
-    if (split >= nsp) return;
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN); };
 
@@ -463,7 +477,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
     typename E::Addr ad;
     ad.init(lane);
     // Set where a kept reference turns out too low, or an entry of the table names no page: then the tiles are walked again, with care.
-    int *flag = (int *)(smem + 8 * SLOT);
+    int *flag = (int *)(smem + 2 * RING * SLOT);
     if (tid == 0) *flag = 0;
     __syncthreads();
 
@@ -483,12 +497,19 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
         return page;
     };
     auto copy_keys = [&](int i, int page) {
-        copy_rows<CROWS, ROWB, false, PAGED>(a, blk, ks, own_token(i), page, lds0 + (i & 3) * SLOT + wave * CROWS * ROWB, kvoff, lane);
+        copy_rows<CROWS, ROWB, false, PAGED>(a, blk, ks, own_token(i), page, lds0 + i % RING * SLOT + wave * CROWS * ROWB, kvoff, lane);
     };
     auto copy_values = [&](int i, int page) {
-        copy_rows<CROWS, ROWB, true, PAGED>(a, blk, vs, own_token(i), page, lds0 + (4 + (i & 3)) * SLOT + wave * CROWS * ROWB, vvoff, lane);
+        copy_rows<CROWS, ROWB, true, PAGED>(a, blk, vs, own_token(i), page, lds0 + (RING + i % RING) * SLOT + wave * CROWS * ROWB, vvoff, lane);
     };
     auto begin = [&]() {
+        if (RING == 2) {
+            const int p = lookup(0);
+            copy_keys(0, p);
+            copy_values(0, p);
+            pages[0] = lookup(1);
+            return;
+        }
         const int p0 = lookup(0), p1 = lookup(1), p2 = lookup(2);
         copy_keys(0, p0);
         copy_keys(1, p1);
@@ -498,8 +519,17 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
         pages[0] = p2;
         pages[1] = lookup(3);
     };
-    // Tile i's values and tile i + 1's keys are there, everybody is done with tile i - 1, and the next copies are on their way.
+    // Tile i's values and tile i + 1's keys (two buffers: tile i's) are there, everybody is done with tile i - 1, and the next copies are on their way.
     auto advance = [&](int i) {
+        if (RING == 2) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            copy_keys(i + 1, pages[0]);
+            copy_values(i + 1, pages[0]);
+            pages[0] = lookup(i + 2);
+            return;
+        }
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * COPIES) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -508,8 +538,8 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
         pages[0] = pages[1];
         pages[1] = lookup(i + 4);
     };
-    auto keys_at = [&](int i, int sub) { return lds0 + (i & 3) * SLOT + (part + sub * 32) * ROWB; };
-    auto values_at = [&](int i, int sub) { return lds0 + (4 + (i & 3)) * SLOT + (part + sub * 32) * ROWB; };
+    auto keys_at = [&](int i, int sub) { return lds0 + i % RING * SLOT + (part + sub * 32) * ROWB; };
+    auto values_at = [&](int i, int sub) { return lds0 + (RING + i % RING) * SLOT + (part + sub * 32) * ROWB; };
     auto follow_tile = [&](int i, bool careful) {
         advance(i);
         if (idle) return;
@@ -518,15 +548,11 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
         typename E::Weights w[SUB];
 #pragma unroll
         for (int sub = 0; sub < SUB; ++sub) E::logits(s[sub], st.q, ad, keys_at(i, sub));
-        if (!careful && tok + SUB * 32 <= blk.all_hi && tok >= blk.all_lo) {
-            st.template weigh<false, SUB>(s, w, a.c, tok, a.sink, half, 0);
-        } else {
-            int absent = 0;
-            if (PAGED && careful) {
-                for (int k = 0; k < SUB * 2; ++k) absent |= (page_of(a, blk, tok + 16 * k) < 0 ? 1 : 0) << k;
-            }
-            st.template weigh<true, SUB>(s, w, a.c, tok, a.sink, half, absent);
+        int absent = 0;
+        if (PAGED && careful) {
+            for (int k = 0; k < SUB * 2; ++k) absent |= (page_of(a, blk, tok + 16 * k) < 0 ? 1 : 0) << k;
         }
+        st.template weigh<SUB>(s, w, a.c, tok, a.sink, half, absent);
 #pragma unroll
         for (int sub = 0; sub < SUB; ++sub) E::values(st.o, w[sub], ad, values_at(i, sub));
     };
@@ -585,19 +611,19 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
         E::values(st.o, w, ad, values_at(g2 - 1, SUB - 1));
     };
 
+    // kept: behind the first tile that all rows see whole, as far as they do
+    int g1 = count, g2 = count;
+    if (DT == ILRE_BF16) {
+        const int from = a.window > 0 ? max((blk.all_lo + TN - 1) / TN, blk.w0) - blk.w0 + blk.ns : 0;
+        const int to = a.window > 0 ? blk.all_hi / TN - blk.w0 + blk.ns : blk.all_hi / TN;
+        g1 = max(from - first, 0) + 1;
+        g2 = min(to - first, count);
+        if (g2 - g1 < 2) g1 = g2 = count;
+    }
     if (count > 0) begin();
     st.load(a, blk, head, row0, l32, half);  // behind the copies: they are on their way together
     st.clear();
     if (count > 0) {
-        // behind the first tile that all rows see whole, as far as they do
-        int g1 = count, g2 = count;
-        if (DT == ILRE_BF16) {
-            const int from = a.window > 0 ? max((blk.all_lo + TN - 1) / TN, blk.w0) - blk.w0 + blk.ns : 0;
-            const int to = a.window > 0 ? blk.all_hi / TN - blk.w0 + blk.ns : blk.all_hi / TN;
-            g1 = max(from - first, 0) + 1;
-            g2 = min(to - first, count);
-            if (g2 - g1 < 2) g1 = g2 = count;
-        }
         for (int i = 0; i < g1; ++i) follow_tile(i, false);
         if (g1 < g2) kept_tiles(g1, g2);
         for (int i = g2; i < count; ++i) follow_tile(i, false);
@@ -619,11 +645,11 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
     float m = st.m, sum = st.sum();
     if (TS == 2) {
         // Each of the two keeps two of the four channel blocks and hands the other two to its partner, 16-byte pieces of row l32 at place piece ^ l32 % 16.
-        static_assert(TS == 1 || WAVES * 32 * 256 <= 8 * SLOT, "half the sums of every wavefront fit where the tiles were");
+        static_assert(TS == 1 || WAVES * 32 * 256 <= 2 * RING * SLOT, "half the sums of every wavefront fit where the tiles were");
         __syncthreads();  // everybody is done with the tiles
         const int mine = wave / GROUPS;
         auto piece = [&](int w, int at) { return (float4 *)(smem + w * 32 * 256 + l32 * 256 + (at ^ (l32 & 15)) * 16); };
-        float2 *stats = (float2 *)(smem + 8 * SLOT + 16);  // [WAVES][32]
+        float2 *stats = (float2 *)(smem + 2 * RING * SLOT + 16);  // [WAVES][32]
         const int other = wave < GROUPS ? wave + GROUPS : wave - GROUPS;
 #pragma unroll
         for (int d = 0; d < 2; ++d)
@@ -668,8 +694,8 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 1 : 2) void attend_row
 
 // Up to 32 rows: each of WAVES wavefronts takes 32 of a tile's 32 * WAVES tokens, with tile buffers of its own and no barrier on the way; what they have is
 // added up at the end.
-template <int DT, int WAVES, int STAGES, bool PAGED>
-__global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 && STAGES == 1 ? 2 : 1) void attend_tokens(const AttnArgs a)
+template <int DT, int WAVES, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_tokens(const AttnArgs a)
 {
     using E = Elem<DT>;
     constexpr int ROWB = E::ROWB, SLOT = 32 * ROWB, TN = 32 * WAVES;
@@ -677,17 +703,16 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 && STAGES == 1 ? 2 : 1)
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, split = rest / a.nblocks;
+    const int head = blockIdx.x % a.Hkv;
     Block blk;
-    if (!find_block<PAGED>(a, rest - split * a.nblocks, 32, blk)) return;
-    tiles_of(blk, mask_of(a), a.G, 32, TN);
+    int split;
+    if (!find_unit<PAGED>(a, blockIdx.x / a.Hkv, 32, TN, blk, split)) return;
     const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
-    if (split >= nsp) return;
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
 
     State<DT> st;
-    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * 2 * STAGES * SLOT;
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * 2 * SLOT;
     typename E::Addr ad;
     ad.init(lane);
 
@@ -701,67 +726,61 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 && STAGES == 1 ? 2 : 1)
     struct Pages {
         int id[2];
     };
-    auto own_token = [&](int i) { return i < count ? token_of(i) : blk.hi; };
     auto lookup = [&](int i) {
         Pages p{};
         if (PAGED) {
-            const int t = own_token(i);
+            const int t = token_of(i);
             p.id[0] = page_of(a, blk, min(t, blk.hi - 1));
             p.id[1] = page_of(a, blk, min(t + 16, blk.hi - 1));
         }
         return p;
     };
     auto copy_keys = [&](int i, const Pages &p) {
-        const unsigned to = lds0 + (i % STAGES) * SLOT;
-        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, own_token(i), p.id[0], to, kvoff, lane);
-        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, own_token(i) + 16, p.id[1], to + 16 * ROWB, kvoff, lane);
+        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, token_of(i), p.id[0], lds0, kvoff, lane);
+        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, token_of(i) + 16, p.id[1], lds0 + 16 * ROWB, kvoff, lane);
     };
     auto copy_values = [&](int i, const Pages &p) {
-        const unsigned to = lds0 + (STAGES + i % STAGES) * SLOT;
-        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, own_token(i), p.id[0], to, vvoff, lane);
-        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, own_token(i) + 16, p.id[1], to + 16 * ROWB, vvoff, lane);
+        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, token_of(i), p.id[0], lds0 + SLOT, vvoff, lane);
+        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, token_of(i) + 16, p.id[1], lds0 + SLOT + 16 * ROWB, vvoff, lane);
     };
 
-    Pages pg[STAGES + 1];
+    Pages now, next;
     if (count > 0) {
-#pragma unroll
-        for (int s = 0; s <= STAGES; ++s) pg[s] = lookup(s);
-#pragma unroll
-        for (int s = 0; s < STAGES; ++s) {
-            copy_keys(s, pg[s]);
-            copy_values(s, pg[s]);
-        }
+        now = lookup(0);
+        next = lookup(min(1, count - 1));
+        copy_keys(0, now);
+        copy_values(0, now);
     }
     st.load(a, blk, head, blk.rows0, l32, half);  // behind the copies: they are on their way together
     st.clear();
-    if (count > 0) {
-        for (int i = 0; i < count; ++i) {
-            const int tok = token_of(i);
-            const int absent = PAGED ? (pg[0].id[0] < 0 ? 1 : 0) | (pg[0].id[1] < 0 ? 2 : 0) : 0;
-            const Pages next = pg[STAGES];
-            // still on their way: this step's values, and both of the steps behind it
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * STAGES - 1) * COPIES) : "memory");
-            f32x16 s[1];
-            typename E::Weights w[1];
-            E::logits(s[0], st.q, ad, lds0 + (i % STAGES) * SLOT);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
-            copy_keys(i + STAGES, next);
-            st.template weigh<true, 1>(s, w, a.c, tok, a.sink, half, absent);
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * STAGES - 1) * COPIES) : "memory");
-            E::values(st.o, w[0], ad, lds0 + (STAGES + i % STAGES) * SLOT);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            copy_values(i + STAGES, next);
-#pragma unroll
-            for (int k = 0; k < STAGES; ++k) pg[k] = pg[k + 1];
-            pg[STAGES] = lookup(i + STAGES + 1);
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        const bool more = i + 1 < count;
+        const int absent = PAGED ? (now.id[0] < 0 ? 1 : 0) | (now.id[1] < 0 ? 2 : 0) : 0;
+        f32x16 s[1];
+        typename E::Weights w[1];
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");  // this step's values may still be on their way
+        E::logits(s[0], st.q, ad, lds0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
+        if (more) copy_keys(i + 1, next);
+        st.template weigh<1>(s, w, a.c, token_of(i), a.sink, half, absent);
+        if (more)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        E::values(st.o, w[0], ad, lds0 + SLOT);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) {
+            copy_values(i + 1, next);
+            now = next;
+            next = lookup(min(i + 2, count - 1));
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     // What the wavefronts have: sums where their tiles were, the 16-byte pieces of row l32 at place piece ^ l32 % 16, references and sums of weights
     // behind all of them.
-    static_assert(32 * kHeadDim * 4 <= 2 * STAGES * SLOT, "a wavefront's sums fit where its tiles were");
-    auto piece = [&](int w, int at) { return (float4 *)(smem + w * 2 * STAGES * SLOT + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
-    float2 *stats = (float2 *)(smem + WAVES * 2 * STAGES * SLOT);  // [WAVES][32]
+    static_assert(32 * kHeadDim * 4 <= 2 * SLOT, "a wavefront's sums fit where its tiles were");
+    auto piece = [&](int w, int at) { return (float4 *)(smem + w * 2 * SLOT + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
+    float2 *stats = (float2 *)(smem + WAVES * 2 * SLOT);  // [WAVES][32]
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -932,13 +951,13 @@ hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const At
 template <int DT, int WAVES, int TS, int TN, bool PAGED>
 hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(attend_rows<DT, WAVES, TS, TN, PAGED>, p, WAVES * 64, 8 * TN * Elem<DT>::ROWB + 16 + (TS == 2 ? WAVES * 32 * sizeof(float2) : 0), a, s);
+    return launch(attend_rows<DT, WAVES, TS, TN, PAGED>, p, WAVES * 64, 2 * Elem<DT>::RING * TN * Elem<DT>::ROWB + 16 + (TS == 2 ? WAVES * 32 * sizeof(float2) : 0), a, s);
 }
 
-template <int DT, int WAVES, int STAGES, bool PAGED>
+template <int DT, int WAVES, bool PAGED>
 hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(attend_tokens<DT, WAVES, STAGES, PAGED>, p, WAVES * 64, WAVES * (2 * STAGES * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
+    return launch(attend_tokens<DT, WAVES, PAGED>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
 template <bool PAGED>
@@ -947,14 +966,14 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
     hipError_t e;
     if (p.dtype == ILRE_BF16) {
         if (p.rows == 32)
-            e = launch_tokens<ILRE_BF16, 4, 1, PAGED>(p, a, s);
+            e = launch_tokens<ILRE_BF16, 4, PAGED>(p, a, s);
         else if (p.rows == 128)
             e = launch_rows<ILRE_BF16, 8, 2, 64, PAGED>(p, a, s);
         else
             e = launch_rows<ILRE_BF16, 8, 1, 64, PAGED>(p, a, s);
     } else {
         if (p.rows == 32)
-            e = launch_tokens<ILRE_F32, 4, 1, PAGED>(p, a, s);
+            e = launch_tokens<ILRE_F32, 4, PAGED>(p, a, s);
         else
             e = launch_rows<ILRE_F32, 4, 1, 32, PAGED>(p, a, s);
     }
@@ -992,7 +1011,7 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
     const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);
-    const int64_t places = p.rows == 32 && dtype == ILRE_BF16 ? 2 * kNumCU : kNumCU;
+    const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
     const int64_t least = p.rows == 32 ? 2 : dtype == ILRE_F32 ? 2 : 12;
     const int64_t per = std::max<int64_t>((work + places - 1) / places, least);
     int64_t n = (most + per - 1) / per;

@@ -64,6 +64,37 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
     if (token >= a.T) return;
     const int u = lane % UNITS, first = lane / UNITS + wave % WPT * (64 / UNITS);
 
+    const int turned = a.rotary / (2 * E);  // units
+    const bool turn = u < turned;
+    // byte offsets of the unit's two chunks
+    int c0, c1;
+    if (PAIRING == ILRE_ROPE_HALF && turn) {
+        c0 = u * 16;
+        c1 = (u + turned) * 16;
+    } else {
+        c0 = 2 * u * 16;
+        c1 = c0 + 16;
+    }
+    // queries, keys and values as one list of heads
+    const int nq = a.q ? a.Hq : 0, nk = a.k ? a.Hkv : 0, nv = a.v ? a.Hkv : 0, n = nq + nk + nv;
+    auto from = [&](int h) -> const unsigned char * {
+        return h < nq ? a.q + token * a.q_token + h * a.q_head : h < nq + nk ? a.k + token * a.k_token + (h - nq) * a.k_head : a.v + token * a.v_token + (h - nq - nk) * a.v_head;
+    };
+    constexpr int AHEAD = 4;
+    uint4 x[AHEAD], y[AHEAD];
+    auto fetch = [&](int h0) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int h = h0 + i * AT_ONCE;
+            if (h < n) {
+                const unsigned char *p = from(h);
+                x[i] = *(const uint4 *)(p + c0);
+                y[i] = *(const uint4 *)(p + c1);
+            }
+        }
+    };
+    if (WPT > 1) fetch(first);  // on their way while the token's place and angles are worked out
+
     // the token's place in its sequence, and where that is in the cache
     int place = a.first_position + token;
     int64_t cell = -1;
@@ -89,17 +120,6 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
     }
     if (a.positions) place = a.positions[token];
 
-    const int turned = a.rotary / (2 * E);  // units
-    const bool turn = u < turned;
-    // byte offsets of the unit's two chunks
-    int c0, c1;
-    if (PAIRING == ILRE_ROPE_HALF && turn) {
-        c0 = u * 16;
-        c1 = (u + turned) * 16;
-    } else {
-        c0 = 2 * u * 16;
-        c1 = c0 + 16;
-    }
     float co[E], si[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -132,31 +152,16 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
         x = C::put(f);
         y = C::put(g);
     };
-    // queries, keys and values as one list of heads
-    const int nq = a.q ? a.Hq : 0, nk = a.k && cell >= 0 ? a.Hkv : 0, nv = a.v && cell >= 0 ? a.Hkv : 0, n = nq + nk + nv;
-    auto from = [&](int h) -> const unsigned char * {
-        return h < nq ? a.q + token * a.q_token + h * a.q_head : h < nq + nk ? a.k + token * a.k_token + (h - nq) * a.k_head : a.v + token * a.v_token + (h - nq - nk) * a.v_head;
-    };
     auto to = [&](int h) -> unsigned char * {
         return h < nq ? a.q_out + token * a.out_token + h * a.out_head
                       : h < nq + nk ? a.k_pages + cell + (h - nq) * a.head_bytes : a.v_pages + cell + (h - nq - nk) * a.head_bytes;
     };
-    constexpr int AHEAD = 4;
     for (int h0 = first; h0 < n; h0 += AT_ONCE * AHEAD) {
-        uint4 x[AHEAD], y[AHEAD];
+        if (WPT == 1 || h0 != first) fetch(h0);
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int h = h0 + i * AT_ONCE;
-            if (h < n) {
-                const unsigned char *p = from(h);
-                x[i] = *(const uint4 *)(p + c0);
-                y[i] = *(const uint4 *)(p + c1);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int h = h0 + i * AT_ONCE;
-            if (h < n) {
+            if (h < nq || (h < n && cell >= 0)) {
                 if (turn && h < nq + nk) turned_unit(x[i], y[i]);
                 unsigned char *p = to(h);
                 *(uint4 *)(p + c0) = x[i];
@@ -170,7 +175,10 @@ template <int DT, int PAIRING>
 hipError_t launch(const TurnArgs &a, hipStream_t s)
 {
     // few tokens: four wavefronts a token, for the latency; many: one, so that the angles are worked out once
-    if (a.T < 1024)
+    #ifndef RT
+#define RT 1024
+#endif
+    if (a.T < RT)
         hipLaunchKernelGGL((turn_kernel<DT, PAIRING, 4>), dim3((unsigned)a.T), dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL((turn_kernel<DT, PAIRING, 1>), dim3((unsigned)((a.T + 3) / 4)), dim3(kThreads), 0, s, a);
