@@ -438,9 +438,13 @@ def _int32_vector(name: str, t: torch.Tensor, n: int) -> int:
 
 
 def _row_strides(t: torch.Tensor):
-    """Strides of [tokens, heads, d]; those of a single token or head say nothing (torch may hold anything there)."""
-    n, h, d = t.shape
-    return (t.stride(0) if n > 1 else 0), (t.stride(1) if h > 1 else 0)
+    """Strides of [tokens, heads, d]; those of a single token or head say nothing (torch may hold anything there).  0 stands for contiguous in the C ABI, so
+    that a tensor expanded over tokens or heads has to be refused here."""
+    n, h, _ = t.shape
+    s0, s1, _ = t.stride()
+    if (s0 == 0 and n > 1) or (s1 == 0 and h > 1):
+        raise ValueError("tensors expanded over tokens or heads are not supported")
+    return (s0 if n > 1 else 0), (s1 if h > 1 else 0)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -499,6 +503,8 @@ class PagedKV:
             raise ValueError("page_table is an int32 device tensor [n_seq, pages] with contiguous rows")
         n_seq = page_table.shape[0]
         num_pages, Hkv, P, d = k_pages.shape
+        if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
+            raise ValueError("pages expanded over a dimension are not supported")
         if d != 128:
             raise IlreError(ILRE_EUNSUPPORTED, f"head_dim {d} unsupported (only 128)")
         self.k_pages, self.v_pages, self.page_table, self.kv_len, self.cu_q = k_pages, v_pages, page_table, kv_len, cu_q

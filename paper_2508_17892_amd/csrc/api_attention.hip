@@ -16,7 +16,7 @@ int check_common(const ilre_opts *o, int32_t T, int32_t Hq, int32_t d)
     if (T < 0 || Hq < 1) return fail(ILRE_EINVAL, "T must be non-negative, the number of heads positive");
     if (d != ILRE_HEAD_DIM) return fail(ILRE_EUNSUPPORTED, "head_dim %d unsupported (only %d)", d, ILRE_HEAD_DIM);
     if (o->dtype != ILRE_F32 && o->dtype != ILRE_BF16) return fail(ILRE_EUNSUPPORTED, "unknown dtype %d", o->dtype);
-    if ((int64_t)Hq * T > 0x3FFFFFFF) return fail(ILRE_EUNSUPPORTED, "too many query rows");
+    if ((int64_t)Hq * T > 0x3FFFFFFF || T > 4 * ilre::kMaxUnits) return fail(ILRE_EUNSUPPORTED, "too many query rows");
     return ILRE_OK;
 }
 
@@ -113,7 +113,7 @@ int run(ilre::AttnArgs &a, const ilre_attn *t, const ilre_opts *o)
     if (a.T == 0) return ILRE_OK;
     const ilre::AttnPlan p = ilre::make_attn_plan(o->dtype, a.T, a.n_seq, a.Hq, a.Hkv, t->max_q, t->max_kv, t->total_kv, t->sink, t->window,
                                                   o->workspace ? o->workspace_bytes : 0);
-    if ((int64_t)p.nblocks * a.Hkv > 0x7FFFFFFFll) return fail(ILRE_EUNSUPPORTED, "too many query rows");
+    if ((int64_t)p.nblocks * a.Hkv > ilre::kMaxUnits) return fail(ILRE_EUNSUPPORTED, "too many query rows");
     const hipError_t e = ilre::launch_attention(p, a, o->workspace, (hipStream_t)o->stream);
     return e == hipSuccess ? ILRE_OK : hip_fail(e, "attention launch");
 }

@@ -128,6 +128,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, in
     const int n = (b.nrows + rows - 1) / rows;
     if (n == 0) return false;
     const int at = __builtin_amdgcn_readfirstlane(w - before);
+    if (at < 0) return false;  // (boundaries that do not ascend)
     split = at / n;
     b.rows0 = (n - 1 - (at - split * n)) * rows;
     tiles_of(b, mask_of(a), a.G, rows, tile);
@@ -568,9 +569,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         if (DT == ILRE_BF16) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction, two LDS reads, an exponential, three other vector instructions
                 __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
             }
         }
     };
@@ -1016,7 +1018,8 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
     const int64_t per = std::max<int64_t>((work + places - 1) / places, least);
     int64_t n = (most + per - 1) / per;
     const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);
-    n = std::max<int64_t>(1, std::min({n, (int64_t)256, (int64_t)(workspace / (size_t)row_bytes), (int64_t)0x7FFFFFFF / ((int64_t)p.nblocks * Hkv)}));
+    n = std::max<int64_t>(1, std::min({n, (int64_t)256, (int64_t)(workspace / (size_t)row_bytes), kMaxUnits / std::max<int64_t>(p.nblocks * (int64_t)Hkv, 1)}));
+    if ((int64_t)T * Hq > kMaxUnits) n = 1;  // (more rows than a merge is launched for)
     p.nsplit = (int)n;
     p.split_tiles = (int)(n == 1 ? most : std::max(per, (most + n - 1) / n));
     p.bytes = n == 1 ? 0 : (size_t)(n * row_bytes);

@@ -256,6 +256,9 @@ struct AttnPlan {
     size_t bytes;  // of workspace
 };
 
+// Most workgroups of a launch (a dimension counts threads in 32 bits, and no workgroup here has more than 512).
+constexpr int64_t kMaxUnits = (int64_t)1 << 22;
+
 AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
 hipError_t launch_attention(const AttnPlan &p, AttnArgs a, void *workspace, hipStream_t s);
 

@@ -90,6 +90,7 @@ def test_shapes_and_pointers_of_every_call(call):
     assert call(T=-1) == call(**{heads: 0}) == il.ILRE_EINVAL
     assert call(d=64) == il.ILRE_EUNSUPPORTED
     assert call(T=1 << 30, **({"Tk": 1 << 30} if call is prompt else {})) == il.ILRE_EUNSUPPORTED
+    assert call(T=1 << 25, **{heads: 2}, **({"Tk": 1 << 25} if call is prompt else {})) == il.ILRE_EUNSUPPORTED  # more than a launch has room for
     first = "x" if call is rope else "q"
     assert call(**{first: FAKE + 8}) == il.ILRE_EINVAL
     assert call(strides=il.IlreStrides(q_token=100)) == call(strides=il.IlreStrides(q_head=132)) == il.ILRE_EINVAL

@@ -175,6 +175,20 @@ def test_pages_that_no_row_sees_are_not_looked_at():
         assert torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
+def test_boundaries_that_do_not_ascend_stay_within_the_tensors():
+    """What comes out then is nobody's business, but it is written inside the outputs and nowhere else, and the call ends."""
+    _announce("paged, unordered boundaries")
+    x = Paged([40] * 3, [300, 41, 1000], 8, 2, 16, "bf16", seed=21, fill=0.0)
+    guard = torch.full((140, 8, 128), 9.0, device="cuda").bfloat16()
+    for cu in ([0, 90, 10, 120], [100, 50, 20, 0], [-7, 1 << 30, -(1 << 30), 60], [0, 120, 0, 120]):
+        x.dev["cu"].copy_(torch.tensor(cu, dtype=torch.int32))
+        for max_q in (1, 40, 120):
+            il.ilre_paged_attention(x.dev["q"], x.cache(), max_q=max_q, max_kv=1000, out=guard[10:130])
+        il.ilre_rope_append(x.dev["q"], x.dev["q"][:, :2].contiguous(), None, x.cache(), il.ilre_rope_frequencies(128, 1e4), q_out=guard[10:130])
+        torch.cuda.synchronize()
+        assert (guard[:10] == 9).all() and (guard[130:] == 9).all()
+
+
 def test_lengths_beyond_the_table_are_cut():
     _announce("paged, kv_len beyond the table")
     x = Paged([3], [64], 8, 2, 16, "bf16", seed=6)
@@ -435,6 +449,12 @@ def test_binding_refusals_on_the_device():
                     (dict(out=torch.zeros(2, 8, 128, device="cuda")), ValueError), (dict(lse=torch.zeros(2, 4, device="cuda")), ValueError)):
         with pytest.raises(exc):
             il.ilre_prompt_attention(q, k, k, cu, max_q=2, **kw)
+    for a, b in ((q[:1].expand(2, 8, 128), k), (q, k[:, :1].expand(2, 2, 128)), (q[:, :1].expand(2, 8, 128), k)):
+        with pytest.raises(ValueError):  # a stride of 0 would be taken for contiguous
+            il.ilre_prompt_attention(a, b, b, cu, max_q=2)
+    i32 = lambda *x: torch.zeros(*x, dtype=torch.int32, device="cuda")  # noqa: E731
+    with pytest.raises(ValueError):
+        il.PagedKV(torch.zeros(1, 1, 1, 128, device="cuda").expand(4, 2, 16, 128), None, i32(1, 4), i32(1), i32(2))
     with pytest.raises(TypeError):
         il.ilre_prompt_attention(q, k.float(), k.float(), cu, max_q=2)
     with pytest.raises(ValueError):
