@@ -463,3 +463,29 @@ def test_binding_refusals_on_the_device():
         il.ilre_prompt_attention(q, k.repeat(1, 2, 1)[:, :3].contiguous(), k.repeat(1, 2, 1)[:, :3].contiguous(), cu, max_q=2)
     with pytest.raises(ValueError):
         il.ilre_rope(q, il.ilre_rope_frequencies(128, 1e4), torch.zeros(3, dtype=torch.int32, device="cuda"))
+
+
+def test_the_example_answers_as_whole_prompts_would():
+    """The last token's attention, step by step over the paged cache, against the fp64 attention of everything before it."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "stream_recall_answer.py")
+    spec = importlib.util.spec_from_file_location("stream_recall_answer", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    _announce("example")
+    r = ex.main(L=3000, budget=300)
+    torch.cuda.synchronize()
+    assert len(r["idx"]) == 304 and (r["kept"] >= 0).all() and r["answer"].shape == (2, ex.STEPS)
+    f = r["freqs"]
+    for s, prompt in enumerate(r["prompts"]):
+        tokens = torch.cat((prompt.long(), r["answer"][s]))
+        q, k, v = r["layer"].project(r["embed"][tokens])
+        n = len(tokens)
+        q, k = (_f64(il.ilre_rope(t, f)) for t in (q, k))
+        # (matrix products over other numbers of tokens may round a state otherwise: its last bit, 2^-8 of it, moves logits by 2^-7 of their reach)
+        want, want_lse, size, reach = oa.attend(q[-1:], k, _f64(v))
+        got = _f64(r["attended"][s:s + 1])
+        tol = HALF["bf16"] * 2 * np.abs(want) + (2 * 2.0 ** -7 * reach[..., None] + 2 * 2.0 ** -8) * size
+        assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
