@@ -31,6 +31,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 
@@ -43,10 +44,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
-__device__ __forceinline__ uint4 lds_read16(unsigned at) 
-{
-    return __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) u32x4 *)(size_t)at);
-}
+__device__ __forceinline__ u32x4 lds_read16(unsigned at) { return *(const __attribute__((address_space(3))) u32x4 *)(size_t)at; }
 __device__ __forceinline__ float lds_read4(unsigned at) { return *(const __attribute__((address_space(3))) float *)(size_t)at; }
 // Four tokens of the lane's channel: the 16 lanes of a group point at 4 rows x 16 channels (8 bytes each), and each gets a column.
 __device__ __forceinline__ u32x2 lds_read_tr(unsigned at)
@@ -206,9 +204,9 @@ template <>
 struct Elem<ILRE_BF16> {
     static constexpr int ROWB = 256, QREGS = 8, RING = 4;  // QREGS: 16-byte pieces a lane holds of its query row
     struct Weights {
-        uint4 p[2];
+        u32x4 p[2];
     };
-    static __device__ __forceinline__ void mma(f32x16 &acc, const uint4 &x, const uint4 &y)
+    static __device__ __forceinline__ void mma(f32x16 &acc, const u32x4 &x, const u32x4 &y)
     {
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
     }
@@ -225,7 +223,7 @@ struct Elem<ILRE_BF16> {
                 v[db] = (4 * half + (l16 >> 2)) * ROWB + ((db ^ (l16 >> 2)) * 64) + ((lane >> 4) & 1) * 32 + (l16 & 3) * 8;
         }
     };
-    static __device__ __forceinline__ void logits(f32x16 &s, const uint4 (&q)[QREGS], const Addr &ad, unsigned kat)
+    static __device__ __forceinline__ void logits(f32x16 &s, const u32x4 (&q)[QREGS], const Addr &ad, unsigned kat)
     {
         s = f32x16{};
 #pragma unroll
@@ -237,8 +235,8 @@ struct Elem<ILRE_BF16> {
         unsigned u[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-        w.p[0] = make_uint4(u[0], u[1], u[2], u[3]);
-        w.p[1] = make_uint4(u[4], u[5], u[6], u[7]);
+        w.p[0] = u32x4{u[0], u[1], u[2], u[3]};
+        w.p[1] = u32x4{u[4], u[5], u[6], u[7]};
     }
     static __device__ __forceinline__ void values(f32x16 (&o)[4], const Weights &w, const Addr &ad, unsigned vat)
     {
@@ -247,7 +245,7 @@ struct Elem<ILRE_BF16> {
 #pragma unroll
             for (int db = 0; db < 4; ++db) {
                 const u32x2 x = lds_read_tr(ad.v[db] + vat + ks * 16 * ROWB), y = lds_read_tr(ad.v[db] + vat + (ks * 16 + 8) * ROWB);
-                mma(o[db], make_uint4(x[0], x[1], y[0], y[1]), w.p[ks]);
+                mma(o[db], u32x4{x[0], x[1], y[0], y[1]}, w.p[ks]);
             }
     }
 };
@@ -270,13 +268,12 @@ struct Elem<ILRE_F32> {
             for (int j = 0; j < 4; ++j) v[j] = 4 * half * ROWB + j * ROWB + (((l32 >> 2) ^ ((j & 1) << 2)) * 16) + (l32 & 3) * 4;
         }
     };
-    static __device__ __forceinline__ void logits(f32x16 &s, const uint4 (&q)[QREGS], const Addr &ad, unsigned kat)
+    static __device__ __forceinline__ void logits(f32x16 &s, const u32x4 (&q)[QREGS], const Addr &ad, unsigned kat)
     {
         s = f32x16{};
 #pragma unroll
         for (int st = 0; st < 16; ++st) {
-            const uint4 kf = lds_read16(ad.k[st] + kat);
-            const unsigned k[4] = {kf.x, kf.y, kf.z, kf.w}, x[4] = {q[st].x, q[st].y, q[st].z, q[st].w};
+            const u32x4 k = lds_read16(ad.k[st] + kat), x = q[st];
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(x[e]), s, 0, 0, 0);
         }
@@ -306,7 +303,7 @@ __device__ __forceinline__ unsigned first_bits(int n) { return n >= 32 ? ~0u : n
 template <int DT>
 struct State {
     using E = Elem<DT>;
-    uint4 q[E::QREGS];
+    u32x4 q[E::QREGS];
     f32x16 o[4];
     float m, z[4];
     int lo, hi;  // the row sees [0, sink) and [lo, hi)
@@ -324,13 +321,13 @@ struct State {
         const int i = r / a.G, g = r - i * a.G;
         const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head_kv * a.G + g) * a.q_head + half * 16;
 #pragma unroll
-        for (int st = 0; st < E::QREGS; ++st) q[st] = *(const uint4 *)(src + st * 32);
+        for (int st = 0; st < E::QREGS; ++st) q[st] = *(const u32x4 *)(src + st * 32);
         // waited for here, not in the loop over tiles, where that would be a wait for the tile copies as well
 #pragma unroll
-        for (int st = 0; st < E::QREGS; ++st) asm volatile("" : "+v"(q[st].x), "+v"(q[st].y), "+v"(q[st].z), "+v"(q[st].w));
+        for (int st = 0; st < E::QREGS; ++st) asm volatile("" : "+v"(q[st]));
         if (want != r) {
 #pragma unroll
-            for (int st = 0; st < E::QREGS; ++st) q[st] = make_uint4(0, 0, 0, 0);
+            for (int st = 0; st < E::QREGS; ++st) q[st] = u32x4{};
         }
         const int p = max(blk.kv - blk.q_len + i, -1);  // a row in front of its sequence sees nothing
         hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
@@ -650,7 +647,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         static_assert(TS == 1 || WAVES * 32 * 256 <= 2 * RING * SLOT, "half the sums of every wavefront fit where the tiles were");
         __syncthreads();  // everybody is done with the tiles
         const int mine = wave / GROUPS;
-        auto piece = [&](int w, int at) { return (float4 *)(smem + w * 32 * 256 + l32 * 256 + (at ^ (l32 & 15)) * 16); };
+        auto piece = [&](int w, int at) { return (f32x4 *)(smem + w * 32 * 256 + l32 * 256 + (at ^ (l32 & 15)) * 16); };
         float2 *stats = (float2 *)(smem + 2 * RING * SLOT + 16);  // [WAVES][32]
         const int other = wave < GROUPS ? wave + GROUPS : wave - GROUPS;
 #pragma unroll
@@ -658,7 +655,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const f32x16 &x = mine == 0 ? st.o[2 + d] : st.o[d];
-                *piece(wave, d * 8 + 2 * k + half) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                *piece(wave, d * 8 + 2 * k + half) = f32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
             }
         if (half == 0) stats[wave * 32 + l32] = make_float2(m, sum);
         __syncthreads();
@@ -674,7 +671,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
             f32x16 x = mine == 0 ? st.o[d] : st.o[2 + d];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float4 y = *piece(other, d * 8 + 2 * k + half);
+                const f32x4 y = *piece(other, d * 8 + 2 * k + half);
                 x[4 * k] = fmaf(x[4 * k], f, y.x * g);
                 x[4 * k + 1] = fmaf(x[4 * k + 1], f, y.y * g);
                 x[4 * k + 2] = fmaf(x[4 * k + 2], f, y.z * g);
@@ -781,13 +778,13 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
     // What the wavefronts have: sums where their tiles were, the 16-byte pieces of row l32 at place piece ^ l32 % 16, references and sums of weights
     // behind all of them.
     static_assert(32 * kHeadDim * 4 <= 2 * SLOT, "a wavefront's sums fit where its tiles were");
-    auto piece = [&](int w, int at) { return (float4 *)(smem + w * 2 * SLOT + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
+    auto piece = [&](int w, int at) { return (f32x4 *)(smem + w * 2 * SLOT + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
     float2 *stats = (float2 *)(smem + WAVES * 2 * SLOT);  // [WAVES][32]
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            *piece(wave, db * 8 + 2 * k + half) = make_float4(st.o[db][4 * k], st.o[db][4 * k + 1], st.o[db][4 * k + 2], st.o[db][4 * k + 3]);
+            *piece(wave, db * 8 + 2 * k + half) = f32x4{st.o[db][4 * k], st.o[db][4 * k + 1], st.o[db][4 * k + 2], st.o[db][4 * k + 3]};
     const float z = st.sum();
     if (half == 0) stats[wave * 32 + l32] = make_float2(st.m, z);
     __syncthreads();
@@ -812,7 +809,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         for (int w = 0; w < WAVES; ++w) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float4 y = *piece(w, db * 8 + 2 * k + half);
+                const f32x4 y = *piece(w, db * 8 + 2 * k + half);
                 x[4 * k] = fmaf(y.x, ms[w].x, x[4 * k]);
                 x[4 * k + 1] = fmaf(y.y, ms[w].x, x[4 * k + 1]);
                 x[4 * k + 2] = fmaf(y.z, ms[w].x, x[4 * k + 2]);
