@@ -423,28 +423,33 @@ def ilre_gather_ids(input_ids: torch.Tensor, idx: torch.Tensor, out: Optional[to
     return out
 
 
-def _tokens_meta(name: str, t: torch.Tensor, heads: Optional[int] = None):
-    if t.dim() != 3 or not t.is_cuda or t.stride(2) != 1:
+def _tokens_view(name: str, t: torch.Tensor, heads: Optional[int] = None):
+    """(tokens, heads, d, token stride, head stride) of a device tensor [tokens, heads, d].  The strides of a lone token or head say nothing (torch may
+    hold anything there) and go as 0; 0 stands for contiguous in the C ABI, so that a tensor expanded over tokens or heads has to be refused here."""
+    shape = t.shape
+    if len(shape) != 3 or not t.is_cuda:
         raise ValueError(f"{name} is a device tensor [tokens, heads, d] with the head dimension contiguous")
-    if heads is not None and t.shape[1] != heads:
-        raise ValueError(f"{name} has {t.shape[1]} heads, not {heads}")
-    return t.shape
+    n, h, d = shape
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        raise ValueError(f"{name} is a device tensor [tokens, heads, d] with the head dimension contiguous")
+    if heads is not None and h != heads:
+        raise ValueError(f"{name} has {h} heads, not {heads}")
+    if n <= 1:
+        s0 = 0
+    elif s0 == 0:
+        raise ValueError(f"{name}: tensors expanded over tokens or heads are not supported")
+    if h <= 1:
+        s1 = 0
+    elif s1 == 0:
+        raise ValueError(f"{name}: tensors expanded over tokens or heads are not supported")
+    return n, h, d, s0, s1
 
 
 def _int32_vector(name: str, t: torch.Tensor, n: int) -> int:
     if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} is a contiguous int32 device vector of {n} entries")
     return t.data_ptr()
-
-
-def _row_strides(t: torch.Tensor):
-    """Strides of [tokens, heads, d]; those of a single token or head say nothing (torch may hold anything there).  0 stands for contiguous in the C ABI, so
-    that a tensor expanded over tokens or heads has to be refused here."""
-    n, h, _ = t.shape
-    s0, s1, _ = t.stride()
-    if (s0 == 0 and n > 1) or (s1 == 0 and h > 1):
-        raise ValueError("tensors expanded over tokens or heads are not supported")
-    return (s0 if n > 1 else 0), (s1 if h > 1 else 0)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -458,12 +463,13 @@ def _attn_ref(causal: int, sink: int, window: int, max_q: int, max_kv: int, tota
     return ctypes.byref(IlreAttn(ctypes.sizeof(IlreAttn), causal, sink, window, max_q, max_kv, total_kv))
 
 
-def _like(name: str, out: Optional[torch.Tensor], ref: torch.Tensor) -> torch.Tensor:
+def _like(name: str, out: Optional[torch.Tensor], ref: torch.Tensor):
+    """(out, its token stride, its head stride): a new tensor, or the caller's of the same shape and element type."""
     if out is None:
-        return torch.empty(ref.shape, dtype=ref.dtype, device=ref.device)
-    if out.shape != ref.shape or out.dtype != ref.dtype or not out.is_cuda or out.stride(2) != 1:
-        raise ValueError(f"{name} must have the shape and element type of its input, with the head dimension contiguous")
-    return out
+        out = torch.empty(ref.shape, dtype=ref.dtype, device=ref.device)
+    elif out.shape != ref.shape or out.dtype != ref.dtype:
+        raise ValueError(f"{name} must have the shape and element type of its input")
+    return (out, *_tokens_view(name, out)[3:])
 
 
 def ilre_rope_frequencies(rotary: int, base: float, *, scaling: int = ILRE_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
@@ -477,9 +483,11 @@ def ilre_rope_frequencies(rotary: int, base: float, *, scaling: int = ILRE_ROPE_
 def ilre_rope(x: torch.Tensor, freqs: IlreRopeFreqs, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
               pairing: int = ILRE_ROPE_HALF, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotary positions of x [T, H, d]; `out` may be x itself, or a view of the recall's key cache: k_cache[:, a:a+T].transpose(0, 1)."""
-    T, H, d = _tokens_meta("x", x)
-    out = _like("out", out, x)
-    st = _strides_ref(*_row_strides(x), *_row_strides(out))
+    T, H, d, x0, x1 = _tokens_view("x", x)
+    out, o0, o1 = _like("out", out, x)
+    if T == 0:
+        return out
+    st = _strides_ref(x0, x1, o0, o1)
     o = _opts(_dtype_code(x), 0, 0.0, ILRE_SCORE_SUM, None)
     _check(load().ilre_rope(x.data_ptr(), out.data_ptr(), T, H, d, None if positions is None else _int32_vector("positions", positions, T),
                             int(first_position), ctypes.byref(freqs), int(pairing), st, ctypes.byref(o)))
@@ -528,27 +536,28 @@ def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[tor
                      ) -> Optional[torch.Tensor]:
     """Turn queries (returned, or in q_out, which may be q) and keys to their positions (default: their places in the cache) and store keys and values in
     the cache.  q [T, Hq, d], k and v [T, Hkv, d], any token and head strides; q None: keys and values only; v None: keys only."""
-    T, _, d = _tokens_meta("k", k, cache.Hkv)
+    T, _, d, k0, k1 = _tokens_view("k", k, cache.Hkv)
     dt = _dtype_code(k)
-    if dt != cache.dtype or any(t is not None and t.dtype != k.dtype for t in (q, v)):
+    if dt != cache.dtype or (q is not None and q.dtype != k.dtype) or (v is not None and v.dtype != k.dtype):
         raise TypeError("q, k, v and the cache must share an element type")
-    qs = os_ = vs = (0, 0)
+    q0 = q1 = o0 = o1 = v0 = v1 = 0
     Hq = cache.Hkv
     if q is not None:
-        Tq, Hq, dq = _tokens_meta("q", q)
+        Tq, Hq, dq, q0, q1 = _tokens_view("q", q)
         if Tq != T or dq != d:
             raise ValueError("q and k differ in tokens or head dimension")
-        q_out = _like("q_out", q_out, q)
-        qs, os_ = _row_strides(q), _row_strides(q_out)
+        q_out, o0, o1 = _like("q_out", q_out, q)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if v is not None:
-        if _tokens_meta("v", v, cache.Hkv) != k.shape:
+        Tv, _, dv, v0, v1 = _tokens_view("v", v, cache.Hkv)
+        if Tv != T or dv != d:
             raise ValueError("k and v differ in shape")
         if cache.v_pages is None:
             raise ValueError("the cache holds keys only")
-        vs = _row_strides(v)
-    st = _strides_ref(*qs, *os_, *_row_strides(k), *vs)
+    if T == 0:
+        return q_out
+    st = _strides_ref(q0, q1, o0, o1, k0, k1, v0, v1)
     o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
     _check(load().ilre_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
                                    None if v is None else v.data_ptr(), T, Hq, d,
@@ -569,12 +578,12 @@ def alloc_workspace_attention(T: int, n_seq: int, Hq: int, Hkv: int, d: int, max
 
 
 def _attention_outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse: Optional[torch.Tensor], T: int, Hq: int):
-    out = _like("out", out, q)
+    out, o0, o1 = _like("out", out, q)
     if lse is None:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
     elif lse.dtype != torch.float32 or lse.shape != (T, Hq) or not lse.is_contiguous() or not lse.is_cuda:
         raise ValueError("lse is a contiguous float32 device tensor [T, Hq]")
-    return out, lse
+    return out, o0, o1, lse
 
 
 def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv: int, total_kv: int = 0, causal: bool = True, sink: int = 0,
@@ -583,17 +592,19 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
     """Attention of new tokens q [T, Hq, d] over a paged cache that holds them already; returns (out [T, Hq, d], lse float32 [T, Hq]).
     max_q, max_kv, total_kv: the most new tokens and tokens of a sequence, and all tokens together (0: not known); they decide how the work is
     cut up, not what comes out."""
-    T, Hq, d = _tokens_meta("q", q)
+    T, Hq, d, q0, q1 = _tokens_view("q", q)
     dt = _dtype_code(q)
     if dt != cache.dtype:
         raise TypeError("q and the cache must share an element type")
     if cache.v_pages is None:
         raise ValueError("the cache holds keys only")
-    out, lse = _attention_outputs(q, out, lse, T, Hq)
+    out, o0, o1, lse = _attention_outputs(q, out, lse, T, Hq)
+    if T == 0:
+        return out, lse
     if workspace is None:
         workspace = alloc_workspace_attention(T, cache.n_seq, Hq, cache.Hkv, d, max_q, max_kv, total_kv=total_kv, dtype=dt, device=q.device)
     at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
-    st = _strides_ref(*_row_strides(q), *_row_strides(out))
+    st = _strides_ref(q0, q1, o0, o1)
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
     _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, at, cache._ref, st, ctypes.byref(o)))
     return out, lse
@@ -605,11 +616,11 @@ def ilre_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_
                           ) -> Tuple[torch.Tensor, torch.Tensor]:
     """Attention of packed sequences, q [T, Hq, d], k and v [Tk, Hkv, d], cut up by cu_q and cu_k (int32 [n_seq + 1]; cu_k None: cu_q); the last
     queries of a sequence stand at its last keys.  Returns (out [T, Hq, d], lse float32 [T, Hq])."""
-    T, Hq, d = _tokens_meta("q", q)
-    Tk, Hkv, dk = _tokens_meta("k", k)
-    if v.shape != k.shape or dk != d:
+    T, Hq, d, q0, q1 = _tokens_view("q", q)
+    Tk, Hkv, dk, k0, k1 = _tokens_view("k", k)
+    Tv, _, dv, v0, v1 = _tokens_view("v", v, Hkv)
+    if Tv != Tk or dv != dk or dk != d:
         raise ValueError("k and v differ in shape, or from q in the head dimension")
-    _tokens_meta("v", v)
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise TypeError("q, k and v must share an element type")
     n_seq = cu_q.numel() - 1
@@ -617,11 +628,13 @@ def ilre_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_
     pk = None if cu_k is None else _int32_vector("cu_k", cu_k, n_seq + 1)
     max_k = max_q if max_k is None else max_k
     dt = _dtype_code(q)
-    out, lse = _attention_outputs(q, out, lse, T, Hq)
+    out, o0, o1, lse = _attention_outputs(q, out, lse, T, Hq)
+    if T == 0:
+        return out, lse
     if workspace is None:
         workspace = alloc_workspace_attention(T, n_seq, Hq, Hkv, d, max_q, max_k, total_kv=Tk, dtype=dt, device=q.device)
     at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_k), Tk)
-    st = _strides_ref(*_row_strides(q), *_row_strides(out), *_row_strides(k), *_row_strides(v))
+    st = _strides_ref(q0, q1, o0, o1, k0, k1, v0, v1)
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
     _check(load().ilre_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Tk, Hq, Hkv, d, pq, pk, n_seq, at, st, ctypes.byref(o)))
     return out, lse

@@ -279,7 +279,7 @@ int ilre_prompt_attention(const void *q, const void *k, const void *v, void *out
 {
     int rc = check_common(opts, T, Hq, d);
     if (rc || (rc = check_attn(attn))) return rc;
-    if (!q || !k || !v || !out || !strides || !cu_q) return fail(ILRE_EINVAL, "q, k, v, out, cu_q or strides is null");
+    if (!q || ((!k || !v) && Tk != 0) || !out || !strides || !cu_q) return fail(ILRE_EINVAL, "q, k, v, out, cu_q or strides is null");
     if (Hkv < 1 || n_seq < 1 || Tk < 0) return fail(ILRE_EINVAL, "Hkv and n_seq must be positive, Tk non-negative");
     if (Hq % Hkv != 0) return fail(ILRE_EINVAL, "Hq (%d) must be a multiple of Hkv (%d)", Hq, Hkv);
     if (!cu_k && Tk != T) return fail(ILRE_EINVAL, "without cu_k there are as many keys as queries");

@@ -122,9 +122,10 @@ def test_cache_description(kw, status):
 
 
 def test_prompt_and_append_arguments():
-    for kw in (dict(k=None), dict(v=None), dict(cu_q=None), dict(Hkv=0), dict(Hkv=3), dict(n_seq=0), dict(Tk=-1), dict(Tk=5), dict(k=FAKE + 4), dict(v=FAKE + 4),
+    for kw in (dict(k=None, Tk=5, cu_k=FAKE), dict(v=None, Tk=5, cu_k=FAKE), dict(cu_q=None), dict(Hkv=0), dict(Hkv=3), dict(n_seq=0), dict(Tk=-1), dict(Tk=5), dict(k=FAKE + 4), dict(v=FAKE + 4),
                dict(strides=il.IlreStrides(k_token=64)), dict(strides=il.IlreStrides(v_head=130))):
         assert prompt(**kw) == il.ILRE_EINVAL, kw
+    assert prompt(k=None, v=None) == il.ILRE_OK  # no keys at all
     assert prompt(Tk=5, cu_k=FAKE) == il.ILRE_OK and prompt(Tk=0x7FFFFFFF, cu_k=FAKE) == il.ILRE_EUNSUPPORTED
     for kw in (dict(k=None), dict(q=None), dict(q_out=None), dict(cache=_cache(v_pages=None)), dict(freqs=None), dict(freqs=_freqs(struct_size=3)),
                dict(freqs=_freqs(rotary=0)), dict(freqs=_freqs(rotary=144)), dict(freqs=_freqs(magnitude=float("inf"))), dict(freqs=_freqs(bad_freq=float("nan"))),

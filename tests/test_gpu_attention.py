@@ -335,6 +335,28 @@ def test_a_neighbour_in_the_packing_may_hold_anything():
         _check(out[s], lse[s], *oa.attend(_f64(q[s]), _f64(k[s]), _f64(v[s])), mine[1] - mine[0], "bf16")
 
 
+def test_no_new_tokens_and_no_keys():
+    _announce("nothing to do")
+    for dtype in DT.values():
+        x = Paged([0, 0], [5, 0], 8, 2, 16, "bf16" if dtype == torch.bfloat16 else "f32")
+        out, lse = il.ilre_paged_attention(x.dev["q"], x.cache(), max_q=0, max_kv=5)
+        assert out.shape == (0, 8, 128) and lse.shape == (0, 8)
+        f = il.ilre_rope_frequencies(128, 10000.0)
+        e = torch.empty(0, 2, 128, dtype=dtype, device="cuda")
+        before = x.kp.clone()
+        assert il.ilre_rope(e, f).shape == (0, 2, 128)
+        assert il.ilre_rope_append(x.dev["q"], e, e, x.cache(), f).shape == (0, 8, 128)
+        assert torch.equal(before.nan_to_num(7.0), x.kp.nan_to_num(7.0))
+        cu = torch.zeros(3, dtype=torch.int32, device="cuda")
+        out, lse = il.ilre_prompt_attention(x.dev["q"], e, e, cu, max_q=0)
+        assert out.shape == (0, 8, 128)
+        # queries without a single key
+        q = torch.randn(4, 8, 128, device="cuda").to(dtype)
+        cu_q = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+        out, lse = il.ilre_prompt_attention(q, e, e, cu_q, cu_k=cu[:2], max_q=4, max_k=0)
+        assert (out == 0).all() and (lse == -float("inf")).all()
+
+
 def test_softmax_scale():
     _announce("prompt, scales")
     g = torch.Generator().manual_seed(12)
