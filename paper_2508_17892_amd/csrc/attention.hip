@@ -91,15 +91,17 @@ __device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b
 template <bool PAGED>
 __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, int tile, Block &b, int &split)
 {
-    int seq = 0, before = 0;
-    if (a.n_seq > 1) {
+    int before = 0;
+    if (a.n_seq == 1) {
+        sequence_of<PAGED>(a, 0, b);
+    } else {
         const int lane = threadIdx.x & 63;
         bool found = false;
         for (int base = 0; base < a.n_seq && !found; base += 64) {
             const int s = base + lane;
+            Block x{};
             int n = 0;
             if (s < a.n_seq) {
-                Block x;
                 sequence_of<PAGED>(a, s, x);
                 n = (x.nrows + rows - 1) / rows;
                 if (a.nsplit > 1 && n > 0) {
@@ -111,22 +113,23 @@ __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, in
             int sum = n;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
-                const int x = __shfl_up(sum, o);
-                if (lane >= o) sum += x;
+                const int y = __shfl_up(sum, o);
+                if (lane >= o) sum += y;
             }
             const unsigned long long past = __ballot(before + sum > w);
             if (past) {
                 const int at = __builtin_ctzll(past);
-                seq = base + at;
-                before += __shfl(sum - n, at);
+                auto of = [&](int y) { return __builtin_amdgcn_readlane(y, at); };
+                b.seq = base + at;
+                b.q0 = of(x.q0), b.q_len = of(x.q_len), b.kv = of(x.kv), b.kv0 = of(x.kv0), b.nrows = of(x.nrows);
+                before += of(sum - n);
                 found = true;
             } else {
-                before += __shfl(sum, 63);
+                before += __builtin_amdgcn_readlane(sum, 63);
             }
         }
         if (!found) return false;
     }
-    sequence_of<PAGED>(a, __builtin_amdgcn_readfirstlane(seq), b);
     const int n = (b.nrows + rows - 1) / rows;
     if (n == 0) return false;
     const int at = __builtin_amdgcn_readfirstlane(w - before);
