@@ -27,6 +27,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 namespace ilre {
 
@@ -340,26 +341,39 @@ struct State {
         hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
         lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
     }
-    // The logits of SUB x 32 tokens from `tok` on become weights; the running maximum is followed.  `absent`: bit k: tokens 16 k .. 16 k + 15 are on no page.
-    // What the row sees of 32 tokens is a word of bits, two instructions a logit: nearly every tile that comes here has an edge in it, and code that
-    // is not there need not be fetched.
-    template <int SUB>
-    __device__ __forceinline__ void weigh(f32x16 (&s)[SUB], typename E::Weights (&w)[SUB], float c, int tok, int sink, int half, int absent)
+    // Logits of tokens that the row does not see become -inf: 32 tokens from `at` on; bit 0 / 1 of `absent`: the first / last 16 are on no page.  What the row
+    // sees is a word of bits, a few instructions a logit: nearly every tile that comes here has an edge in it.
+    __device__ __forceinline__ void hide(f32x16 &s, int at, int sink, int half, int absent) const
     {
-        float top = -INFINITY;
+        unsigned bits = first_bits(hi - at) & (~first_bits(lo - at) | first_bits(sink - at));
+        bits &= ~((absent & 1 ? 0xFFFFu : 0u) | (absent & 2 ? 0xFFFF0000u : 0u));
+        bits >>= 4 * half;
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            const int at = tok + 32 * u;
-            unsigned bits = first_bits(hi - at) & (~first_bits(lo - at) | first_bits(sink - at));
-            bits &= ~((absent >> (2 * u) & 1 ? 0xFFFFu : 0u) | (absent >> (2 * u + 1) & 1 ? 0xFFFF0000u : 0u));
-            bits >>= 4 * half;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int seen = (int)(bits << (31 - (8 * (i >> 2) + (i & 3)))) >> 31;
-                s[u][i] = __int_as_float((__float_as_int(s[u][i]) & seen) | (__float_as_int(-INFINITY) & ~seen));
-                top = fmaxf(top, s[u][i]);
-            }
+        for (int i = 0; i < 16; ++i) {
+            const int seen = (int)(bits << (31 - (8 * (i >> 2) + (i & 3)))) >> 31;
+            s[i] = __int_as_float((__float_as_int(s[i]) & seen) | (__float_as_int(-INFINITY) & ~seen));
         }
+    }
+    __device__ __forceinline__ float largest(const f32x16 &s) const
+    {
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        return top;
+    }
+    // A reference for a row that has none, from the logits of 32 tokens that it sees.
+    __device__ __forceinline__ void refer(const f32x16 &s, float c)
+    {
+        const float top = largest(s);
+        m = fmaxf(fmaxf(top, other_half(top)) * c, kFloor);
+    }
+    // The logits of SUB x 32 tokens become weights; the running maximum is followed.
+    template <int SUB>
+    __device__ __forceinline__ void weigh(const f32x16 (&s)[SUB], typename E::Weights (&w)[SUB], float c)
+    {
+        float top = largest(s[0]);
+#pragma unroll
+        for (int u = 1; u < SUB; ++u) top = fmaxf(top, largest(s[u]));
         top = fmaxf(top, other_half(top));
         const float mnew = fmaxf(m, top * c);
         if (__ballot(mnew != m)) {
@@ -375,7 +389,7 @@ struct State {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) weigh_kept(s[u], w[u], c);
     }
-    // The same against the reference as it is, all tokens seen.
+    // The same against the reference as it is.
     __device__ __forceinline__ void weigh_kept(const f32x16 &s, typename E::Weights &w, float c)
     {
         float p[16];
@@ -545,7 +559,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     };
     auto keys_at = [&](int i, int sub) { return lds0 + i % RING * SLOT + (part + sub * 32) * ROWB; };
     auto values_at = [&](int i, int sub) { return lds0 + (RING + i % RING) * SLOT + (part + sub * 32) * ROWB; };
-    auto follow_tile = [&](int i, bool careful) {
+    // A tile that some rows see a part of, following the maximum or (kept) against the references as they are.
+    auto edge_tile = [&](int i, bool careful, auto kept) {
         advance(i);
         if (idle) return;
         const int tok = token_of(i) + part;
@@ -557,7 +572,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         if (PAGED && careful) {
             for (int k = 0; k < SUB * 2; ++k) absent |= (page_of(a, blk, tok + 16 * k) < 0 ? 1 : 0) << k;
         }
-        st.template weigh<SUB>(s, w, a.c, tok, a.sink, half, absent);
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub) st.hide(s[sub], tok + 32 * sub, a.sink, half, absent >> (2 * sub));
+        if (kept.value) {
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) st.weigh_kept(s[sub], w[sub], a.c);
+        } else {
+            st.template weigh<SUB>(s, w, a.c);
+        }
 #pragma unroll
         for (int sub = 0; sub < SUB; ++sub) E::values(st.o, w[sub], ad, values_at(i, sub));
     };
@@ -588,6 +610,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         f32x16 s[2];
         typename E::Weights w;
         E::logits(s[0], st.q, ad, keys_at(g1, 0));
+        if (g1 == 0) st.refer(s[0], a.c);
         advance(g1);
         // the first step has no weights before it
         if (SUB == 2) {
@@ -617,22 +640,30 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         E::values(st.o, w, ad, values_at(g2 - 1, SUB - 1));
     };
 
-    // kept: behind the first tile that all rows see whole, as far as they do
+    // g1 .. g2 - 1: the tiles that all rows see whole, if the rows have references before them: from the first 32 tokens of the range's first tile, from the
+    // sink part, or from one such tile that is followed.
     int g1 = count, g2 = count;
     if (DT == ILRE_BF16) {
         const int from = a.window > 0 ? max((blk.all_lo + TN - 1) / TN, blk.w0) - blk.w0 + blk.ns : 0;
         const int to = a.window > 0 ? blk.all_hi / TN - blk.w0 + blk.ns : blk.all_hi / TN;
-        g1 = max(from - first, 0) + 1;
+        g1 = max(from - first, 0);
+        if (g1 > 0 && (first > 0 || blk.ns == 0)) ++g1;
         g2 = min(to - first, count);
-        if (g2 - g1 < 2) g1 = g2 = count;
+        if (g2 <= g1) g1 = g2 = count;
     }
     if (count > 0) begin();
     st.load(a, blk, head, row0, l32, half);  // behind the copies: they are on their way together
     st.clear();
     if (count > 0) {
-        for (int i = 0; i < g1; ++i) follow_tile(i, false);
-        if (g1 < g2) kept_tiles(g1, g2);
-        for (int i = g2; i < count; ++i) follow_tile(i, false);
+        for (int i = 0; i < g1; ++i) edge_tile(i, false, std::false_type{});
+        if (g1 < g2) {
+            if (g1 == 0) {  // nobody has waited for the first keys yet (other than along with the queries)
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+            }
+            kept_tiles(g1, g2);
+        }
+        for (int i = g2; i < count; ++i) edge_tile(i, false, std::true_type{});
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (PAGED || g1 < g2) {
             bool far = false;
@@ -643,7 +674,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
             if (__builtin_amdgcn_readfirstlane(*flag)) {
                 st.clear();
                 begin();
-                for (int i = 0; i < count; ++i) follow_tile(i, PAGED);
+                for (int i = 0; i < count; ++i) edge_tile(i, PAGED, std::false_type{});
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             }
         }
@@ -771,7 +802,8 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         E::logits(s[0], st.q, ad, lds0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
         if (more) copy_keys(i + 1, next);
-        st.template weigh<1>(s, w, a.c, token_of(i), a.sink, half, absent);
+        st.hide(s[0], token_of(i), a.sink, half, absent);
+        st.template weigh<1>(s, w, a.c);
         if (more)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
         else
