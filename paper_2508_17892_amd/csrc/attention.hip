@@ -12,7 +12,7 @@
 // which place of the contraction is free as long as both operands agree, and V^T is read from LDS with the transposing
 // read (four tokens of one channel a lane) in that very order.  P never goes through LDS.
 //
-// Weights are taken relative to a reference m per row.  attend_rows follows the running maximum over a row's first tiles and then
+// Weights are taken relative to a reference m per row.  attend_rows takes it from the first tokens that all of a workgroup's rows see and then
 // keeps it: any m gives the same quotient as long as the exponentials stay in range, and the maximum, the rescaling and the branch in
 // front of it are a fifth of the vector work.  A row whose later logits exceed its reference by more than 2^60 shows in its
 // sum, and the workgroup walks its tiles again, following the maximum all the way.
@@ -1026,7 +1026,7 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 
 // Which kernel, and how the tokens are cut up.
 //   - Up to 32 rows: attend_tokens.  More: 256 rows a workgroup, unless that leaves compute units without one and the lists are short, or there are 128 rows
-//     at most: then 128 (1024 tokens of 32/8 heads, window 512: 128 workgroups of 256 rows, cut in two, 54 us with the merge; 256 of 128 rows 25 us; over
+//     at most: then 128 (1024 tokens of 32/8 heads, window 512: 128 workgroups of 256 rows, cut in two, 54 us with the merge; 256 of 128 rows 24 us; over
 //     66560 tokens 256 rows cut in two take 1.02 ms, 128 rows 1.24 ms).
 //   - A list is cut so that the ranges of all sequences together are one for each place that LDS has room for (twice as many: 48 requests 75 -> 78 us).  A
 //     range has 2 tiles of 128 tokens at least (1: one token of 4097 15.1 -> 18.1 us, with a merge of 33; 4: 17.1), 12 of 64 (the merge costs as much as 8), or 2
