@@ -292,7 +292,8 @@ int ilre_rope(const void *x, void *out, int32_t T, int32_t H, int32_t d, const i
    kv_len - q_len + i.  (kv_len counts the new tokens already.)  Places outside the table, or on no page, are left out.
    q, q_out   dev  [T, Hq, d] (strides->q_*, out_*); both NULL: keys and values only.  q_out may be q
    k, v       dev  [T, Hkv, d] (strides->k_*, v_*); v NULL: keys only (the cache's v_pages may then be NULL)
-   positions  dev  T int32, or NULL: the tokens' places in the cache */
+   positions  dev  T int32, or NULL: the tokens' places in the cache
+   Tokens of no sequence (past cu_q[n_seq], before cu_q[0]) are left out, and their part of q_out as it is. */
 int ilre_rope_append(const void *q, void *q_out, const void *k, const void *v, int32_t T, int32_t Hq, int32_t d, const int32_t *positions,
                      const ilre_rope_freqs *freqs, int32_t pairing, const ilre_paged_kv *cache, const ilre_strides *strides, const ilre_opts *opts);
 

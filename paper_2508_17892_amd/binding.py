@@ -522,8 +522,8 @@ class PagedKV:
         c.page_tokens, c.num_pages, c.Hkv = P, num_pages, Hkv
         # the strides of a lone page or head say nothing
         c.stride_token = k_pages.stride(2)
-        c.stride_head = k_pages.stride(1) if Hkv > 1 else max(k_pages.stride(1), d)
-        c.stride_page = k_pages.stride(0) if num_pages > 1 else max(k_pages.stride(0), d)
+        c.stride_head = k_pages.stride(1) if Hkv > 1 else d
+        c.stride_page = k_pages.stride(0) if num_pages > 1 else d
         c.k_pages, c.v_pages = k_pages.data_ptr(), 0 if v_pages is None else v_pages.data_ptr()
         c.page_table, c.table_width, c.n_seq = page_table.data_ptr(), page_table.shape[1], n_seq
         c.table_stride = page_table.stride(0) if n_seq > 1 else page_table.shape[1]
