@@ -1031,8 +1031,9 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 //   - A list is cut so that the ranges of all sequences together are one for each place that LDS has room for (twice as many: 48 requests 75 -> 78 us).
 //     Up to three tiles of 128 tokens stay whole, as a merge costs more (four requests of 300 tokens 11.9 -> 9.3 us); more are cut down to single tiles while those
 //     are one for each compute unit at most (four requests of 1000 tokens: 1 11.0 us, 2 12.8; one of 2000: 10.5 and 10.9), else into two at least (one of 4097: 12.1 and
-//     11.7; 30000 tokens, 8/2 heads: 17.7 and 15.7).  More rows: 12 tiles of 64 tokens at least (the merge costs as much as 8), 2 of 32 in fp32 (prompts of
-//     77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6, 6 74).
+//     11.7; 30000 tokens, 8/2 heads: 17.7 and 15.7).  More rows: 12 tiles of 64 tokens at least, and 4 while the merge has little to do (32/8 heads, 4096 tokens: 16
+//     new ones 18.4 us with 4, 25.2 with 12, 64 29.7 and 35.7, 200 51.9 and 40.3), 2 of 32 in fp32 (prompts of 77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6,
+//     6 74).
 AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
 {
     AttnPlan p{};
@@ -1062,7 +1063,7 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
     const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);
     const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
-    const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : 12;
+    const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
     const int64_t per = std::max<int64_t>((work + places - 1) / places, least);
     int64_t n = (most + per - 1) / per;
     const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);
