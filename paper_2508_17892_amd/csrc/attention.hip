@@ -86,9 +86,8 @@ __device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b
     b.nrows = b.q_len * a.G;
 }
 
-// Unit w: a block of `rows` rows and one range of its tiles.  The units of all sequences come one after the other, a sequence's first ranges before its second
-// ones and, within them, the last block first (with a causal mask it has most to do); what is left of the grid has none and ends at once, behind all that
-// work (between them, 48 requests with contexts of 1 to 16384 tokens, it cost 10 of 85 us).  False where there is none.
+// Unit w of the call.  The units of all sequences come one after the other; what is left of the grid has none and ends at once, behind all that work (between
+// them, 48 requests with contexts of 1 to 16384 tokens, it cost 10 of 85 us).  False where there is none.
 template <bool PAGED>
 __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, int tile, Block &b, int &split)
 {
@@ -104,12 +103,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, in
             int n = 0;
             if (s < a.n_seq) {
                 sequence_of<PAGED>(a, s, x);
-                n = (x.nrows + rows - 1) / rows;
-                if (a.nsplit > 1 && n > 0) {
-                    x.rows0 = (n - 1) * rows;
-                    tiles_of(x, mask_of(a), a.G, rows, tile);
-                    n *= ranges_of(x.nt + (a.window > 0), a.split_tiles, a.nsplit);  // (with a window another block may have one tile more)
-                }
+                n = units_of(x, mask_of(a), a.G, rows, tile, a.split_tiles, a.nsplit);
             }
             int sum = n;
 #pragma unroll
@@ -131,14 +125,8 @@ __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, in
         }
         if (!found) return false;
     }
-    const int n = (b.nrows + rows - 1) / rows;
-    if (n == 0) return false;
-    const int at = __builtin_amdgcn_readfirstlane(w - before);
-    if (at < 0) return false;  // (boundaries that do not ascend)
-    split = at / n;
-    b.rows0 = (n - 1 - (at - split * n)) * rows;
-    tiles_of(b, mask_of(a), a.G, rows, tile);
-    return split < ranges_of(b.nt, a.split_tiles, a.nsplit);
+    const int at = __builtin_amdgcn_readfirstlane(w - before);  // (negative where boundaries do not ascend)
+    return take_unit(b, at, mask_of(a), a.G, rows, tile, a.split_tiles, a.nsplit, split);
 }
 
 // ------------------------------------------------------------------------------------------------ tile copies

@@ -56,6 +56,34 @@ __host__ __device__ __forceinline__ int ranges_of(int nt, int per, int nsplit)
     return n < nsplit ? n : nsplit;
 }
 
+// A unit is a block of `rows` rows and one range of its tiles.  A sequence's units have consecutive numbers: its first ranges before its second ones and, within
+// them, the last block first (with a causal mask it has most to do).
+__host__ __device__ __forceinline__ int blocks_of(const Block &b, int rows) { return (b.nrows + rows - 1) / rows; }
+
+// How many numbers a sequence (q_len, kv, nrows) has: at least one for each range of each block.  Without a window no block has more tiles than the last one.  With
+// one, a block whose first and last rows are `apart` tokens apart sees window + apart tokens in a row, the last block window at the least (where a sequence is shorter
+// than that it sees everything), and the two may lie otherwise over the tiles: (apart - 1) / tile, rounded up, + 1 tiles more.  Numbers that no range needs end at once.
+__host__ __device__ __forceinline__ int units_of(Block b, const Mask &m, int G, int rows, int tile, int per, int nsplit)
+{
+    const int n = blocks_of(b, rows);
+    if (nsplit == 1 || n == 0) return n;
+    b.rows0 = (n - 1) * rows;
+    tiles_of(b, m, G, rows, tile);
+    const int apart = (rows + G - 2) / G;
+    return n * ranges_of(m.window > 0 ? b.nt + (apart + tile - 2) / tile + 1 : b.nt, per, nsplit);
+}
+
+// The sequence's unit number `at`: fills in the block and its tiles, and says which range.  False where the block has no such range.
+__host__ __device__ __forceinline__ bool take_unit(Block &b, int at, const Mask &m, int G, int rows, int tile, int per, int nsplit, int &split)
+{
+    const int n = blocks_of(b, rows);
+    if (n == 0 || at < 0) return false;
+    split = at / n;
+    b.rows0 = (n - 1 - (at - split * n)) * rows;
+    tiles_of(b, m, G, rows, tile);
+    return split < ranges_of(b.nt, per, nsplit);
+}
+
 // The page table's column for token t: within the table whatever t >= 0 is.
 __host__ __device__ __forceinline__ int page_column(int t, int page_shift, int table_width)
 {

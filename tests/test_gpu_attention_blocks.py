@@ -1,0 +1,91 @@
+"""GPU parity of the attention kernels where a call is cut into blocks and ranges, against the fp64 oracle; tolerances as in test_gpu_attention."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_17892_amd as il
+from oracle import attention as oa
+from test_gpu_attention import DT, Paged, _announce, _check, _f64
+
+pytestmark = pytest.mark.gpu
+
+
+class Packed:
+    """Random packed prompts, keys and values side by side in one row."""
+
+    def __init__(self, lens, Hq, Hkv, dtype, seed):
+        g = torch.Generator().manual_seed(seed)
+        self.lens, self.dtype, self.Hq, self.Hkv = lens, dtype, Hq, Hkv
+        self.q = torch.randn(sum(lens), Hq, 128, generator=g).to(DT[dtype])
+        self.kv = torch.randn(sum(lens), 2 * Hkv + 1, 128, generator=g).to(DT[dtype])
+        self.dev = self.q.cuda(), self.kv.cuda(), torch.tensor([0] + list(np.cumsum(lens)), dtype=torch.int32, device="cuda")
+
+    def attend(self, **kw):
+        q, kv, cu = self.dev
+        return il.ilre_prompt_attention(q, kv[:, :self.Hkv], kv[:, self.Hkv + 1:], cu, max_q=max(self.lens), **kw)
+
+    def workspace(self):
+        return il.alloc_workspace_attention(sum(self.lens), len(self.lens), self.Hq, self.Hkv, 128, max(self.lens), max(self.lens), total_kv=sum(self.lens),
+                                            dtype=il.ILRE_BF16 if self.dtype == "bf16" else il.ILRE_F32)
+
+    def check(self, out, lse, **mask):
+        row = 0
+        for n in self.lens:
+            s = slice(row, row + n)
+            _check(out[s], lse[s], *oa.attend(_f64(self.q[s]), _f64(self.kv[s, :self.Hkv]), _f64(self.kv[s, self.Hkv + 1:]), **mask), n, self.dtype, f"{n} tokens")
+            row += n
+
+
+def _workspace_of(x, Hq, Hkv):
+    return il.alloc_workspace_attention(sum(x.q_lens), len(x.q_lens), Hq, Hkv, 128, max(x.q_lens), max(x.kv_lens), total_kv=sum(x.kv_lens),
+                                        dtype=il.ILRE_BF16 if x.dtype == "bf16" else il.ILRE_F32)
+
+
+# The last block of a sequence, often of a single row, sees fewer tiles of its window than a full one, and lists are cut into ranges right in between.
+STREAMS = [
+    # q_lens, kv_lens, Hq, Hkv, dtype, sink, window
+    ([14, 132], [295, 528], 1, 1, "bf16", 4, 320),
+    ([129, 129], [600, 600], 4, 4, "bf16", 4, 320),
+    ([388, 79], [2725, 2332], 4, 4, "bf16", 4, 64),
+    ([262, 27, 16], [1623, 363, 332], 1, 1, "bf16", 140, 1173),
+    ([97, 282, 254], [1166, 1820, 576], 16, 8, "bf16", 168, 1183),
+    ([215, 69, 79], [1216, 382, 612], 3, 1, "bf16", 4, 624),
+    ([158, 63, 6], [1273, 638, 1074], 20, 4, "bf16", 4, 622),
+    ([134, 0], [364, 109], 1, 1, "f32", 4, 192),
+    ([150, 150], [900, 900], 8, 8, "f32", 4, 512),
+    ([46, 76], [18, 303], 4, 2, "f32", 4, 97),
+    ([392, 444], [2019, 1118], 12, 4, "f32", 4, 512),
+    ([139, 129], [509, 286], 5, 1, "f32", 20, 240),
+    ([249, 148], [255, 464], 7, 1, "f32", 4, 113),
+]
+
+
+@pytest.mark.parametrize("q_lens,kv_lens,Hq,Hkv,dtype,sink,window", STREAMS, ids=[f"{c[4]}-{c[2]}.{c[3]}-q{sum(c[0])}-kv{sum(c[1])}-w{c[6]}" for c in STREAMS])
+def test_streamed_chunks_of_several_sequences(q_lens, kv_lens, Hq, Hkv, dtype, sink, window):
+    _announce(f"streams {q_lens} of {kv_lens} {Hq}/{Hkv} {dtype} sink {sink} window {window}")
+    x = Paged(q_lens, kv_lens, Hq, Hkv, 16, dtype, seed=sum(kv_lens) + Hq)
+    ws = _workspace_of(x, Hq, Hkv)
+    ws.fill_(255)  # NaN, in the partial results and their logarithms: what no workgroup writes must not be added up
+    out, lse = x.attend(sink=sink, window=window, workspace=ws)
+    torch.cuda.synchronize()
+    x.check(out, lse, sink=sink, window=window)
+
+
+PACKED = [
+    ([171, 0, 285], 1, 1, "f32", 4, 70),
+    ([104, 223], 3, 1, "f32", 4, 39),
+    ([282, 229], 20, 4, "f32", 4, 58),
+    ([15, 221], 7, 1, "f32", 4, 59),
+    ([700, 300, 513], 4, 4, "bf16", 4, 128),
+]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,dtype,sink,window", PACKED, ids=[f"{c[3]}-{c[1]}.{c[2]}-{sum(c[0])}-w{c[5]}" for c in PACKED])
+def test_packed_prompts_with_a_window(lens, Hq, Hkv, dtype, sink, window):
+    _announce(f"packed {lens} {Hq}/{Hkv} {dtype} sink {sink} window {window}")
+    x = Packed(lens, Hq, Hkv, dtype, sum(lens))
+    ws = x.workspace()
+    ws.fill_(255)
+    out, lse = x.attend(sink=sink, window=window, workspace=ws)
+    torch.cuda.synchronize()
+    x.check(out, lse, sink=sink, window=window)
