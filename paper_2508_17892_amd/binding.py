@@ -510,6 +510,8 @@ class PagedKV:
         if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_cuda or page_table.stride(1) != 1:
             raise ValueError("page_table is an int32 device tensor [n_seq, pages] with contiguous rows")
         n_seq = page_table.shape[0]
+        if n_seq > 1 and page_table.stride(0) == 0:  # (0 stands for contiguous in the C ABI)
+            raise ValueError("a page_table expanded over sequences is not supported")
         num_pages, Hkv, P, d = k_pages.shape
         if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
             raise ValueError("pages expanded over a dimension are not supported")
