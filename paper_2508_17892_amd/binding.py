@@ -605,6 +605,8 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
         return out, lse
     if workspace is None:
         workspace = alloc_workspace_attention(T, cache.n_seq, Hq, cache.Hkv, d, max_q, max_kv, total_kv=total_kv, dtype=dt, device=q.device)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace is a contiguous device tensor")
     at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
     st = _strides_ref(q0, q1, o0, o1)
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
@@ -635,6 +637,8 @@ def ilre_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_
         return out, lse
     if workspace is None:
         workspace = alloc_workspace_attention(T, n_seq, Hq, Hkv, d, max_q, max_k, total_kv=Tk, dtype=dt, device=q.device)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace is a contiguous device tensor")
     at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_k), Tk)
     st = _strides_ref(q0, q1, o0, o1, k0, k1, v0, v1)
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)

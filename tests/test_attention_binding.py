@@ -29,3 +29,16 @@ def test_a_page_table_expanded_over_sequences_is_refused():
     # rows with something between them, and a lone row whatever its stride says
     assert _cache(_i32(3, 9)[:, 2:6]).c.table_stride == 9
     assert _cache(_i32(1, 4).expand(1, 4), n_seq=1).c.table_stride == 4
+
+
+@pytest.mark.parametrize("workspace", [torch.zeros(4096, dtype=torch.uint8), _device(16, dtype=torch.uint8).expand(4096, 16), _device(8192, dtype=torch.uint8)[::2]],
+                         ids=["host", "expanded", "strided"])
+def test_a_workspace_that_is_not_one_piece_of_device_memory_is_refused(workspace):
+    """Its number of bytes says where the library may write, from its first one on."""
+    cu = _i32(2)
+    q, k = _device(2, 8, 128), _device(2, 2, 128)
+    out, lse = _device(2, 8, 128), _device(2, 8, dtype=torch.float32)
+    with pytest.raises(ValueError, match="workspace"):
+        il.ilre_prompt_attention(q, k, k, cu, max_q=2, workspace=workspace, out=out, lse=lse)
+    with pytest.raises(ValueError, match="workspace"):
+        il.ilre_paged_attention(q, _cache(_i32(1, 4), n_seq=1), max_q=2, max_kv=64, workspace=workspace, out=out, lse=lse)
