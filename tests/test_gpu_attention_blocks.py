@@ -89,3 +89,33 @@ def test_packed_prompts_with_a_window(lens, Hq, Hkv, dtype, sink, window):
     out, lse = x.attend(sink=sink, window=window, workspace=ws)
     torch.cuda.synchronize()
     x.check(out, lse, sink=sink, window=window)
+
+
+def test_a_stream_that_lies_evenly_over_the_tiles_takes_no_longer():
+    """Where the window begins with a tile, a wavefront whose half of the sink tile holds nothing has seen nothing before the first whole tile: its rows take their
+    references from there.  (Weights against no reference send the workgroup through its tiles a second time, 1.6 times as long.)"""
+    _announce("stream, 9216 and 9220 tokens")
+    calls = []
+    for kv in (9216, 9220):
+        x = Paged([1024], [kv], 16, 4, 64, "bf16", seed=kv)
+        cache, ws = x.cache(), _workspace_of(x, 16, 4)
+        out, lse = x.attend(sink=4, window=512)
+        rows = torch.tensor(sorted({0, 1, 31, 32, 63, 64, 65, 500, 991, 992, 1023}))
+        for i in rows.tolist():  # a row alone, at the end of what it may see
+            n = kv - 1024 + i + 1
+            want = oa.attend(_f64(x.q[i:i + 1]), _f64(x.k[0][:n]), _f64(x.v[0][:n]), sink=4, window=512)
+            _check(out[i:i + 1], lse[i:i + 1], *want, 516, "bf16", f"row {i} of {kv}")
+        calls.append(lambda x=x, cache=cache, ws=ws, out=out, lse=lse: il.ilre_paged_attention(x.dev["q"], cache, max_q=1024, max_kv=max(x.kv_lens), sink=4, window=512,
+                                                                                             workspace=ws, out=out, lse=lse))
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    best = [float("inf"), float("inf")]
+    for _ in range(15):
+        for i, call in enumerate(calls):
+            call()
+            begin.record()
+            for _ in range(40):
+                call()
+            end.record()
+            end.synchronize()
+            best[i] = min(best[i], begin.elapsed_time(end))
+    assert best[0] < 1.25 * best[1], best
