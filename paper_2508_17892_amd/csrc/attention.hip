@@ -138,10 +138,10 @@ struct Source {
     int64_t page, token;  // bytes
 };
 
-// A page's number, clamped to the table; -1 where the entry names no page (its tokens count as absent).
+// The number of a token's page (blk.hi > 0); -1 where the entry names no page (its tokens count as absent).
 __device__ __forceinline__ int page_of(const AttnArgs &a, const Block &b, int tok)
 {
-    const int id = read_i32(a.table + (int64_t)b.seq * a.table_stride + page_column(tok, a.page_shift, a.table_width));
+    const int id = read_i32(a.table + (int64_t)b.seq * a.table_stride + page_column(b, tok, a.page_shift, a.table_width));
     return (unsigned)id < (unsigned)a.num_pages ? id : -1;
 }
 
@@ -761,8 +761,8 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         Pages p{};
         if (PAGED) {
             const int t = token_of(i);
-            p.id[0] = page_of(a, blk, min(t, blk.hi - 1));
-            p.id[1] = page_of(a, blk, min(t + 16, blk.hi - 1));
+            p.id[0] = page_of(a, blk, t);
+            p.id[1] = page_of(a, blk, t + 16);
         }
         return p;
     };

@@ -91,6 +91,12 @@ __host__ __device__ __forceinline__ int page_column(int t, int page_shift, int t
     return at < table_width ? at : table_width - 1;
 }
 
+// The same for a workgroup: tokens behind the last one that its rows see are looked up as that one, so that entries past a sequence's length are not read.
+__host__ __device__ __forceinline__ int page_column(const Block &b, int t, int page_shift, int table_width)
+{
+    return page_column(t < b.hi ? t : b.hi - 1, page_shift, table_width);
+}
+
 // Whether a row at position p sees token t.
 __host__ __device__ __forceinline__ bool row_sees(const Mask &m, int64_t p, int kv, int t)
 {

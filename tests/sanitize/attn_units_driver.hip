@@ -1,5 +1,6 @@
 // Host driver for the numbering of the attention kernels' units (test infrastructure, no kernel and no GPU call): calls of several sequences, cut up as the library
-// cuts them; every number of the grid is taken as a workgroup takes it, and every range that the merge adds up has to have been taken, once.
+// cuts them; every number of the grid is taken as a workgroup takes it, and every range that the merge adds up has to have been taken, once.  And no lookup of a page reads
+// an entry past its sequence's length.
 //
 // With arguments "plan" it reads calls from stdin, a line each (dtype T n_seq Hq Hkv max_q max_kv total_kv sink window), and prints the rows of a workgroup and
 // the number of ranges.
@@ -69,6 +70,13 @@ static int faults(const Call &c, const AttnPlan &p)
             b.rows0 = i * p.rows;
             tiles_of(b, c.m, G, p.rows, p.tile);
             const int ranges = ranges_of(b.nt, p.split_tiles, p.nsplit);
+            // whatever token of its tiles, or behind them, a workgroup looks up: the entry is one of the sequence's
+            const int shift = 4 + i % 3, width = ((b.kv + 9000) >> shift) + 1;
+            for (int k = 0; k < b.nt; k += 1 + b.nt / 4)
+                for (int t = tile_token(b, b.nt - 1 - k, p.tile), e = t + p.tile + 64; t < e; t += 16) {
+                    const int at = page_column(b, t, shift, width);
+                    if (at < 0 || at > (b.kv - 1) >> shift || (t < b.hi && at != t >> shift)) ++bad;
+                }
             for (int k = 0; k < p.nsplit; ++k)
                 if (taken[s][(size_t)i * p.nsplit + k] != (k < ranges)) ++bad;
         }
