@@ -119,3 +119,98 @@ def test_a_stream_that_lies_evenly_over_the_tiles_takes_no_longer():
             end.synchronize()
             best[i] = min(best[i], begin.elapsed_time(end))
     assert best[0] < 1.25 * best[1], best
+
+
+# Calls whose blocks have 256 rows: lists of more than 24 tiles, or blocks enough for every compute unit; and the other kernels where they are cut into ranges.
+PROMPTS = [
+    # q_lens, Hq, Hkv, dtype, mask
+    ([1700], 2, 1, "bf16", {}),
+    ([1600, 5, 1801, 257], 4, 2, "bf16", {}),
+    ([1601, 300], 7, 1, "bf16", {}),
+    ([1921], 3, 3, "bf16", {}),
+    ([1600, 1], 8, 1, "bf16", dict(causal=False)),
+    ([2300, 333], 4, 4, "bf16", dict(sink=4, window=1500)),
+    ([1800, 1], 4, 1, "bf16", dict(sink=70, window=1472)),
+    ([1024, 33], 64, 8, "bf16", dict(sink=4, window=100)),
+    ([1100], 5, 1, "f32", {}),
+    ([9], 5, 1, "f32", {}),
+    ([9, 1, 20], 3, 1, "bf16", {}),
+    ([5, 1, 8], 4, 1, "f32", {}),
+]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,dtype,mask", PROMPTS, ids=[f"{c[3]}-{c[1]}.{c[2]}-{sum(c[0])}-" + ("".join(f"{k}{v}" for k, v in c[4].items()) or "causal") for c in PROMPTS])
+def test_prompts_in_every_kind_of_block(lens, Hq, Hkv, dtype, mask):
+    _announce(f"prompts {lens} {Hq}/{Hkv} {dtype} {mask}")
+    x = Packed(lens, Hq, Hkv, dtype, sum(lens) + Hq)
+    ws = x.workspace()
+    ws.fill_(255)
+    out, lse = x.attend(workspace=ws, **mask)
+    torch.cuda.synchronize()
+    x.check(out, lse, **mask)
+    again, lse2 = x.attend(workspace=ws, **mask)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_long_prompts_beside_neighbours_that_may_hold_anything():
+    _announce("prompts of 1700 tokens, NaN in the other sequences")
+    for lens, mine in (([100, 1700, 67], (100, 1800)), ([1700, 1650], (1700, 3350))):
+        x = Packed(lens, 4, 1, "bf16", sum(lens))
+        q, kv, cu = x.dev
+        for a, b in ((0, mine[0]), (mine[1], sum(lens))):
+            kv[a:b, :1] = float("nan")
+            kv[a:b, 2:] = float("inf")
+        out, lse = x.attend()
+        s = slice(*mine)
+        _check(out[s], lse[s], *oa.attend(_f64(x.q[s]), _f64(x.kv[s, :1]), _f64(x.kv[s, 2:])), mine[1] - mine[0], "bf16")
+
+
+@pytest.mark.parametrize("lens", [[1700, 129], [700]])
+def test_prompts_whose_late_tokens_outweigh_everything_before(lens):
+    """Logits that rise, or fall, by hundreds of units along a prompt."""
+    _announce(f"prompts, rising logits, {lens}")
+    for sign in (1, -1):
+        x = Packed(lens, 4, 2, "bf16", 7)
+        step = torch.cat([torch.linspace(-1, 1, n) for n in lens])[:, None, None] * sign * 40
+        x.q = (x.q.float() * 0.1 + 1).bfloat16()
+        x.kv[:, :2] = (x.kv[:, :2].float() * 0.1 + step).bfloat16()
+        x.dev = x.q.cuda(), x.kv.cuda(), x.dev[2]
+        x.check(*x.attend())
+
+
+# The same over pages.
+CHUNKS = [
+    # q_lens, kv_lens, Hq, Hkv, page, layout, dtype, mask
+    ([300], [2000], 2, 1, 16, "head", "bf16", {}),
+    ([257, 90, 1], [1700, 2100, 5], 8, 2, 32, "token", "bf16", {}),
+    ([150], [1601], 14, 2, 64, "head", "bf16", {}),
+    ([200, 64], [1800, 64], 8, 1, 16, "head", "bf16", dict(causal=False)),
+    ([400, 131], [2600, 1900], 4, 4, 16, "head", "bf16", dict(sink=4, window=1600)),
+    ([600], [2304], 4, 1, 64, "token", "bf16", dict(sink=4, window=1472)),
+    ([1024, 40], [1500, 700], 64, 8, 64, "head", "bf16", dict(sink=4, window=100)),
+    ([1, 1], [2000, 9], 4, 1, 16, "head", "f32", {}),
+    ([60], [700], 5, 1, 16, "token", "f32", {}),
+    ([9], [40], 5, 1, 16, "head", "f32", {}),
+]
+
+
+@pytest.mark.parametrize("q_lens,kv_lens,Hq,Hkv,page,layout,dtype,mask", CHUNKS,
+                         ids=[f"{c[6]}-q{sum(c[0])}-kv{sum(c[1])}-{c[2]}.{c[3]}-" + ("".join(f"{k}{v}" for k, v in c[7].items()) or "causal") for c in CHUNKS])
+def test_chunks_in_every_kind_of_block(q_lens, kv_lens, Hq, Hkv, page, layout, dtype, mask):
+    _announce(f"chunks {q_lens} of {kv_lens} {Hq}/{Hkv} page {page} {layout} {dtype} {mask}")
+    x = Paged(q_lens, kv_lens, Hq, Hkv, page, dtype, layout, seed=sum(kv_lens) + Hq)
+    ws = _workspace_of(x, Hq, Hkv)
+    ws.fill_(255)
+    out, lse = x.attend(workspace=ws, **mask)
+    torch.cuda.synchronize()
+    x.check(out, lse, **mask)
+    # pages that are not there: the first one, some in between, the last one
+    absent = []
+    for s, n in enumerate(kv_lens):
+        gone = np.zeros(n, bool)
+        for col in {0, 3, n // page // 2, (n - 1) // page}:
+            x.dev["table"][s, min(col, x.table.shape[1] - 1)] = (-1, 1 << 30, x.kp.shape[0])[col % 3]
+            gone[col * page:col * page + page] = True
+        absent.append(gone)
+    out, lse = x.attend(workspace=ws, **mask)
+    x.check(out, lse, absent=absent, **mask)
