@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
     if (WPT > 1) fetch(first);  // on their way while the token's place and angles are worked out
 
     // the token's place in its sequence, and where that is in the cache
-    int place = a.first_position + token;
+    double place = (double)a.first_position + token;  // (their sum may not fit 32 bits)
     int64_t cell = -1;
     if (a.cu_q) {
         int seq = -1;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
         const int q0 = max(a.cu_q[seq], 0), q1 = min(a.cu_q[seq + 1], a.T);
         if (token < q0) return;
         const int64_t at = (int64_t)a.kv_len[seq] - (q1 - q0) + (token - q0);
-        place = (int)at;
+        place = (double)at;
         if (at >= 0 && at < a.kv_limit) {
             const int page = a.table[seq * a.table_stride + (at >> a.page_shift)];
             if ((unsigned)page < (unsigned)a.num_pages) cell = page * a.page_bytes + (at & (((int64_t)1 << a.page_shift) - 1)) * a.token_bytes;
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
     float co[E], si[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const double n = (double)place * a.turns[turn ? u * E + e : 0];
+        const double n = place * a.turns[turn ? u * E + e : 0];
         sincospif(2.0f * (float)(n - rint(n)), &si[e], &co[e]);
         si[e] *= a.magnitude;
         co[e] *= a.magnitude;

@@ -62,3 +62,14 @@ def test_append_of_many_tokens(dtype, layout, pairing, given):
     k0[page, :, cell] = x.kp[page, :, cell]
     v0[page, :, cell] = x.vp[page, :, cell]
     assert torch.equal(k0, x.kp) and torch.equal(v0, x.vp)
+
+
+def test_positions_past_32_bits():
+    """first_position + i is the token's position whatever they add up to."""
+    _announce("rope, positions around 2^31")
+    f = il.ilre_rope_frequencies(128, 500000.0)
+    g = torch.Generator().manual_seed(3)
+    for T in (9, 4100):
+        x = torch.randn(T, 2, 128, generator=g)
+        for first in (2 ** 31 - 4, -2 ** 31):
+            _rope_check(il.ilre_rope(x.cuda(), f, first_position=first), x, first + np.arange(T), f, "half", "f32", 128)
