@@ -7,7 +7,8 @@
 // half-split pairing, chunks 2u and 2u + 1 of the interleaved one; the channels behind `rotary` are units that are copied.
 //
 // The angle is reduced in turns in fp64 (position * inv_freq / 2 pi reaches 10^5 turns at a million positions, and its fraction is all that counts), then
-// sine and cosine of the fraction are fp32: their argument is off by 2^-25 of half a turn at most.
+// sine and cosine of the fraction are fp32: of its upper 24 bits, and the rest of it, 2^-26 of a turn at most, by the first term of the addition theorem, so that small sines
+// and cosines keep their bits too.
 #include "ilre_internal.h"
 
 namespace ilre {
@@ -124,9 +125,12 @@ __global__ __launch_bounds__(kThreads) void turn_kernel(const TurnArgs a)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const double n = place * a.turns[turn ? u * E + e : 0];
-        sincospif(2.0f * (float)(n - rint(n)), &si[e], &co[e]);
-        si[e] *= a.magnitude;
-        co[e] *= a.magnitude;
+        const double part = n - rint(n);
+        const float upper = (float)part, lower = (float)(part - upper) * 6.283185307f;
+        float s, c;
+        sincospif(2.0f * upper, &s, &c);
+        si[e] = fmaf(c, lower, s) * a.magnitude;
+        co[e] = fmaf(-s, lower, c) * a.magnitude;
     }
     auto turned_unit = [&](uint4 &x, uint4 &y) {
         float f[E], g[E];

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import paper_2508_17892_amd as il
-from test_gpu_attention import DT, Paged, _announce, _rope_check
+from oracle import attention as oa
+from test_gpu_attention import DT, Paged, _announce, _f64, _rope_check
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +74,28 @@ def test_positions_past_32_bits():
         x = torch.randn(T, 2, 128, generator=g)
         for first in (2 ** 31 - 4, -2 ** 31):
             _rope_check(il.ilre_rope(x.cuda(), f, first_position=first), x, first + np.arange(T), f, "half", "f32", 128)
+
+
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+def test_sines_and_cosines_keep_the_bits_of_fp32_where_they_are_small(pairing):
+    """One channel of every pair is zero, so that a result is one product, m x cos a or m x sin a, whose error is taken relative to itself.  Angles in fp64 reach
+    10^6 positions with less than 2^-33 of a turn lost; sincospi of the fraction's upper part is off by 2 units in the last place (2^-22), what is added for the lower part, the
+    magnitude and its rounding, the product and its rounding by 2^-24 each: 9 * 2^-24, with the last rounding 10.  (An angle rounded to fp32 is off by 2^-26 of a
+    turn, 1.6 * 2^-24 by itself: more than that share of every cosine below a sixth.)"""
+    _announce(f"rope, small sines and cosines, {pairing}")
+    for T in (600, 4100):
+        f = il.ilre_rope_frequencies(128, 500000.0, scaling=il.ILRE_ROPE_PARTS, factor=8.0, low=1.0, high=32.0, original_len=4096)
+        g = torch.Generator().manual_seed(T)
+        x = torch.randn(T, 2, 128, generator=g)
+        if pairing == "half":
+            x[:, 0, :64] = 0
+            x[:, 1, 64:] = 0
+        else:
+            x[:, 0, 0::2] = 0
+            x[:, 1, 1::2] = 0
+        pos = torch.randint(0, 1000000, (T,), generator=g).int()
+        got = _f64(il.ilre_rope(x.cuda(), f, pos.cuda(), pairing=CODE[pairing]))
+        want = oa.rope(_f64(x), pos.numpy(), np.array(f.inv_freq), f.magnitude, pairing)
+        lost = 2.0 ** -33 * 2 * np.pi * np.abs(_f64(x)).max(-1, keepdims=True) * f.magnitude
+        err = np.abs(got - want) / (10 * 2.0 ** -24 * np.abs(want) + lost)
+        assert (err <= 1).all(), (float(err.max()), np.argwhere(err > 1)[:3].tolist())
