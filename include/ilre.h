@@ -305,7 +305,8 @@ int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t
 /* Attention of the new tokens of n_seq sequences over a paged cache that holds them already: one token each, a chunk of a prompt, or any mixture.
    out[i,h,:] = sum_t softmax_t(q[i,h,:] . K[g(h),t,:] * scale) V[g(h),t,:] over the tokens that ilre_attn lets row i see; consecutive query heads share a kv
    head as in Eq. 4.  Rows that see nothing give zeros and lse = -inf.  Logits, softmax and sums are fp32, weights are rounded to opts->dtype for the
-   product with V.  Values and keys that some row of the call sees have to be finite; what no row sees may hold anything.
+   product with V (their sum is taken before that).  Values and keys that some row of the call sees have to be finite, and its logits below 2^30 in magnitude: fp32
+   holds a logit and its row's reference to 2^-24 of themselves, and beyond that the exponential of what is left overflows.  What no row sees may hold anything.
    q, out     dev  [T, Hq, d] (strides->q_*, out_*); out must not overlap q
    lse        dev  [T, Hq] float, the natural logarithm of each row's sum of exponentials; may be NULL
    Tokens of no sequence (past cu_q[n_seq], before cu_q[0]) are left as they are. */
