@@ -12,8 +12,8 @@
 // which place of the contraction is free as long as both operands agree, and V^T is read from LDS with the transposing
 // read (four tokens of one channel a lane) in that very order.  P never goes through LDS.
 //
-// Weights are taken relative to a reference m per row.  attend_rows takes it from the first tokens that all of a workgroup's rows see and then
-// keeps it: any m gives the same quotient as long as the exponentials stay in range, and the maximum, the rescaling and the branch in
+// Weights are taken relative to a reference m per row.  attend_rows takes it from the tiles before those that all of a workgroup's rows see whole, or from the
+// first 32 tokens of these, and then keeps it: any m gives the same quotient as long as the exponentials stay in range, and the maximum, the rescaling and the branch in
 // front of it are a fifth of the vector work.  A row whose later logits exceed its reference by more than 2^60 shows in its
 // sum, and the workgroup walks its tiles again, following the maximum all the way.
 //
@@ -87,7 +87,8 @@ __device__ __forceinline__ void sequence_of(const AttnArgs &a, int seq, Block &b
 }
 
 // Unit w of the call.  The units of all sequences come one after the other; what is left of the grid has none and ends at once, behind all that work (between
-// them, 48 requests with contexts of 1 to 16384 tokens, it cost 10 of 85 us).  False where there is none.
+// them, 48 requests with contexts of 1 to 16384 tokens, it cost 10 of 85 us).  64 sequences a step: 256 requests of 512 tokens 47 us (5.7 TB/s), 1024 210 us (5.1),
+// 4096 1.6 ms (2.7).  False where there is none.
 template <bool PAGED>
 __device__ __forceinline__ bool find_unit(const AttnArgs &a, int w, int rows, int tile, Block &b, int &split)
 {
@@ -225,7 +226,8 @@ struct Elem<ILRE_BF16> {
 #pragma unroll
         for (int st = 0; st < 8; ++st) mma(s, lds_read16(ad.k[st] + kat), q[st]);
     }
-    // The weights are rounded to bf16 for the product with V, like V itself; their sum is taken before.
+    // The weights are rounded to bf16 for the product with V, as the matrix instruction has one type for both operands; their sum is taken before.  Of the 2-norm that is 0.6e-3 to
+    // 1.3e-3, beside 1.7e-3 from rounding the result; weights in two parts, upper and lower, would be half as many matrix instructions again.
     static __device__ __forceinline__ void pack(Weights &w, const float (&p)[16])
     {
         unsigned u[8];
