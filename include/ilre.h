@@ -248,6 +248,36 @@ typedef struct {
     int32_t n_seq;
 } ilre_paged_kv;
 
+/* A cache of pages held in 8 or 4 bits.  Every token and kv head has d codes and d / ILRE_KV_BLOCK scales, a byte for each ILRE_KV_BLOCK consecutive channels; byte b stands
+   for 2^(b - 127), 1 <= b <= 254, and a channel for its code's value times its block's scale.
+   ILRE_KV_FP8  a byte a channel: sign, 4 exponent bits (bias 7), 3 fraction bits, largest 448
+   ILRE_KV_FP4  half a byte: sign, 2 exponent bits (bias 1), 1 fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6); channel 2i is the lower half of byte i
+   Where the library writes one, the scale is the smallest power of two (2^-126 at least) with which the block's largest magnitude is no larger than the largest code's, so
+   that nothing is cut off, and codes are rounded to nearest, ties to even, from values that have not been rounded before: keys in fp64 after norm and rotation, values as they
+   come.  What a cache holds is thereby a function of the states alone.  A block with an infinity or a NaN gets byte 255, which stands for NaN, and codes of zero.
+   The description is an ilre_paged_kv with more behind it: its struct_size says sizeof(ilre_quant_kv), k_pages and v_pages are the codes, strides count channels and are multiples
+   of 128 (a lone channel's address is pages + offset * bits / 8, its scale's k_scales + offset / ILRE_KV_BLOCK: the scales have the layout of the codes).  Every call that takes
+   an ilre_paged_kv takes &quant->kv; opts->dtype is then the element type of the states alone. */
+#define ILRE_KV_BLOCK 32
+typedef enum { ILRE_KV_FP8 = 1, ILRE_KV_FP4 = 2 } ilre_kv_format;
+
+typedef struct {
+    ilre_paged_kv kv;              /* kv.struct_size = sizeof(ilre_quant_kv) */
+    int32_t format;                /* ilre_kv_format */
+    int32_t reserved;              /* 0 */
+    uint8_t *k_scales, *v_scales;  /* dev, 4-byte aligned */
+} ilre_quant_kv;
+
+/* Norms of queries and keys, each head by itself, before the rotation: y = x / sqrt(mean(x^2) + eps) * (weight + offset).  Sums are fp32 (fp64 for keys of a quantised cache), the
+   result is not rounded before it is turned.  (offset 1: weights that are kept as differences from one.) */
+typedef struct {
+    int32_t struct_size;      /* sizeof(ilre_head_norms) */
+    int32_t q_norm, k_norm;   /* 1: normed, 0: as they are */
+    float offset;
+    double eps;               /* >= 0 */
+    const void *q_weight, *k_weight; /* dev, d elements of opts->dtype, 16-byte aligned; NULL: weight + offset is one */
+} ilre_head_norms;
+
 /* Which tokens a row sees.  New token i of a sequence stands at p = kv_len - q_len + i and sees the tokens t < kv_len with t <= p (causal) and,
    where window > 0, with t > p - window or t < sink (the sink part and sliding window of streaming chunked prefill). */
 typedef struct {
@@ -297,6 +327,29 @@ int ilre_rope(const void *x, void *out, int32_t T, int32_t H, int32_t d, const i
 int ilre_rope_append(const void *q, void *q_out, const void *k, const void *v, int32_t T, int32_t Hq, int32_t d, const int32_t *positions,
                      const ilre_rope_freqs *freqs, int32_t pairing, const ilre_paged_kv *cache, const ilre_strides *strides, const ilre_opts *opts);
 
+/* ilre_rope_append with norms, and with positions along several axes (time, height and width of images and video).
+   positions  dev  [n_axes, T] int32; pair j turns by positions[axes[j]][token] * inv_freq[j].  NULL with one axis: the tokens' places in the cache
+   axes       host rotary / 2 bytes below n_axes (1 .. ILRE_MAX_AXES); NULL: all zero
+   freqs      NULL: nothing is turned (positions and axes are then not read)
+   norms      NULL: nothing is normed */
+#define ILRE_MAX_AXES 8
+int ilre_norm_rope_append(const void *q, void *q_out, const void *k, const void *v, int32_t T, int32_t Hq, int32_t d, const int32_t *positions, int32_t n_axes,
+                          const uint8_t *axes, const ilre_rope_freqs *freqs, int32_t pairing, const ilre_head_norms *norms, const ilre_paged_kv *cache,
+                          const ilre_strides *strides, const ilre_opts *opts);
+
+/* ilre_rope with norms (norms->q_*) and axes, as above.  positions NULL with one axis: first_position + i. */
+int ilre_norm_rope(const void *x, void *out, int32_t T, int32_t H, int32_t d, const int32_t *positions, int32_t n_axes, const uint8_t *axes, int32_t first_position,
+                   const ilre_rope_freqs *freqs, int32_t pairing, const ilre_head_norms *norms, const ilre_strides *strides, const ilre_opts *opts);
+
+/* Keys and values out of a paged cache, quantised or not: all of a context as the recall's key cache (k_out = k_cache, k_token = d, k_head = L * d), the tokens that a recall
+   kept, or what a call has just stored.  Row i of the T rows belongs to the sequence s with cache->cu_q[s] <= i < cache->cu_q[s+1].  Rounded to opts->dtype (nearest even; codes
+   times scales are exact in it down to 2^-133).
+   k_out, v_out  dev [T, Hkv, d] (strides->k_*, v_*); either may be NULL
+   tokens        dev T int32, the token of each row, or NULL: a sequence's rows are its last tokens (row i is token kv_len - rows + i)
+   A row whose token is not in [0, kv_len), or on no page, is zeros; rows of no sequence (past cu_q[n_seq], before cu_q[0]) are left as they are. */
+int ilre_cache_read(void *k_out, void *v_out, int32_t T, int32_t d, const int32_t *tokens, const ilre_paged_kv *cache, const ilre_strides *strides,
+                    const ilre_opts *opts);
+
 /* Bytes of workspace the two attention calls can make use of (host computation only): partial results of sequences that are cut into several ranges of
    tokens.  With less the calls cut less; without any they run all the same, slowly where few rows meet a long cache.  out_bytes: host. */
 int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_q, int32_t max_kv,
@@ -312,6 +365,15 @@ int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t
    Tokens of no sequence (past cu_q[n_seq], before cu_q[0]) are left as they are. */
 int ilre_paged_attention(const void *q, void *out, float *lse, int32_t T, int32_t Hq, int32_t d, const ilre_attn *attn,
                          const ilre_paged_kv *cache, const ilre_strides *strides, const ilre_opts *opts);
+
+/* Attention of a tree of drafted tokens: the new tokens of a sequence, stored at its end, see all of the context before them (t < kv_len - q_len) and, of the
+   new tokens, those that their mask says: token i sees new token j of its sequence where bit j % 32 of word tree[i * tree_stride + j / 32] is set (its ancestors
+   and itself, or any other set; positions are what the tokens were turned to, not their order).  Bits at and past q_len are not looked at.
+   tree        dev T rows of tree_words words, tree_words * 32 >= attn->max_q
+   tree_stride words between rows; 0 = tree_words
+   New tokens of a sequence with more than tree_words * 32 of them see none beyond those.  attn->causal, sink and window must be 0; all else as ilre_paged_attention. */
+int ilre_tree_attention(const void *q, void *out, float *lse, int32_t T, int32_t Hq, int32_t d, const uint32_t *tree, int32_t tree_words, int64_t tree_stride,
+                        const ilre_attn *attn, const ilre_paged_kv *cache, const ilre_strides *strides, const ilre_opts *opts);
 
 /* The same over whole packed prompts: k, v dev [Tk, Hkv, d] (strides->k_*, v_*), the tokens of sequence s being cu_k[s] .. cu_k[s+1] - 1.
    cu_q, cu_k dev n_seq + 1 int32 each, ascending; cu_k NULL: cu_q (then Tk = T). */

@@ -23,6 +23,9 @@ ILRE_FLAG_EXACT_ROW_MAX = 1
 ILRE_ROPE_HALF, ILRE_ROPE_INTERLEAVED = 0, 1
 ILRE_ROPE_PLAIN, ILRE_ROPE_LINEAR, ILRE_ROPE_BANDS, ILRE_ROPE_PARTS = range(4)
 ILRE_MIN_PAGE_TOKENS, ILRE_MAX_PAGE_TOKENS = 16, 32768
+ILRE_KV_FP8, ILRE_KV_FP4 = 1, 2
+ILRE_KV_BLOCK = 32
+ILRE_MAX_AXES = 8
 ILRE_MAX_BUDGET = 8192
 ILRE_MAX_POOL_KERNEL = 2047
 ILRE_MAX_POOL_KERNELS = 64
@@ -34,7 +37,7 @@ ILRE_STATIC_SCRATCH_BYTES = 4 << 20
 EXPORTS = ("ilre_workspace_bytes", "ilre_recall", "ilre_row_stats", "ilre_row_stats_static", "ilre_col_scores", "ilre_select",
            "ilre_select_max_avg", "ilre_recall_max_avg", "ilre_workspace_bytes_max_avg", "ilre_rerope_keys",
            "ilre_gather_ids", "ilre_rope_frequencies", "ilre_rope", "ilre_rope_append", "ilre_attention_workspace_bytes",
-           "ilre_paged_attention", "ilre_prompt_attention", "ilre_probe_mfma_ceiling", "ilre_probe_describe", "ilre_last_error")
+           "ilre_paged_attention", "ilre_prompt_attention", "ilre_norm_rope", "ilre_norm_rope_append", "ilre_cache_read", "ilre_tree_attention", "ilre_probe_mfma_ceiling", "ilre_probe_describe", "ilre_last_error")
 
 
 class IlreOpts(ctypes.Structure):
@@ -78,6 +81,28 @@ class IlrePagedKv(ctypes.Structure):
         ("cu_q", ctypes.c_void_p),
         ("table_width", ctypes.c_int32),
         ("n_seq", ctypes.c_int32),
+    ]
+
+
+class IlreQuantKv(ctypes.Structure):
+    _fields_ = [
+        ("kv", IlrePagedKv),
+        ("format", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("k_scales", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
+    ]
+
+
+class IlreHeadNorms(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_int32),
+        ("q_norm", ctypes.c_int32),
+        ("k_norm", ctypes.c_int32),
+        ("offset", ctypes.c_float),
+        ("eps", ctypes.c_double),
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
     ]
 
 
@@ -160,6 +185,15 @@ def load() -> ctypes.CDLL:
         lib.ilre_paged_attention.argtypes = [vp, vp, vp, i32, i32, i32, pa, pc, ps, po]
         lib.ilre_prompt_attention.restype = ctypes.c_int
         lib.ilre_prompt_attention.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, i32, pa, ps, po]
+        pn = ctypes.POINTER(IlreHeadNorms)
+        lib.ilre_norm_rope.restype = ctypes.c_int
+        lib.ilre_norm_rope.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, i32, pf, i32, pn, ps, po]
+        lib.ilre_norm_rope_append.restype = ctypes.c_int
+        lib.ilre_norm_rope_append.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, i32, vp, pf, i32, pn, pc, ps, po]
+        lib.ilre_cache_read.restype = ctypes.c_int
+        lib.ilre_cache_read.argtypes = [vp, vp, i32, i32, vp, pc, ps, po]
+        lib.ilre_tree_attention.restype = ctypes.c_int
+        lib.ilre_tree_attention.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, i64, pa, pc, ps, po]
         lib.ilre_probe_mfma_ceiling.restype = ctypes.c_int
         lib.ilre_probe_mfma_ceiling.argtypes = [i32, i32, vp, vp, ctypes.POINTER(ctypes.c_double), po]
         lib.ilre_probe_describe.restype = ctypes.c_char_p
@@ -507,25 +541,32 @@ class PagedKV:
         if v_pages is not None and (v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype
                                     or not v_pages.is_cuda):
             raise ValueError("v_pages must have the shape, strides and element type of k_pages")
+        if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
+            raise ValueError("pages expanded over a dimension are not supported")
+        self.dtype = _dtype_code(k_pages)
+        c = IlrePagedKv()
+        c.struct_size = ctypes.sizeof(IlrePagedKv)
+        self._describe(c, k_pages, v_pages, page_table, kv_len, cu_q, 1)
+
+    def _describe(self, c: IlrePagedKv, k_pages, v_pages, page_table, kv_len, cu_q, per: int) -> None:
+        """Fill in c; an element of the pages holds `per` channels."""
         if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_cuda or page_table.stride(1) != 1:
             raise ValueError("page_table is an int32 device tensor [n_seq, pages] with contiguous rows")
         n_seq = page_table.shape[0]
         if n_seq > 1 and page_table.stride(0) == 0:  # (0 stands for contiguous in the C ABI)
             raise ValueError("a page_table expanded over sequences is not supported")
         num_pages, Hkv, P, d = k_pages.shape
-        if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
-            raise ValueError("pages expanded over a dimension are not supported")
+        d *= per
         if d != 128:
             raise IlreError(ILRE_EUNSUPPORTED, f"head_dim {d} unsupported (only 128)")
         self.k_pages, self.v_pages, self.page_table, self.kv_len, self.cu_q = k_pages, v_pages, page_table, kv_len, cu_q
-        self.dtype, self.n_seq, self.Hkv = _dtype_code(k_pages), n_seq, Hkv
-        c = self.c = IlrePagedKv()
-        c.struct_size = ctypes.sizeof(IlrePagedKv)
+        self.n_seq, self.Hkv = n_seq, Hkv
+        self.c = c
         c.page_tokens, c.num_pages, c.Hkv = P, num_pages, Hkv
         # the strides of a lone page or head say nothing
-        c.stride_token = k_pages.stride(2)
-        c.stride_head = k_pages.stride(1) if Hkv > 1 else d
-        c.stride_page = k_pages.stride(0) if num_pages > 1 else d
+        c.stride_token = k_pages.stride(2) * per
+        c.stride_head = k_pages.stride(1) * per if Hkv > 1 else d
+        c.stride_page = k_pages.stride(0) * per if num_pages > 1 else d
         c.k_pages, c.v_pages = k_pages.data_ptr(), 0 if v_pages is None else v_pages.data_ptr()
         c.page_table, c.table_width, c.n_seq = page_table.data_ptr(), page_table.shape[1], n_seq
         c.table_stride = page_table.stride(0) if n_seq > 1 else page_table.shape[1]
@@ -533,14 +574,112 @@ class PagedKV:
         self._ref = ctypes.byref(c)
 
 
+class QuantKV(PagedKV):
+    """A cache of pages held in 8 or 4 bits with a scale for every 32 channels, described once and kept like a PagedKV; every call that takes a PagedKV takes one.
+
+    k_pages, v_pages: codes, float8_e4m3fn [num_pages, Hkv, page_tokens, 128] (8 bits) or uint8 [num_pages, Hkv, page_tokens, 64] (4 bits, channel 2i in the lower half
+    of byte i), in any layout of pages, heads and tokens; k_scales, v_scales: uint8 [num_pages, Hkv, page_tokens, 4] in the same layout (a byte b stands for 2^(b - 127));
+    v_pages and v_scales None: keys only."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], k_scales: torch.Tensor, v_scales: Optional[torch.Tensor], page_table: torch.Tensor,
+                 kv_len: torch.Tensor, cu_q: torch.Tensor):
+        if k_pages.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise TypeError(f"unsupported element type {k_pages.dtype}: codes are float8_e4m3fn or (4 bits) uint8")
+        fp8 = k_pages.dtype == torch.float8_e4m3fn
+        if k_pages.dim() != 4 or not k_pages.is_cuda or k_pages.stride(3) != 1 or k_scales.dim() != 4 or k_scales.stride(3) != 1:
+            raise ValueError("k_pages and k_scales are device tensors [num_pages, Hkv, page_tokens, .] with the last dimension contiguous")
+        if (v_pages is None) != (v_scales is None):
+            raise ValueError("v_pages and v_scales go together")
+        if v_pages is not None and (v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype
+                                    or not v_pages.is_cuda):
+            raise ValueError("v_pages must have the shape, strides and element type of k_pages")
+        per, scale = (1, 32) if fp8 else (2, 16)  # channels an element of the pages, elements a scale
+        for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+            if t is None:
+                continue
+            if t.dtype != torch.uint8 or not t.is_cuda or t.shape != (*k_pages.shape[:3], 4):
+                raise ValueError(f"{name} is a uint8 device tensor [num_pages, Hkv, page_tokens, 4]")
+            if t.stride(3) != 1 or any(n > 1 and a != b * scale for n, a, b in zip(k_pages.shape[:3], k_pages.stride(), t.stride())):
+                raise ValueError(f"{name} must have the layout of the codes (a {scale}th of their strides)")
+        if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
+            raise ValueError("pages expanded over a dimension are not supported")
+        self.dtype = None  # of the states: any
+        self.k_scales, self.v_scales = k_scales, v_scales
+        q = self.quant = IlreQuantKv()
+        q.format = ILRE_KV_FP8 if fp8 else ILRE_KV_FP4
+        q.k_scales, q.v_scales = k_scales.data_ptr(), 0 if v_scales is None else v_scales.data_ptr()
+        c = q.kv
+        c.struct_size = ctypes.sizeof(IlreQuantKv)
+        self._describe(c, k_pages, v_pages, page_table, kv_len, cu_q, per)
+
+
+class HeadNorms:
+    """Norms of queries and keys for each head, x / sqrt(mean(x^2) + eps) * (weight + offset), described once and kept.  q_weight, k_weight [128] in the states' element
+    type; None: that one is not normed."""
+
+    def __init__(self, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor] = None, *, eps: float = 1e-6, offset: float = 0.0):
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None and (not w.is_cuda or w.dim() != 1 or w.numel() != 128 or not w.is_contiguous()):
+                raise ValueError(f"{name} is a contiguous device vector of 128 entries")
+        if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+            raise TypeError("q_weight and k_weight must share an element type")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        w = q_weight if q_weight is not None else k_weight
+        self.dtype = None if w is None else _dtype_code(w)
+        self.c = IlreHeadNorms(ctypes.sizeof(IlreHeadNorms), 0 if q_weight is None else 1, 0 if k_weight is None else 1, float(offset), float(eps),
+                               None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+        self._ref = ctypes.byref(self.c)
+
+
+@functools.lru_cache(maxsize=256)
+def _axes_array(axes: Tuple[int, ...]):
+    if any(not 0 <= a < 256 for a in axes):
+        raise ValueError("axes are numbers of rows of positions")
+    return (ctypes.c_uint8 * len(axes))(*axes)
+
+
+def _turn_arguments(freqs: Optional[IlreRopeFreqs], positions: Optional[torch.Tensor], axes: Optional[Sequence[int]], T: int):
+    """(positions, number of axes, axes, frequencies) as the C ABI takes them: positions [T], or [number of axes, T] with `axes`, the axis that each pair turns by."""
+    if freqs is None:
+        return None, 1, None, None
+    if axes is None:
+        return None if positions is None else _int32_vector("positions", positions, T), 1, None, ctypes.byref(freqs)
+    if len(axes) != freqs.rotary // 2:
+        raise ValueError(f"axes has an entry for each of the {freqs.rotary // 2} pairs")
+    if positions is None or positions.dtype != torch.int32 or not positions.is_cuda or positions.dim() != 2 or positions.shape[1] != T or not positions.is_contiguous():
+        raise ValueError(f"positions is a contiguous int32 device tensor [axes, {T}]")
+    return positions.data_ptr(), positions.shape[0], _axes_array(tuple(axes)), ctypes.byref(freqs)
+
+
+def _same_device(*tensors: Optional[torch.Tensor]) -> None:
+    """The library works on the current device: a tensor of another one would be reached over the link, or not at all, on a stream that does not wait for it."""
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() not in (here, -1):
+            raise ValueError(f"a tensor on device {t.get_device()}, the current device is {here}")
+
+
 def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], cache: PagedKV, freqs: IlreRopeFreqs,
                      positions: Optional[torch.Tensor] = None, *, pairing: int = ILRE_ROPE_HALF, q_out: Optional[torch.Tensor] = None
                      ) -> Optional[torch.Tensor]:
     """Turn queries (returned, or in q_out, which may be q) and keys to their positions (default: their places in the cache) and store keys and values in
     the cache.  q [T, Hq, d], k and v [T, Hkv, d], any token and head strides; q None: keys and values only; v None: keys only."""
+    T, Hq, d, dt, q_out, st = _append_arguments(q, k, v, cache, q_out)
+    if T == 0:
+        return q_out
+    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    _check(load().ilre_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
+                                   None if v is None else v.data_ptr(), T, Hq, d,
+                                   None if positions is None else _int32_vector("positions", positions, T), ctypes.byref(freqs), int(pairing),
+                                   cache._ref, st, ctypes.byref(o)))
+    return q_out
+
+
+def _append_arguments(q, k, v, cache: PagedKV, q_out):
+    """(tokens, query heads, d, element type, q_out, strides) of a call that fills a cache."""
     T, _, d, k0, k1 = _tokens_view("k", k, cache.Hkv)
     dt = _dtype_code(k)
-    if dt != cache.dtype or (q is not None and q.dtype != k.dtype) or (v is not None and v.dtype != k.dtype):
+    if cache.dtype not in (dt, None) or (q is not None and q.dtype != k.dtype) or (v is not None and v.dtype != k.dtype):
         raise TypeError("q, k, v and the cache must share an element type")
     q0 = q1 = o0 = o1 = v0 = v1 = 0
     Hq = cache.Hkv
@@ -557,15 +696,79 @@ def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[tor
             raise ValueError("k and v differ in shape")
         if cache.v_pages is None:
             raise ValueError("the cache holds keys only")
+    return T, Hq, d, dt, q_out, _strides_ref(q0, q1, o0, o1, k0, k1, v0, v1)
+
+
+def ilre_norm_rope(x: torch.Tensor, freqs: Optional[IlreRopeFreqs], positions: Optional[torch.Tensor] = None, *, norms: Optional[HeadNorms] = None,
+                   axes: Optional[Sequence[int]] = None, first_position: int = 0, pairing: int = ILRE_ROPE_HALF, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Norm of every head of x [T, H, d] (norms.q_weight) and rotation to its position; freqs None: no rotation; positions [T], or [number of axes, T] with `axes`, the axis
+    that each pair turns by; `out` may be x itself."""
+    T, H, d, x0, x1 = _tokens_view("x", x)
+    dt = _dtype_code(x)
+    if norms is not None and norms.dtype not in (dt, None):
+        raise TypeError("x and the norms' weights must share an element type")
+    out, o0, o1 = _like("out", out, x)
+    _same_device(x, out, positions)
+    pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
+    if T == 0:
+        return out
+    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    _check(load().ilre_norm_rope(x.data_ptr(), out.data_ptr(), T, H, d, pos, n_axes, ax, int(first_position), fr, int(pairing),
+                                 None if norms is None else norms._ref, _strides_ref(x0, x1, o0, o1), ctypes.byref(o)))
+    return out
+
+
+def ilre_norm_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], cache: PagedKV, freqs: Optional[IlreRopeFreqs],
+                          positions: Optional[torch.Tensor] = None, *, norms: Optional[HeadNorms] = None, axes: Optional[Sequence[int]] = None,
+                          pairing: int = ILRE_ROPE_HALF, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """ilre_rope_append with a norm of every query and key head before the rotation, and with positions along several axes (positions [number of axes, T], axes: the
+    axis that each pair turns by); freqs None: no rotation.  The cache may be a QuantKV."""
+    T, Hq, d, dt, q_out, st = _append_arguments(q, k, v, cache, q_out)
+    if norms is not None and norms.dtype not in (dt, None):
+        raise TypeError("the states and the norms' weights must share an element type")
+    _same_device(q, k, v, q_out, positions, cache.k_pages)
+    pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return q_out
-    st = _strides_ref(q0, q1, o0, o1, k0, k1, v0, v1)
     o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
-    _check(load().ilre_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
-                                   None if v is None else v.data_ptr(), T, Hq, d,
-                                   None if positions is None else _int32_vector("positions", positions, T), ctypes.byref(freqs), int(pairing),
-                                   cache._ref, st, ctypes.byref(o)))
+    _check(load().ilre_norm_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
+                                        None if v is None else v.data_ptr(), T, Hq, d, pos, n_axes, ax, fr, int(pairing),
+                                        None if norms is None else norms._ref, cache._ref, st, ctypes.byref(o)))
     return q_out
+
+
+def ilre_cache_read(cache: PagedKV, T: int, tokens: Optional[torch.Tensor] = None, *, dtype: torch.dtype = torch.bfloat16, values: bool = True,
+                    k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Keys and values out of a paged cache, T rows cut up by cache.cu_q: the tokens `tokens` (int32 [T]), or the last tokens of each sequence.  Returns (k_out, v_out) [T,
+    Hkv, d]; the caller's own tensors (k_out alone: keys only) may be views of the recall's key cache, k_cache.transpose(0, 1)."""
+    if k_out is None and v_out is None:
+        dt = dtype if cache.dtype is None else cache.k_pages.dtype
+        k_out = torch.empty((T, cache.Hkv, 128), dtype=dt, device=cache.k_pages.device)
+        v_out = torch.empty_like(k_out) if values and cache.v_pages is not None else None
+    k0 = k1 = v0 = v1 = 0
+    ref = k_out if k_out is not None else v_out
+    dt = _dtype_code(ref)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is None:
+            continue
+        n, _, d, s0, s1 = _tokens_view(name, t, cache.Hkv)
+        if n != T or d != 128 or t.dtype != ref.dtype:
+            raise ValueError(f"{name} is a device tensor [{T}, {cache.Hkv}, 128] of one element type")
+        if name == "k_out":
+            k0, k1 = s0, s1
+        else:
+            v0, v1 = s0, s1
+    if cache.dtype not in (dt, None):
+        raise TypeError("the cache and what is read from it must share an element type")
+    if v_out is not None and cache.v_pages is None:
+        raise ValueError("the cache holds keys only")
+    _same_device(k_out, v_out, tokens, cache.k_pages)
+    if T == 0:
+        return k_out, v_out
+    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    _check(load().ilre_cache_read(None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(), T, 128,
+                                  None if tokens is None else _int32_vector("tokens", tokens, T), cache._ref, _strides_ref(0, 0, 0, 0, k0, k1, v0, v1), ctypes.byref(o)))
+    return k_out, v_out
 
 
 def ilre_attention_workspace_bytes(T: int, n_seq: int, Hq: int, Hkv: int, d: int, max_q: int, max_kv: int, total_kv: int, dtype: int) -> int:
@@ -596,7 +799,7 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
     cut up, not what comes out."""
     T, Hq, d, q0, q1 = _tokens_view("q", q)
     dt = _dtype_code(q)
-    if dt != cache.dtype:
+    if cache.dtype not in (dt, None):
         raise TypeError("q and the cache must share an element type")
     if cache.v_pages is None:
         raise ValueError("the cache holds keys only")
@@ -611,6 +814,37 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
     st = _strides_ref(q0, q1, o0, o1)
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
     _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, at, cache._ref, st, ctypes.byref(o)))
+    return out, lse
+
+
+def ilre_tree_attention(q: torch.Tensor, cache: PagedKV, tree: torch.Tensor, *, max_q: int, max_kv: int, total_kv: int = 0, scale: float = 0.0,
+                        workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                        ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of drafted tokens q [T, Hq, d], stored at the ends of their sequences: each sees all of the context before them, and those of its sequence's drafted tokens
+    whose bit is set in its row of `tree` (int32 [T, words], bit j % 32 of word j / 32).  Returns (out [T, Hq, d], lse float32 [T, Hq])."""
+    T, Hq, d, q0, q1 = _tokens_view("q", q)
+    dt = _dtype_code(q)
+    if cache.dtype not in (dt, None):
+        raise TypeError("q and the cache must share an element type")
+    if cache.v_pages is None:
+        raise ValueError("the cache holds keys only")
+    if tree.dtype != torch.int32 or not tree.is_cuda or tree.dim() != 2 or tree.shape[0] != T or (tree.shape[1] > 1 and tree.stride(1) != 1):
+        raise ValueError(f"tree is an int32 device tensor [{T}, words] with contiguous rows")
+    words, row = tree.shape[1], tree.stride(0) if T > 1 else 0
+    if T > 1 and row == 0:  # (0 stands for contiguous in the C ABI)
+        raise ValueError("a tree expanded over tokens is not supported")
+    out, o0, o1, lse = _attention_outputs(q, out, lse, T, Hq)
+    _same_device(q, tree, out, lse, workspace, cache.k_pages)
+    if T == 0:
+        return out, lse
+    if workspace is None:
+        workspace = alloc_workspace_attention(T, cache.n_seq, Hq, cache.Hkv, d, max_q, max_kv, total_kv=total_kv, dtype=dt, device=q.device)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace is a contiguous device tensor")
+    at = _attn_ref(0, 0, 0, int(max_q), int(max_kv), int(total_kv))
+    o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
+    _check(load().ilre_tree_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, tree.data_ptr(), words, row, at, cache._ref,
+                                      _strides_ref(q0, q1, o0, o1), ctypes.byref(o)))
     return out, lse
 
 

@@ -10,7 +10,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libilre.so")
-SOURCES = ["scoring.hip", "select.hip", "rerope.hip", "ceiling.hip", "attention.hip", "rope.hip", "api.hip", "api_attention.hip"]
+SOURCES = ["scoring.hip", "select.hip", "rerope.hip", "ceiling.hip", "attention.hip", "attention_fp8.hip", "attention_fp4.hip", "attention_tree.hip", "attention_tree_fp8.hip",
+           "attention_tree_fp4.hip", "rope.hip", "fill.hip", "api.hip", "api_attention.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

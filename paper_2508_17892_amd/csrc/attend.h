@@ -24,6 +24,7 @@
 
 #include "attn_blocks.h"
 #include "ilre_internal.h"
+#include "kv_codes.h"
 
 #include <math.h>
 
@@ -194,6 +195,97 @@ __device__ __forceinline__ void copy_offsets(int (&voff)[ROWS * ROWB / 1024], in
     }
 }
 
+// ------------------------------------------------------------------------------------------------ tiles of a quantised cache
+
+// Eight tokens of a kv head at a time: lane l has channels 16 (l % 8) .. + 15 of token l / 8, as codes in registers until they are written to LDS as numbers of the states' type,
+// where and as copy_rows would have put them.  Tokens that no row of the block sees are zeros here too (codes and scales past the end of a buffer read as zero).
+template <int FMT>
+struct Codes {
+    static constexpr int W = FMT == ILRE_KV_FP8 ? 4 : 2;  // words of 16 channels
+    unsigned w[W];
+    unsigned char scale;
+};
+
+struct QuantSource {
+    const unsigned char *codes, *scales;  // of the kv head
+    int64_t page, token;                  // channels
+    template <int FMT>
+    static __device__ __forceinline__ QuantSource of(const unsigned char *codes, const unsigned char *scales, int64_t head, int64_t page, int64_t token)
+    {
+        return {codes + code_bytes<FMT>(head), scales + head / ILRE_KV_BLOCK, page, token};
+    }
+};
+
+template <int FMT>
+__device__ __forceinline__ void fetch_codes(const AttnArgs &a, const Block &b, const QuantSource &src, int tok, int page, Codes<FMT> &c, int lane)
+{
+    const int n = page < 0 ? 0 : clamp_to(b.hi - tok, 0, 8);
+    const int64_t at = (int64_t)max(page, 0) * src.page + (int64_t)(tok & ((1 << a.page_shift) - 1)) * src.token;
+    constexpr int ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM);
+    const int token_bytes = (int)code_bytes<FMT>(src.token), token_scales = (int)(src.token / ILRE_KV_BLOCK);
+    auto buffer = [&](const unsigned char *p, int step, int row) {
+        const uint64_t u = (uint64_t)p;
+        const uint64_t base = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
+        return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * step + row : 0), 0x00020000);
+    };
+    const __amdgpu_buffer_rsrc_t codes = buffer(src.codes + code_bytes<FMT>(at), token_bytes, ROW),
+                                 scales = buffer(src.scales + at / ILRE_KV_BLOCK, token_scales, ILRE_HEAD_DIM / ILRE_KV_BLOCK);
+    const int row = lane >> 3, u = lane & 7, t = tok + row;
+    const bool gap = t < b.lo && t >= b.sink;
+    const int from = gap ? -1 : row * token_bytes + u * (ROW / 8), scale_from = gap ? -1 : row * token_scales + u / 2;
+    if constexpr (FMT == ILRE_KV_FP8) {
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, from, 0, 0));
+        c.w[0] = x[0], c.w[1] = x[1], c.w[2] = x[2], c.w[3] = x[3];
+    } else {
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, from, 0, 0));
+        c.w[0] = x[0], c.w[1] = x[1];
+    }
+    c.scale = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_from, 0, 0);
+}
+
+__device__ __forceinline__ void lds_write16(unsigned at, const u32x4 &x) { *(__attribute__((address_space(3))) u32x4 *)(size_t)at = x; }
+
+// The eight tokens to rows first_row .. of a tile of rows at LDS address `to`.  (first_row a multiple of 8.)
+template <int DT, int FMT, bool VALUES>
+__device__ __forceinline__ void write_codes(const Codes<FMT> &c, unsigned to, int first_row, int lane)
+{
+    const float scale = scale_of(c.scale);
+    const int r = first_row + (lane >> 3), u = lane & 7, swap = VALUES ? (r & 3) << 2 : r & 15;
+    constexpr int ROWB = DT == ILRE_BF16 ? 256 : 512;
+    const unsigned row = to + r * ROWB;
+    if constexpr (DT == ILRE_BF16) {
+        unsigned x[8];
+        if constexpr (FMT == ILRE_KV_FP8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[2 * k] = bf16_pair<FMT, 0>(c.w[k], scale), x[2 * k + 1] = bf16_pair<FMT, 1>(c.w[k], scale);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                x[4 * k] = bf16_pair<FMT, 0>(c.w[k], scale), x[4 * k + 1] = bf16_pair<FMT, 1>(c.w[k], scale);
+                x[4 * k + 2] = bf16_pair<FMT, 2>(c.w[k], scale), x[4 * k + 3] = bf16_pair<FMT, 3>(c.w[k], scale);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) lds_write16(row + ((2 * u + k) ^ swap) * 16, u32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]});
+    } else {
+        float2 x[8];
+        if constexpr (FMT == ILRE_KV_FP8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[2 * k] = f32_pair<FMT, 0>(c.w[k], scale), x[2 * k + 1] = f32_pair<FMT, 1>(c.w[k], scale);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                x[4 * k] = f32_pair<FMT, 0>(c.w[k], scale), x[4 * k + 1] = f32_pair<FMT, 1>(c.w[k], scale);
+                x[4 * k + 2] = f32_pair<FMT, 2>(c.w[k], scale), x[4 * k + 3] = f32_pair<FMT, 3>(c.w[k], scale);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            lds_write16(row + ((4 * u + k) ^ swap) * 16,
+                        u32x4{__float_as_uint(x[2 * k].x), __float_as_uint(x[2 * k].y), __float_as_uint(x[2 * k + 1].x), __float_as_uint(x[2 * k + 1].y)});
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ products
 
 template <int DT>
@@ -335,9 +427,9 @@ struct State {
     }
     // Logits of tokens that the row does not see become -inf: 32 tokens from `at` on; bit 0 / 1 of `absent`: the first / last 16 are on no page.  What the row
     // sees is a word of bits, a few instructions a logit: nearly every tile that comes here has an edge in it.
-    __device__ __forceinline__ void hide(f32x16 &s, int at, int sink, int half, int absent) const
+    __device__ __forceinline__ void hide(f32x16 &s, int at, int sink, int half, int absent, unsigned drafted = ~0u) const
     {
-        unsigned bits = first_bits(hi - at) & (~first_bits(lo - at) | first_bits(sink - at));
+        unsigned bits = first_bits(hi - at) & (~first_bits(lo - at) | first_bits(sink - at)) & drafted;
         bits &= ~((absent & 1 ? 0xFFFFu : 0u) | (absent & 2 ? 0xFFFF0000u : 0u));
         bits >>= 4 * half;
 #pragma unroll
@@ -398,6 +490,28 @@ struct State {
     {
         const float x = (z[0] + z[1]) + (z[2] + z[3]);
         return x + other_half(x);
+    }
+};
+
+// What a row sees of a tree of drafted tokens, which are the tokens from `base` on (it may lie in front of the sequence).
+struct Drafted {
+    const uint32_t *words;
+    int base, n;
+    __device__ __forceinline__ void init(const AttnArgs &a, const Block &blk, int want)
+    {
+        base = blk.kv - blk.q_len;
+        n = a.tree_words;
+        words = a.tree + (int64_t)(blk.q0 + min(want, blk.nrows - 1) / a.G) * a.tree_stride;
+    }
+    // The bits of 32 tokens from `at` on, all set in front of the drafted ones.
+    __device__ __forceinline__ unsigned bits(int at) const
+    {
+        const int j = at - base;
+        if (j <= -32) return ~0u;
+        if (j < 0) return first_bits(-j) | words[0] << -j;
+        const int w = j >> 5;
+        const unsigned lo = w < n ? words[w] : 0, hi = w + 1 < n ? words[w + 1] : 0;
+        return (unsigned)(((unsigned long long)hi << 32 | lo) >> (j & 31));
     }
 };
 
@@ -463,13 +577,17 @@ __device__ __forceinline__ void store_sum(const AttnArgs &a, const Target &t, in
 // they have at the end.  Keys and values have four tile buffers each; while tile i is worked on, its values, the keys of tile i + 1 and (in the pipelined
 // loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.  fp32 tiles have two buffers
 // each, so that two workgroups of four wavefronts fit a compute unit: with one wavefront a SIMD every wait for LDS is a hole between matrix instructions.
-template <int DT, int WAVES, int TS, int TN, bool PAGED>
+//
+// Of a quantised cache (FMT) the next tiles' codes are in registers: the keys of tile i + 2 and the values of tile i + 1 are asked for when those of the tiles before them have been
+// written to LDS, a tile ahead of their use.
+template <int DT, int WAVES, int TS, int TN, bool PAGED, int FMT = kPlain, bool TREE = false>
 __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
 {
     using E = Elem<DT>;
     constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, GROUPS = WAVES / TS, ROWS = GROUPS * 32, SUB = TN / 32 / TS, RING = E::RING;
     constexpr int CROWS = TN / WAVES, COPIES = CROWS * ROWB / 1024;  // a wavefront's rows and copies of a tile
     static_assert(CROWS <= 16 && CROWS * ROWB % 1024 == 0 && TN % 32 == 0, "a wavefront's rows lie on one page");
+    static_assert(FMT == kPlain || (PAGED && CROWS == 8), "a wavefront has eight rows of codes of a tile");
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
@@ -478,6 +596,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     Block blk;
     int split;
     if (!find_unit<PAGED>(a, blockIdx.x / a.Hkv, ROWS, TN, blk, split)) return;
+    if (TREE) blk.all_hi = max(blk.kv - blk.q_len, 0);
     const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN); };
@@ -485,6 +604,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     State<DT> st;
     const int row0 = blk.rows0 + wave % GROUPS * 32, part = wave / GROUPS * SUB * 32;  // its rows, and where its part of a tile begins
     const bool idle = row0 >= blk.nrows;
+    Drafted drafted;
+    if (TREE) drafted.init(a, blk, row0 + l32);
 
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem;
     typename E::Addr ad;
@@ -501,8 +622,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     int kvoff[COPIES], vvoff[COPIES];
     copy_offsets<CROWS, ROWB, false>(kvoff, wave * CROWS, a.k_token, lane);
     copy_offsets<CROWS, ROWB, true>(vvoff, wave * CROWS, a.v_token, lane);
-    int pages[2];  // of this wavefront's rows: of the last tile whose keys were asked for, and the next one
     auto own_token = [&](int i) { return i < count ? token_of(i) + wave * CROWS : blk.hi; };
+    // of a quantised cache: where the head lies, and the codes that are on their way
+    constexpr int QF = FMT == kPlain ? ILRE_KV_FP8 : FMT;
+    const QuantSource qk = QuantSource::of<QF>(a.k, a.k_scales, head * a.k_head, a.k_page, a.k_token), qv = QuantSource::of<QF>(a.v, a.v_scales, head * a.v_head, a.v_page, a.v_token);
+    Codes<QF> key_codes, value_codes;
+    auto fetch_keys = [&](int i, int page) { fetch_codes<QF>(a, blk, qk, own_token(i), page, key_codes, lane); };
+    auto fetch_values = [&](int i, int page) { fetch_codes<QF>(a, blk, qv, own_token(i), page, value_codes, lane); };
+    auto write_keys = [&](int i) { write_codes<DT, QF, false>(key_codes, lds0 + i % RING * SLOT, wave * CROWS, lane); };
+    auto write_values = [&](int i) { write_codes<DT, QF, true>(value_codes, lds0 + (RING + i % RING) * SLOT, wave * CROWS, lane); };
+    int pages[2];  // of this wavefront's rows: of the last tile whose keys were asked for, and the next one
     auto lookup = [&](int i) {
         if (!PAGED) return 0;
         const int t = min(own_token(i), blk.hi - 1), page = page_of(a, blk, t);
@@ -516,6 +645,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         copy_rows<CROWS, ROWB, true, PAGED>(a, blk, vs, own_token(i), page, lds0 + (RING + i % RING) * SLOT + wave * CROWS * ROWB, vvoff, lane);
     };
     auto begin = [&]() {
+        if constexpr (FMT != kPlain) {
+            const int p0 = lookup(0);
+            fetch_keys(0, p0);
+            fetch_values(0, p0);
+            pages[0] = lookup(1);
+            if (RING != 2) {
+                write_keys(0);
+                fetch_keys(1, pages[0]);
+                pages[1] = lookup(2);
+            }
+            return;
+        }
         if (RING == 2) {
             const int p = lookup(0);
             copy_keys(0, p);
@@ -534,6 +675,24 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     };
     // Tile i's values and tile i + 1's keys (two buffers: tile i's) are there, everybody is done with tile i - 1, and the next copies are on their way.
     auto advance = [&](int i) {
+        if constexpr (FMT != kPlain) {
+            write_keys(RING == 2 ? i : i + 1);
+            write_values(i);
+            if (RING == 2) {
+                fetch_keys(i + 1, pages[0]);
+                fetch_values(i + 1, pages[0]);
+                pages[0] = lookup(i + 2);
+            } else {
+                fetch_keys(i + 2, pages[1]);
+                fetch_values(i + 1, pages[0]);
+                pages[0] = pages[1];
+                pages[1] = lookup(i + 3);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            return;
+        }
         if (RING == 2) {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
@@ -567,7 +726,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
             for (int k = 0; k < SUB * 2; ++k) absent |= (page_of(a, blk, tok + 16 * k) < 0 ? 1 : 0) << k;
         }
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) st.hide(s[sub], tok + 32 * sub, a.sink, half, absent >> (2 * sub));
+        for (int sub = 0; sub < SUB; ++sub) st.hide(s[sub], tok + 32 * sub, a.sink, half, absent >> (2 * sub), TREE ? drafted.bits(tok + 32 * sub) : ~0u);
         if (kept.value) {
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) st.weigh_kept(s[sub], w[sub], a.c);
@@ -729,7 +888,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
 // tile buffers of its own and no barrier on the way; what they have is added up at the end.  One buffer each for keys and values (the next keys are asked for
 // when these have become logits) and two workgroups a compute unit: a workgroup's start is 3 us of dependent loads, and the other one reads meanwhile.
 // Two buffers each and one workgroup, 48 requests with 1 to 16384 tokens 96 -> 86 us, one token of 4097 15.4 -> 13.0 us, of a million 695 either way.
-template <int DT, int WAVES, bool PAGED>
+//
+// Of a quantised cache (FMT) the codes of the next tile are on their way to registers while this one's are numbers in LDS.
+template <int DT, int WAVES, bool PAGED, int FMT = kPlain, bool TREE = false>
 __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_tokens(const AttnArgs a)
 {
     using E = Elem<DT>;
@@ -742,6 +903,8 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
     Block blk;
     int split;
     if (!find_unit<PAGED>(a, blockIdx.x / a.Hkv, 32, TN, blk, split)) return;
+    Drafted drafted;
+    if (TREE) drafted.init(a, blk, blk.rows0 + l32);
     const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
@@ -779,12 +942,26 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         copy_rows<16, ROWB, true, PAGED>(a, blk, vs, token_of(i) + 16, p.id[1], lds0 + SLOT + 16 * ROWB, vvoff, lane);
     };
 
+    // of a quantised cache
+    constexpr int QF = FMT == kPlain ? ILRE_KV_FP8 : FMT;
+    const QuantSource qk = QuantSource::of<QF>(a.k, a.k_scales, head * a.k_head, a.k_page, a.k_token), qv = QuantSource::of<QF>(a.v, a.v_scales, head * a.v_head, a.v_page, a.v_token);
+    Codes<QF> key_codes[4], value_codes[4];
+    auto fetch = [&](int i, const Pages &p, const QuantSource &src, Codes<QF> (&c)[4]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) fetch_codes<QF>(a, blk, src, i < count ? token_of(i) + 8 * k : blk.hi, p.id[k / 2], c[k], lane);
+    };
+
     Pages now, next;
     if (count > 0) {
         now = lookup(0);
         next = lookup(min(1, count - 1));
-        copy_keys(0, now);
-        copy_values(0, now);
+        if constexpr (FMT == kPlain) {
+            copy_keys(0, now);
+            copy_values(0, now);
+        } else {
+            fetch(0, now, qk, key_codes);
+            fetch(0, now, qv, value_codes);
+        }
     }
     st.load(a, blk, head, blk.rows0, l32, half);  // behind the copies: they are on their way together
     st.clear();
@@ -794,20 +971,32 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         const int absent = PAGED ? (now.id[0] < 0 ? 1 : 0) | (now.id[1] < 0 ? 2 : 0) : 0;
         f32x16 s[1];
         typename E::Weights w[1];
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");  // this step's values may still be on their way
+        if constexpr (FMT == kPlain) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");  // this step's values may still be on their way
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) write_codes<DT, QF, false>(key_codes[k], lds0, 8 * k, lane);
+            fetch(i + 1, next, qk, key_codes);
+        }
         E::logits(s[0], st.q, ad, lds0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
-        if (more) copy_keys(i + 1, next);
-        st.hide(s[0], token_of(i), a.sink, half, absent);
+        if (FMT == kPlain && more) copy_keys(i + 1, next);
+        st.hide(s[0], token_of(i), a.sink, half, absent, TREE ? drafted.bits(token_of(i)) : ~0u);
         st.template weigh<1>(s, w, a.c);
-        if (more)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if constexpr (FMT == kPlain) {
+            if (more)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) write_codes<DT, QF, true>(value_codes[k], lds0 + SLOT, 8 * k, lane);
+            fetch(i + 1, next, qv, value_codes);
+        }
         E::values(st.o, w[0], ad, lds0 + SLOT);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) {
-            copy_values(i + 1, next);
+            if (FMT == kPlain) copy_values(i + 1, next);
             now = next;
             next = lookup(min(i + 2, count - 1));
         }
@@ -985,34 +1174,34 @@ hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const At
     return hipGetLastError();
 }
 
-template <int DT, int WAVES, int TS, int TN, bool PAGED>
+template <int DT, int WAVES, int TS, int TN, bool PAGED, int FMT, bool TREE>
 hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(attend_rows<DT, WAVES, TS, TN, PAGED>, p, WAVES * 64, 2 * Elem<DT>::RING * TN * Elem<DT>::ROWB + 16 + (TS == 2 ? WAVES * 32 * sizeof(float2) : 0), a, s);
+    return launch(attend_rows<DT, WAVES, TS, TN, PAGED, FMT, TREE>, p, WAVES * 64, 2 * Elem<DT>::RING * TN * Elem<DT>::ROWB + 16 + (TS == 2 ? WAVES * 32 * sizeof(float2) : 0), a, s);
 }
 
-template <int DT, int WAVES, bool PAGED>
+template <int DT, int WAVES, bool PAGED, int FMT, bool TREE>
 hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(attend_tokens<DT, WAVES, PAGED>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
+    return launch(attend_tokens<DT, WAVES, PAGED, FMT, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
-template <bool PAGED>
+template <bool PAGED, int FMT = kPlain, bool TREE = false>
 hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
     hipError_t e;
     if (p.dtype == ILRE_BF16) {
         if (p.rows == 32)
-            e = launch_tokens<ILRE_BF16, 4, PAGED>(p, a, s);
+            e = launch_tokens<ILRE_BF16, 4, PAGED, FMT, TREE>(p, a, s);
         else if (p.rows == 128)
-            e = launch_rows<ILRE_BF16, 8, 2, 64, PAGED>(p, a, s);
+            e = launch_rows<ILRE_BF16, 8, 2, 64, PAGED, FMT, TREE>(p, a, s);
         else
-            e = launch_rows<ILRE_BF16, 8, 1, 64, PAGED>(p, a, s);
+            e = launch_rows<ILRE_BF16, 8, 1, 64, PAGED, FMT, TREE>(p, a, s);
     } else {
         if (p.rows == 32)
-            e = launch_tokens<ILRE_F32, 4, PAGED>(p, a, s);
+            e = launch_tokens<ILRE_F32, 4, PAGED, FMT, TREE>(p, a, s);
         else
-            e = launch_rows<ILRE_F32, 4, 1, 32, PAGED>(p, a, s);
+            e = launch_rows<ILRE_F32, 4, 1, 32, PAGED, FMT, TREE>(p, a, s);
     }
     if (e != hipSuccess || p.nsplit == 1) return e;
     return p.dtype == ILRE_BF16 ? launch_merge<ILRE_BF16, PAGED>(p, a, s) : launch_merge<ILRE_F32, PAGED>(p, a, s);

@@ -54,7 +54,7 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
     return p;
 }
 
-hipError_t launch_attention(const AttnPlan &p, AttnArgs a, void *workspace, hipStream_t s)
+hipError_t launch_attention(const AttnPlan &p, AttnArgs a, int format, void *workspace, hipStream_t s)
 {
     a.nsplit = p.nsplit;
     a.split_tiles = p.split_tiles;
@@ -63,6 +63,9 @@ hipError_t launch_attention(const AttnPlan &p, AttnArgs a, void *workspace, hipS
     a.tile = p.tile;
     a.part_o = (float *)workspace;
     a.part_e = a.part_o + (int64_t)p.nsplit * a.T * a.Hq * kHeadDim;
+    if (format == ILRE_KV_FP8) return a.tree ? launch_attention_tree_fp8(p, a, s) : launch_attention_fp8(p, a, s);
+    if (format == ILRE_KV_FP4) return a.tree ? launch_attention_tree_fp4(p, a, s) : launch_attention_fp4(p, a, s);
+    if (a.tree) return launch_attention_tree(p, a, s);
     return a.table ? launch_kernels<true>(p, a, s) : launch_kernels<false>(p, a, s);
 }
 

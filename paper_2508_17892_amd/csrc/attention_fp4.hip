@@ -1,0 +1,8 @@
+// Attention over a cache of 4-bit codes.
+#include "attend.h"
+
+namespace ilre {
+
+hipError_t launch_attention_fp4(const AttnPlan &p, const AttnArgs &a, hipStream_t s) { return launch_kernels<true, ILRE_KV_FP4, false>(p, a, s); }
+
+}  // namespace ilre

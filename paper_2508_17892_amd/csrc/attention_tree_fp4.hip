@@ -1,0 +1,8 @@
+// Attention of a tree of drafted tokens over a cache of 4-bit codes.
+#include "attend.h"
+
+namespace ilre {
+
+hipError_t launch_attention_tree_fp4(const AttnPlan &p, const AttnArgs &a, hipStream_t s) { return launch_kernels<true, ILRE_KV_FP4, true>(p, a, s); }
+
+}  // namespace ilre

@@ -1,0 +1,487 @@
+// Norms of queries and keys, their rotation to positions along one axis or several, and the fill of a cache of pages held in 16 (32), 8 or 4 bits, in one pass, for gfx950.
+//
+//   y = x w / sqrt(mean(x^2) + eps),   (y_1, y_2) -> m (y_1 cos a - y_2 sin a, y_2 cos a + y_1 sin a),   a = position[axis of pair j] * inv_freq[j]
+//
+// A wavefront has one token.  Lane j makes sine and cosine of pair j, once for all heads of the token, and leaves them in LDS; eight lanes then share a head, each with channels 8u .. 8u + 7
+// and 64 + 8u .. 64 + 8u + 7, so that a head's loads and stores are whole, and the 32 channels that share a scale lie with four neighbouring lanes.  A channel is
+// r (x A + p B): p the other channel of its pair, A and B its cosine and signed sine times the weights of the two, r the norm.
+//
+// Queries and caches of the states' own type: fp32 (the angle's fraction of a turn in fp64).  Keys of a quantised cache: fp64 throughout, fp64 sines and cosines too, and one rounding, to the code.  A
+// code's border is met by one key in 2^19 or so if the key itself is off by 2^-24, and then what a cache holds depends on the order of operations of whoever fills it.
+#include "kv_codes.h"
+
+#include <type_traits>
+
+namespace ilre {
+namespace {
+
+constexpr int kThreads = 256;
+// Where the other channel of a pair is: with the same lane (half-split pairing over all 128 channels), anywhere (half-split over fewer), next to it.
+enum { kSameLane, kElsewhere, kNeighbour };
+
+template <int DT>
+struct Eight {  // channels, as they lie in memory
+    static constexpr int N = DT == ILRE_BF16 ? 1 : 2;
+    uint4 v[N];
+    __device__ __forceinline__ void load(const unsigned char *p)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = ((const uint4 *)p)[i];
+    }
+    __device__ __forceinline__ void store(unsigned char *p) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) ((uint4 *)p)[i] = v[i];
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (DT == ILRE_BF16) {
+                    f[2 * k] = __uint_as_float(w[k] << 16);
+                    f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+                } else {
+                    f[4 * i + k] = __uint_as_float(w[k]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(const float (&f)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                w[k] = DT == ILRE_BF16 ? __builtin_bit_cast(uint32_t, __builtin_convertvector((kv_f32x2{f[2 * k], f[2 * k + 1]}), kv_bf16x2)) : __float_as_uint(f[4 * i + k]);
+            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+};
+
+template <int DT, int FMT, int PAIR, int WPT>
+__global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
+{
+    using Real = std::conditional_t<FMT == kPlain, float, double>;  // of keys
+    struct Turn {
+        Real c, s;  // cosine and sine, times the magnitude
+    };
+    constexpr int ES = DT == ILRE_BF16 ? 2 : 4;
+    __shared__ Turn wheels[kThreads / 64][ILRE_HEAD_DIM / 2];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int token = (int)blockIdx.x * (kThreads / 64 / WPT) + wave / WPT;
+    if (token >= a.T) return;
+    const int u = lane & 7, slot = lane >> 3;
+    Turn *wheel = wheels[wave];
+
+    // the token's place in its sequence, and where that is in the cache
+    double place = (double)a.first_position + token;
+    int64_t cell = -1;
+    if (a.cu_q) {
+        int seq = -1;
+        for (int base = 0; base < a.n_seq; base += 64) {
+            const int s = base + lane;
+            const unsigned long long past = __ballot(s < a.n_seq && a.cu_q[s + 1] > token);
+            if (past) {
+                seq = __builtin_amdgcn_readfirstlane(base + __builtin_ctzll(past));
+                break;
+            }
+        }
+        if (seq < 0) return;  // a token of no sequence
+        const int q0 = max(a.cu_q[seq], 0), q1 = min(a.cu_q[seq + 1], a.T);
+        if (token < q0) return;
+        const int64_t at = (int64_t)a.kv_len[seq] - (q1 - q0) + (token - q0);
+        place = (double)at;
+        if (at >= 0 && at < a.kv_limit) {
+            const int page = a.table[seq * a.table_stride + (at >> a.page_shift)];
+            if ((unsigned)page < (unsigned)a.num_pages) cell = page * a.page + (at & (((int64_t)1 << a.page_shift) - 1)) * a.token;
+        }
+    }
+    if (lane < a.rotary / 2) {
+        if (a.positions) place = a.positions[(int64_t)a.axes[lane] * a.T + token];
+        const double n = place * a.turns[lane], part = n - rint(n);
+        if (FMT == kPlain) {
+            const float upper = (float)part, lower = (float)(part - upper) * 6.283185307f, m = (float)a.magnitude;
+            float s, c;
+            sincospif(2.0f * upper, &s, &c);
+            wheel[lane].s = fmaf(c, lower, s) * m;
+            wheel[lane].c = fmaf(-s, lower, c) * m;
+        } else {
+            double s, c;
+            sincospi(2.0 * part, &s, &c);
+            wheel[lane].s = (Real)(s * a.magnitude);
+            wheel[lane].c = (Real)(c * a.magnitude);
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+    // of the lane's two runs of eight channels: where they begin, whether they are turned, their pairs, and where the others of these begin
+    const int half = a.rotary / 2;
+    int from[2], pair[2], other[2];
+    bool turned[2], first[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        from[s] = 64 * s + 8 * u;
+        turned[s] = PAIR == kSameLane || from[s] < a.rotary;
+        first[s] = PAIR == kSameLane ? s == 0 : from[s] < half;
+        pair[s] = PAIR == kNeighbour ? from[s] / 2 : first[s] ? from[s] : from[s] - half;
+        other[s] = !turned[s] ? from[s] : first[s] ? from[s] + half : from[s] - half;
+    }
+    // Channel e of run s: its pair's cosine and sine (with the sign that its part takes); what is not turned is multiplied with one and added to minus zero, which changes nothing.
+    auto turn_of = [&](int s, int e) {
+        Turn t;
+        if (PAIR == kNeighbour) {
+            t = wheel[(pair[s] + e / 2) & 63];
+            t.s = e & 1 ? t.s : -t.s;
+        } else {
+            t = wheel[(pair[s] + e) & 63];
+            t.s = first[s] ? -t.s : t.s;
+        }
+        if (!turned[s]) t.c = 1, t.s = -(Real)0;
+        return t;
+    };
+    auto weights = [&](const unsigned char *w, int at, float (&f)[8]) {
+        if (!w) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = 1.f;
+            return;
+        }
+        Eight<DT> x;
+        x.load(w + at * ES);
+        x.get(f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] += a.offset;
+    };
+    // the weights of the lane's channels and of the others of their pairs
+    auto weights_of = [&](const unsigned char *w, float (&own)[2][8], float (&others)[2][8]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) weights(w, from[s], own[s]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (PAIR == kElsewhere) weights(w, other[s], others[s]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (PAIR == kSameLane) others[s][e] = own[1 - s][e];
+                if (PAIR == kNeighbour) others[s][e] = own[s][e ^ 1];
+            }
+        }
+    };
+    // A head's channels, and the others of their pairs (zeros where nothing is turned: an infinity there would not stay out).
+    struct Head {
+        Eight<DT> x[2], p[2];
+    };
+    auto fetch = [&](Head &h, const unsigned char *at) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            h.x[s].load(at + from[s] * ES);
+            if (PAIR == kElsewhere) h.p[s].load(at + other[s] * ES);
+        }
+    };
+    auto values = [&](const Head &h, float (&x)[2][8], float (&p)[2][8]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) h.x[s].get(x[s]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (PAIR == kElsewhere) h.p[s].get(p[s]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (PAIR == kSameLane) p[s][e] = x[1 - s][e];
+                if (PAIR == kNeighbour) p[s][e] = x[s][e ^ 1];
+                if (PAIR != kSameLane) p[s][e] = turned[s] ? p[s][e] : 0.f;
+            }
+        }
+    };
+    // 1 / sqrt(mean + eps) of a head, the same for its eight lanes
+    auto norm32 = [&](const float (&x)[2][8]) {
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[s][e], x[s][e], sum);
+#pragma unroll
+        for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
+        return 1.f / sqrtf(sum * (1.f / ILRE_HEAD_DIM) + (float)a.eps);
+    };
+    auto norm64 = [&](const float (&x)[2][8]) {
+        double sum = 0.0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fma((double)x[s][e], (double)x[s][e], sum);
+#pragma unroll
+        for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
+        return 1.0 / sqrt(sum * (1.0 / ILRE_HEAD_DIM) + a.eps);
+    };
+    // fp32: coefficients of the token's heads, and a head from its place to another
+    float A[2][8], B[2][8];
+    auto coefficients = [&](const unsigned char *w) {
+        float own[2][8], others[2][8];
+        weights_of(w, own, others);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const Turn t = turn_of(s, e);
+                A[s][e] = own[s][e] * (float)t.c;
+                B[s][e] = turned[s] ? others[s][e] * (float)t.s : -0.f;
+            }
+    };
+    auto turn32 = [&](Head &h, bool norm) {
+        float x[2][8], p[2][8];
+        values(h, x, p);
+        const float r = norm ? norm32(x) : 1.f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[s][e] = fmaf(x[s][e], A[s][e], p[s][e] * B[s][e]) * r;
+            h.x[s].put(x[s]);
+        }
+    };
+
+    // queries eight heads at a time, then keys and values as one list of heads
+    const int nq = a.q ? a.Hq : 0, nk = a.k ? a.Hkv : 0, nv = a.v ? a.Hkv : 0;
+    const int steps_q = (nq + 7) / 8, steps = steps_q + (nk + nv + 7) / 8;
+    int step = wave % WPT;
+    if (step < steps_q) coefficients(a.q_norm ? a.q_weight : nullptr);
+    for (; step < steps_q; step += WPT) {
+        const int h = step * 8 + slot;
+        const int at = min(h, nq - 1);
+        Head x;
+        fetch(x, a.q + (int64_t)token * a.q_token + at * a.q_head);
+        turn32(x, a.q_norm);
+        if (h < nq) {
+            unsigned char *to = a.q_out + (int64_t)token * a.out_token + h * a.out_head;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) x.x[s].store(to + from[s] * ES);
+        }
+    }
+    if (step >= steps || cell < 0) return;
+    const unsigned char *kw = a.k_norm ? a.k_weight : nullptr;
+    if (FMT == kPlain) coefficients(kw);
+    for (; step < steps; step += WPT) {
+        const int h = (step - steps_q) * 8 + slot, at = min(h, nk + nv - 1);
+        const bool key = at < nk;
+        Head x;
+        fetch(x, key ? a.k + (int64_t)token * a.k_token + at * a.k_head : a.v + (int64_t)token * a.v_token + (at - nk) * a.v_head);
+        const int64_t to = cell + (key ? h : h - nk) * a.head;
+        if (FMT == kPlain) {
+            Head y = x;
+            turn32(y, a.k_norm);
+            if (h < nk + nv) {
+                unsigned char *p = (key ? a.k_pages : a.v_pages) + to * ES;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) (key ? y.x[s] : x.x[s]).store(p + from[s] * ES);
+            }
+            continue;
+        }
+        float f[2][8], p[2][8];
+        values(x, f, p);
+        if (__ballot(key)) {
+            const double r = a.k_norm ? norm64(f) : 1.0;
+            float own[2][8], others[2][8];
+            weights_of(kw, own, others);
+            float y[2][8];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const Turn t = turn_of(s, e);
+                    y[s][e] = cut_off(((double)f[s][e] * own[s][e] * t.c + (double)p[s][e] * others[s][e] * t.s) * r);
+                }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[s][e] = key ? y[s][e] : f[s][e];
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            unsigned top = 0;  // the largest magnitude, as bits: a NaN's are larger than any number's
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[s][e]) & 0x7FFFFFFFu);
+            top = max(top, (unsigned)__shfl_xor((int)top, 1));
+            top = max(top, (unsigned)__shfl_xor((int)top, 2));
+            const unsigned byte = scale_byte<FMT == kPlain ? ILRE_KV_FP8 : FMT>(__uint_as_float(top));
+            const float inv = inverse_scale(byte);
+            const int64_t channel = to + from[s];
+            if (h >= nk + nv) continue;
+            unsigned char *codes = (key ? a.k_pages : a.v_pages) + (FMT == ILRE_KV_FP8 ? channel : channel / 2);
+            if (FMT == ILRE_KV_FP8)
+                *(uint2 *)codes = byte == 255 ? make_uint2(0, 0) : to_fp8(f[s], inv);
+            else
+                *(unsigned *)codes = byte == 255 ? 0 : to_fp4(f[s], inv);
+            if ((u & 3) == 0) (key ? a.k_scales : a.v_scales)[channel / ILRE_KV_BLOCK] = (unsigned char)byte;
+        }
+    }
+}
+
+template <int DT, int FMT, int PAIR>
+hipError_t launch(const FillArgs &a, hipStream_t s)
+{
+    if (a.T < 4096)
+        hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 4>), dim3((unsigned)a.T), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 1>), dim3((unsigned)((a.T + 3) / 4)), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int DT, int FMT>
+hipError_t launch_pairing(const FillArgs &a, int pairing, hipStream_t s)
+{
+    if (pairing == ILRE_ROPE_INTERLEAVED) return launch<DT, FMT, kNeighbour>(a, s);
+    return a.rotary == ILRE_HEAD_DIM ? launch<DT, FMT, kSameLane>(a, s) : launch<DT, FMT, kElsewhere>(a, s);
+}
+
+template <int DT>
+hipError_t launch_format(const FillArgs &a, int format, int pairing, hipStream_t s)
+{
+    return format == ILRE_KV_FP8   ? launch_pairing<DT, ILRE_KV_FP8>(a, pairing, s)
+           : format == ILRE_KV_FP4 ? launch_pairing<DT, ILRE_KV_FP4>(a, pairing, s)
+                                   : launch_pairing<DT, kPlain>(a, pairing, s);
+}
+
+// ------------------------------------------------------------------------------------------------ reading a cache back
+
+// Rows (token, head) with eight lanes each, which have the channels that they have above; kItems rows a lane, whose loads are under way together.  One pass, HBM.
+constexpr int kItems = 4;
+
+template <int DT, int FMT>
+__global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int rows_first)
+{
+    constexpr int ES = DT == ILRE_BF16 ? 2 : 4;
+    const int lane = threadIdx.x & 63, u = lane & 7;
+    const int64_t items = (int64_t)a.T * a.Hkv, first = (int64_t)blockIdx.x * (kThreads / 8 * kItems) + (threadIdx.x >> 6) * (8 * kItems) + (lane >> 3);
+    int row[kItems], head[kItems];
+    bool real[kItems];
+    int64_t cell[kItems];  // -1: zeros
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {  // rows or heads running fastest
+        const int64_t item = min(first + 8 * k, items - 1);
+        real[k] = first + 8 * k < items;
+        row[k] = (int)(rows_first ? item % a.T : item / a.Hkv);
+        head[k] = (int)(rows_first ? item / a.T : item % a.Hkv);
+    }
+    // the rows' sequences: the wavefront looks for its lowest row's, the others look on from there
+    int lowest = __builtin_amdgcn_readfirstlane(row[0]), begin = a.n_seq;
+    if (__ballot(row[0] < lowest || row[1] < lowest || row[2] < lowest || row[3] < lowest)) lowest = 0;  // on to the next head's rows
+    for (int base = 0; base < a.n_seq; base += 64) {
+        const int s = base + lane;
+        const unsigned long long past = __ballot(s < a.n_seq && a.cu_q[s + 1] > lowest);
+        if (past) {
+            begin = base + __builtin_ctzll(past);
+            break;
+        }
+    }
+    static_assert(kItems == 4, "the rows named above");
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        int seq = begin;
+        while (seq < a.n_seq && a.cu_q[seq + 1] <= row[k]) ++seq;
+        cell[k] = -1;
+        const int r0 = seq < a.n_seq ? max(a.cu_q[seq], 0) : 0x7FFFFFFF;
+        real[k] = real[k] && row[k] >= r0;  // otherwise a row of no sequence
+        if (!real[k]) continue;
+        const int r1 = min(a.cu_q[seq + 1], a.T), len = a.kv_len[seq];
+        const int64_t at = a.tokens ? (int64_t)a.tokens[row[k]] : (int64_t)len - (r1 - r0) + (row[k] - r0);
+        if (at < 0 || at >= min((int64_t)len, a.kv_limit)) continue;
+        const int page = a.table[seq * a.table_stride + (at >> a.page_shift)];
+        if ((unsigned)page < (unsigned)a.num_pages) cell[k] = page * a.page + (at & (((int64_t)1 << a.page_shift) - 1)) * a.token + head[k] * a.head;
+    }
+    // Codes and scales of a run of eight channels, all zeros where there is nothing to read.
+    struct Run {
+        Eight<DT> x;
+        uint2 codes;
+        unsigned byte;
+    };
+    auto fetch = [&](Run &r, const unsigned char *pages, const unsigned char *scales, int64_t at) {
+        r.x.zero();
+        r.codes = make_uint2(0, 0);
+        r.byte = 0;
+        if (at < 0) return;
+        if (FMT == kPlain) {
+            r.x.load(pages + at * ES);
+            return;
+        }
+        r.byte = scales[at / ILRE_KV_BLOCK];
+        if (FMT == ILRE_KV_FP8)
+            r.codes = *(const uint2 *)(pages + at);
+        else
+            r.codes.x = *(const unsigned *)(pages + at / 2);
+    };
+    auto store = [&](Run &r, unsigned char *to) {
+        if constexpr (FMT != kPlain) {
+            const float scale = r.byte == 255 ? __uint_as_float(0x7FC00000u) : scale_of(r.byte);
+            float f[8];
+            if constexpr (FMT == ILRE_KV_FP8) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const unsigned c = k ? r.codes.y : r.codes.x;
+                    const float2 x = f32_pair<FMT, 0>(c, 1.f), z = f32_pair<FMT, 1>(c, 1.f);
+                    f[4 * k] = x.x * scale, f[4 * k + 1] = x.y * scale, f[4 * k + 2] = z.x * scale, f[4 * k + 3] = z.y * scale;
+                }
+            } else {
+                const unsigned c = r.codes.x;
+                const float2 x[4] = {f32_pair<FMT, 0>(c, 1.f), f32_pair<FMT, 1>(c, 1.f), f32_pair<FMT, 2>(c, 1.f), f32_pair<FMT, 3>(c, 1.f)};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[2 * k] = x[k].x * scale, f[2 * k + 1] = x[k].y * scale;
+            }
+            r.x.put(f);
+        }
+        r.x.store(to);
+    };
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        unsigned char *out = t ? a.v_out : a.k_out;
+        if (!out) continue;
+        const unsigned char *pages = t ? a.v_pages : a.k_pages, *scales = t ? a.v_scales : a.k_scales;
+        const int64_t out_token = t ? a.v_token : a.k_token, out_head = t ? a.v_head : a.k_head;
+        Run r[kItems][2];
+#pragma unroll
+        for (int k = 0; k < kItems; ++k)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) fetch(r[k][s], pages, scales, cell[k] < 0 ? -1 : cell[k] + 64 * s + 8 * u);
+#pragma unroll
+        for (int k = 0; k < kItems; ++k)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (real[k]) store(r[k][s], out + row[k] * out_token + head[k] * out_head + (64 * s + 8 * u) * ES);
+    }
+}
+
+template <int DT>
+hipError_t launch_read_format(const ReadArgs &a, int format, hipStream_t s)
+{
+    const int64_t items = (int64_t)a.T * a.Hkv;
+    const int64_t each = kThreads / 8 * kItems;
+    const dim3 grid((unsigned)((items + each - 1) / each));
+    const int rows_first = a.k_out ? a.k_token < a.k_head : a.v_token < a.v_head;
+    if (format == ILRE_KV_FP8)
+        hipLaunchKernelGGL((read_kernel<DT, ILRE_KV_FP8>), grid, dim3(kThreads), 0, s, a, rows_first);
+    else if (format == ILRE_KV_FP4)
+        hipLaunchKernelGGL((read_kernel<DT, ILRE_KV_FP4>), grid, dim3(kThreads), 0, s, a, rows_first);
+    else
+        hipLaunchKernelGGL((read_kernel<DT, kPlain>), grid, dim3(kThreads), 0, s, a, rows_first);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_fill(const FillArgs &a, int dtype, int format, int pairing, hipStream_t s)
+{
+    return dtype == ILRE_BF16 ? launch_format<ILRE_BF16>(a, format, pairing, s) : launch_format<ILRE_F32>(a, format, pairing, s);
+}
+
+hipError_t launch_read(const ReadArgs &a, int dtype, int format, hipStream_t s)
+{
+    return dtype == ILRE_BF16 ? launch_read_format<ILRE_BF16>(a, format, s) : launch_read_format<ILRE_F32>(a, format, s);
+}
+
+}  // namespace ilre

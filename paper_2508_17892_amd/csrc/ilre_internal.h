@@ -230,6 +230,47 @@ struct TurnArgs {
 
 hipError_t launch_turn(const TurnArgs &a, int dtype, int pairing, hipStream_t s);
 
+// ---------------------------------------------------------------- norms, rotary positions on axes, fill of a quantised cache; reading a cache back
+
+constexpr int kPlain = 0;  // beside ILRE_KV_FP8, ILRE_KV_FP4: a cache of the states' element type
+
+struct FillArgs {
+    const unsigned char *q, *k, *v;  // [T, heads, d]; each may be null
+    unsigned char *q_out;
+    int64_t q_token, q_head, out_token, out_head, k_token, k_head, v_token, v_head;  // bytes
+    const unsigned char *q_weight, *k_weight;  // null: weight + offset is one
+    int q_norm, k_norm;
+    float offset;
+    double eps;
+    const int32_t *positions;        // [n_axes, T]; null: first_position + token, or the place in the cache
+    int T, Hq, Hkv, rotary, first_position;  // rotary 0: nothing is turned
+    double magnitude;
+    // the cache
+    unsigned char *k_pages, *v_pages, *k_scales, *v_scales;
+    int64_t page, head, token;       // strides in channels
+    const int32_t *table, *kv_len, *cu_q;
+    int64_t table_stride, kv_limit;
+    int n_seq, num_pages, page_shift;
+    double turns[ILRE_HEAD_DIM / 2];  // of pair j, a position
+    uint8_t axes[ILRE_HEAD_DIM / 2];
+};
+
+hipError_t launch_fill(const FillArgs &a, int dtype, int format, int pairing, hipStream_t s);
+
+struct ReadArgs {
+    unsigned char *k_out, *v_out;    // [T, Hkv, d]; each may be null
+    int64_t k_token, k_head, v_token, v_head;  // bytes
+    const int32_t *tokens;           // null: a sequence's last tokens
+    int T, Hkv;
+    const unsigned char *k_pages, *v_pages, *k_scales, *v_scales;
+    int64_t page, head, token;       // strides in channels
+    const int32_t *table, *kv_len, *cu_q;
+    int64_t table_stride, kv_limit;
+    int n_seq, num_pages, page_shift;
+};
+
+hipError_t launch_read(const ReadArgs &a, int dtype, int format, hipStream_t s);
+
 // ---------------------------------------------------------------- attention over a paged cache or packed keys and values
 
 struct AttnArgs {
@@ -247,6 +288,12 @@ struct AttnArgs {
     // the plan
     int nsplit, split_tiles, nblocks, rows, tile;
     float *part_o, *part_e;  // [nsplit][T * Hq][d], [nsplit][T * Hq]
+    // a quantised cache: k and v are its codes, and a code's scale lies at its offset in channels / ILRE_KV_BLOCK
+    const unsigned char *k_scales, *v_scales;
+    // a tree of drafted tokens: which of its sequence's new tokens each one sees, as bits of words
+    const uint32_t *tree;
+    int64_t tree_stride;
+    int tree_words;
 };
 
 // How a call is cut up: blocks of `rows` query rows a kv head (32: attend_tokens, otherwise attend_rows), tiles of `tile` tokens, up to nsplit ranges of
@@ -260,7 +307,13 @@ struct AttnPlan {
 constexpr int64_t kMaxUnits = (int64_t)1 << 22;
 
 AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
-hipError_t launch_attention(const AttnPlan &p, AttnArgs a, void *workspace, hipStream_t s);
+hipError_t launch_attention(const AttnPlan &p, AttnArgs a, int format, void *workspace, hipStream_t s);
+// The kernels by kind of call; `a` has its plan already.
+hipError_t launch_attention_fp8(const AttnPlan &p, const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_fp4(const AttnPlan &p, const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_tree(const AttnPlan &p, const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_tree_fp8(const AttnPlan &p, const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_tree_fp4(const AttnPlan &p, const AttnArgs &a, hipStream_t s);
 
 // ---------------------------------------------------------------- of api.hip, for the other entry points
 
