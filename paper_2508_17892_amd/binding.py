@@ -708,10 +708,10 @@ def ilre_norm_rope(x: torch.Tensor, freqs: Optional[IlreRopeFreqs], positions: O
     if norms is not None and norms.dtype not in (dt, None):
         raise TypeError("x and the norms' weights must share an element type")
     out, o0, o1 = _like("out", out, x)
-    _same_device(x, out, positions)
     pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return out
+    _same_device(x, out, positions)
     o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
     _check(load().ilre_norm_rope(x.data_ptr(), out.data_ptr(), T, H, d, pos, n_axes, ax, int(first_position), fr, int(pairing),
                                  None if norms is None else norms._ref, _strides_ref(x0, x1, o0, o1), ctypes.byref(o)))
@@ -726,10 +726,10 @@ def ilre_norm_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optiona
     T, Hq, d, dt, q_out, st = _append_arguments(q, k, v, cache, q_out)
     if norms is not None and norms.dtype not in (dt, None):
         raise TypeError("the states and the norms' weights must share an element type")
-    _same_device(q, k, v, q_out, positions, cache.k_pages)
     pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return q_out
+    _same_device(q, k, v, q_out, positions, cache.k_pages)
     o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
     _check(load().ilre_norm_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
                                         None if v is None else v.data_ptr(), T, Hq, d, pos, n_axes, ax, fr, int(pairing),
@@ -762,12 +762,13 @@ def ilre_cache_read(cache: PagedKV, T: int, tokens: Optional[torch.Tensor] = Non
         raise TypeError("the cache and what is read from it must share an element type")
     if v_out is not None and cache.v_pages is None:
         raise ValueError("the cache holds keys only")
-    _same_device(k_out, v_out, tokens, cache.k_pages)
     if T == 0:
         return k_out, v_out
+    at = None if tokens is None else _int32_vector("tokens", tokens, T)
+    _same_device(k_out, v_out, tokens, cache.k_pages)
     o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
-    _check(load().ilre_cache_read(None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(), T, 128,
-                                  None if tokens is None else _int32_vector("tokens", tokens, T), cache._ref, _strides_ref(0, 0, 0, 0, k0, k1, v0, v1), ctypes.byref(o)))
+    _check(load().ilre_cache_read(None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(), T, 128, at,
+                                  cache._ref, _strides_ref(0, 0, 0, 0, k0, k1, v0, v1), ctypes.byref(o)))
     return k_out, v_out
 
 
@@ -834,7 +835,6 @@ def ilre_tree_attention(q: torch.Tensor, cache: PagedKV, tree: torch.Tensor, *, 
     if T > 1 and row == 0:  # (0 stands for contiguous in the C ABI)
         raise ValueError("a tree expanded over tokens is not supported")
     out, o0, o1, lse = _attention_outputs(q, out, lse, T, Hq)
-    _same_device(q, tree, out, lse, workspace, cache.k_pages)
     if T == 0:
         return out, lse
     if workspace is None:
@@ -842,6 +842,7 @@ def ilre_tree_attention(q: torch.Tensor, cache: PagedKV, tree: torch.Tensor, *, 
     elif not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace is a contiguous device tensor")
     at = _attn_ref(0, 0, 0, int(max_q), int(max_kv), int(total_kv))
+    _same_device(q, tree, out, lse, workspace, cache.k_pages)
     o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
     _check(load().ilre_tree_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, tree.data_ptr(), words, row, at, cache._ref,
                                       _strides_ref(q0, q1, o0, o1), ctypes.byref(o)))

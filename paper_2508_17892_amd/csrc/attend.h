@@ -407,13 +407,15 @@ struct State {
         z[0] = z[1] = z[2] = z[3] = 0.f;
     }
     // Query row row0 + l32 of the sequence; past the last one zeros, which see what the last one sees and are written nowhere.
+    // HALVES: a lane has the row's first or second 64 channels; otherwise every second 16 bytes.
+    template <bool HALVES = false>
     __device__ __forceinline__ void load(const AttnArgs &a, const Block &blk, int head_kv, int row0, int l32, int half)
     {
         const int want = row0 + l32, r = min(want, blk.nrows - 1);
         const int i = r / a.G, g = r - i * a.G;
-        const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head_kv * a.G + g) * a.q_head + half * 16;
+        const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head_kv * a.G + g) * a.q_head + half * (HALVES ? E::QREGS * 16 : 16);
 #pragma unroll
-        for (int st = 0; st < E::QREGS; ++st) q[st] = *(const u32x4 *)(src + st * 32);
+        for (int st = 0; st < E::QREGS; ++st) q[st] = *(const u32x4 *)(src + st * (HALVES ? 16 : 32));
         // waited for here, not in the loop over tiles, where that would be a wait for the tile copies as well
 #pragma unroll
         for (int st = 0; st < E::QREGS; ++st) asm volatile("" : "+v"(q[st]));
@@ -884,13 +886,60 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
 
 // ------------------------------------------------------------------------------------------------ few rows
 
+// What the wavefronts of a few-row kernel have, added up: sums in LDS where their tiles were (`pitch` bytes a wavefront), the 16-byte pieces of row l32 at place piece ^ l32 % 16,
+// references and sums of weights behind all of them.
+template <int DT, int WAVES, int PITCH>
+__device__ __forceinline__ void join_waves(const AttnArgs &a, const Block &blk, const State<DT> &st, unsigned char *smem, int head, int wave, int l32, int half, bool direct, int split)
+{
+    static_assert(32 * kHeadDim * 4 <= PITCH, "a wavefront's sums fit where its tiles were");
+    auto piece = [&](int w, int at) { return (f32x4 *)(smem + w * PITCH + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
+    float2 *stats = (float2 *)(smem + WAVES * PITCH);  // [WAVES][32]
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *piece(wave, db * 8 + 2 * k + half) = f32x4{st.o[db][4 * k], st.o[db][4 * k + 1], st.o[db][4 * k + 2], st.o[db][4 * k + 3]};
+    const float z = st.sum();
+    if (half == 0) stats[wave * 32 + l32] = make_float2(st.m, z);
+    __syncthreads();
+    float2 ms[WAVES];
+    float top = kFloor, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        ms[w] = stats[w * 32 + l32];
+        top = fmaxf(top, ms[w].x);
+    }
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        ms[w].x = exp2_fast(ms[w].x - top);
+        sum = fmaf(ms[w].y, ms[w].x, sum);
+    }
+    const Target t = target_of(a, blk, head, blk.rows0 + l32, direct, split, top, sum);
+    static_assert(4 % WAVES == 0, "a wavefront's share of the four channel blocks");
+#pragma unroll
+    for (int db = wave; db < 4; db += WAVES) {
+        f32x16 x = f32x16{};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const f32x4 y = *piece(w, db * 8 + 2 * k + half);
+                x[4 * k] = fmaf(y.x, ms[w].x, x[4 * k]);
+                x[4 * k + 1] = fmaf(y.y, ms[w].x, x[4 * k + 1]);
+                x[4 * k + 2] = fmaf(y.z, ms[w].x, x[4 * k + 2]);
+                x[4 * k + 3] = fmaf(y.w, ms[w].x, x[4 * k + 3]);
+            }
+        }
+        store_channels<DT>(a, t, db, x, half);
+    }
+    if (wave == 0) store_sum(a, t, half);
+}
+
 // Bound by reading the cache, and by latency where that is short.  Up to 32 rows: each of WAVES wavefronts takes 32 of a tile's 32 * WAVES tokens, with
 // tile buffers of its own and no barrier on the way; what they have is added up at the end.  One buffer each for keys and values (the next keys are asked for
 // when these have become logits) and two workgroups a compute unit: a workgroup's start is 3 us of dependent loads, and the other one reads meanwhile.
 // Two buffers each and one workgroup, 48 requests with 1 to 16384 tokens 96 -> 86 us, one token of 4097 15.4 -> 13.0 us, of a million 695 either way.
-//
-// Of a quantised cache (FMT) the codes of the next tile are on their way to registers while this one's are numbers in LDS.
-template <int DT, int WAVES, bool PAGED, int FMT = kPlain, bool TREE = false>
+template <int DT, int WAVES, bool PAGED, bool TREE = false>
 __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_tokens(const AttnArgs a)
 {
     using E = Elem<DT>;
@@ -942,26 +991,12 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         copy_rows<16, ROWB, true, PAGED>(a, blk, vs, token_of(i) + 16, p.id[1], lds0 + SLOT + 16 * ROWB, vvoff, lane);
     };
 
-    // of a quantised cache
-    constexpr int QF = FMT == kPlain ? ILRE_KV_FP8 : FMT;
-    const QuantSource qk = QuantSource::of<QF>(a.k, a.k_scales, head * a.k_head, a.k_page, a.k_token), qv = QuantSource::of<QF>(a.v, a.v_scales, head * a.v_head, a.v_page, a.v_token);
-    Codes<QF> key_codes[4], value_codes[4];
-    auto fetch = [&](int i, const Pages &p, const QuantSource &src, Codes<QF> (&c)[4]) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) fetch_codes<QF>(a, blk, src, i < count ? token_of(i) + 8 * k : blk.hi, p.id[k / 2], c[k], lane);
-    };
-
     Pages now, next;
     if (count > 0) {
         now = lookup(0);
         next = lookup(min(1, count - 1));
-        if constexpr (FMT == kPlain) {
-            copy_keys(0, now);
-            copy_values(0, now);
-        } else {
-            fetch(0, now, qk, key_codes);
-            fetch(0, now, qv, value_codes);
-        }
+        copy_keys(0, now);
+        copy_values(0, now);
     }
     st.load(a, blk, head, blk.rows0, l32, half);  // behind the copies: they are on their way together
     st.clear();
@@ -971,80 +1006,222 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         const int absent = PAGED ? (now.id[0] < 0 ? 1 : 0) | (now.id[1] < 0 ? 2 : 0) : 0;
         f32x16 s[1];
         typename E::Weights w[1];
-        if constexpr (FMT == kPlain) {
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");  // this step's values may still be on their way
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) write_codes<DT, QF, false>(key_codes[k], lds0, 8 * k, lane);
-            fetch(i + 1, next, qk, key_codes);
-        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");  // this step's values may still be on their way
         E::logits(s[0], st.q, ad, lds0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
-        if (FMT == kPlain && more) copy_keys(i + 1, next);
+        if (more) copy_keys(i + 1, next);
         st.hide(s[0], token_of(i), a.sink, half, absent, TREE ? drafted.bits(token_of(i)) : ~0u);
         st.template weigh<1>(s, w, a.c);
-        if constexpr (FMT == kPlain) {
-            if (more)
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
-            else
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) write_codes<DT, QF, true>(value_codes[k], lds0 + SLOT, 8 * k, lane);
-            fetch(i + 1, next, qv, value_codes);
-        }
+        if (more)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         E::values(st.o, w[0], ad, lds0 + SLOT);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) {
-            if (FMT == kPlain) copy_values(i + 1, next);
+            copy_values(i + 1, next);
             now = next;
             next = lookup(min(i + 2, count - 1));
         }
     }
-    // What the wavefronts have: sums where their tiles were, the 16-byte pieces of row l32 at place piece ^ l32 % 16, references and sums of weights
-    // behind all of them.
-    static_assert(32 * kHeadDim * 4 <= 2 * SLOT, "a wavefront's sums fit where its tiles were");
-    auto piece = [&](int w, int at) { return (f32x4 *)(smem + w * 2 * SLOT + l32 * kHeadDim * 4 + (at ^ (l32 & 15)) * 16); };
-    float2 *stats = (float2 *)(smem + WAVES * 2 * SLOT);  // [WAVES][32]
+    join_waves<DT, WAVES, 2 * SLOT>(a, blk, st, smem, head, wave, l32, half, nsp == 1, split);
+}
+
+// ------------------------------------------------------------------------------------------------ few rows over a quantised cache
+
+// The same for a quantised cache: 132 or 68 bytes a token and head instead of 256, so that instructions and LDS count as much as bytes do.  Each wavefront takes 32 of a tile's tokens.
+//   - Keys never go through LDS: lane l has half of token l % 32's codes (channels 64 (l / 32) ..), which is the left operand of the matrix instruction once they are converted, two
+//     channels an instruction, scale included.  Which channel stands at which place of the contraction is free; the queries are loaded in the same order.
+//   - Values are converted, 16 or 32 channels of a token a lane, and written to LDS as numbers, from where the transposing read takes them.
+//   - The next tile's codes are asked for when this one's have been converted.
+// Rows that a wavefront does not see: a key's logit is masked whatever it is (the codes come from a page of the pool in any case); values are read through a buffer that ends with the
+// last token, and are zeros past it.
+template <int FMT>
+struct KeyCodes {
+    static constexpr int N = FMT == ILRE_KV_FP8 ? 4 : 2;  // 16-byte pieces of half a token
+    u32x4 w[N];
+    unsigned scales;  // of the whole token
+};
+template <int FMT>
+struct ValueCodes {
+    static constexpr int N = FMT == ILRE_KV_FP8 ? 4 : 2, ROWS = 32 / N;  // pieces a lane, rows that a piece of all lanes holds
+    u32x4 w[N];
+    unsigned char scale[N];
+};
+
+// Two channels (word i of a piece, pair k of the word) as the states' type.
+template <int DT, int FMT>
+__device__ __forceinline__ void piece_to_numbers(const u32x4 &w, float scale, u32x4 (&x)[FMT == ILRE_KV_FP8 ? DT == ILRE_BF16 ? 2 : 4 : DT == ILRE_BF16 ? 4 : 8])
+{
+    constexpr int PER = FMT == ILRE_KV_FP8 ? 2 : 4;  // pairs a word
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+    for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            *piece(wave, db * 8 + 2 * k + half) = f32x4{st.o[db][4 * k], st.o[db][4 * k + 1], st.o[db][4 * k + 2], st.o[db][4 * k + 3]};
-    const float z = st.sum();
-    if (half == 0) stats[wave * 32 + l32] = make_float2(st.m, z);
-    __syncthreads();
-    float2 ms[WAVES];
-    float top = kFloor, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        ms[w] = stats[w * 32 + l32];
-        top = fmaxf(top, ms[w].x);
-    }
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        ms[w].x = exp2_fast(ms[w].x - top);
-        sum = fmaf(ms[w].y, ms[w].x, sum);
-    }
-    const Target t = target_of(a, blk, head, blk.rows0 + l32, nsp == 1, split, top, sum);
-    static_assert(4 % WAVES == 0, "a wavefront's share of the four channel blocks");
-#pragma unroll
-    for (int db = wave; db < 4; db += WAVES) {
-        f32x16 x = f32x16{};
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const f32x4 y = *piece(w, db * 8 + 2 * k + half);
-                x[4 * k] = fmaf(y.x, ms[w].x, x[4 * k]);
-                x[4 * k + 1] = fmaf(y.y, ms[w].x, x[4 * k + 1]);
-                x[4 * k + 2] = fmaf(y.z, ms[w].x, x[4 * k + 2]);
-                x[4 * k + 3] = fmaf(y.w, ms[w].x, x[4 * k + 3]);
+        for (int k = 0; k < PER; ++k) {
+            const int at = i * PER + k;
+            if constexpr (DT == ILRE_BF16) {
+                x[at / 4][at % 4] = k == 0   ? bf16_pair<FMT, 0>(w[i], scale)
+                                    : k == 1 ? bf16_pair<FMT, 1>(w[i], scale)
+                                    : k == 2 ? bf16_pair<FMT, PER == 4 ? 2 : 0>(w[i], scale)
+                                             : bf16_pair<FMT, PER == 4 ? 3 : 0>(w[i], scale);
+            } else {
+                const float2 f = k == 0   ? f32_pair<FMT, 0>(w[i], scale)
+                                 : k == 1 ? f32_pair<FMT, 1>(w[i], scale)
+                                 : k == 2 ? f32_pair<FMT, PER == 4 ? 2 : 0>(w[i], scale)
+                                          : f32_pair<FMT, PER == 4 ? 3 : 0>(w[i], scale);
+                x[at / 2][at % 2 * 2] = __float_as_uint(f.x);
+                x[at / 2][at % 2 * 2 + 1] = __float_as_uint(f.y);
             }
         }
-        store_channels<DT>(a, t, db, x, half);
     }
-    if (wave == 0) store_sum(a, t, half);
+}
+
+template <int DT>
+constexpr size_t codes_lds(int waves)
+{
+    return waves * (32 * kHeadDim * 4 + 32 * sizeof(float2));
+}
+
+template <int DT, int WAVES, int FMT, bool TREE>
+__global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_codes(const AttnArgs a)
+{
+    using E = Elem<DT>;
+    using K = KeyCodes<FMT>;
+    using V = ValueCodes<FMT>;
+    constexpr int ROWB = E::ROWB, PITCH = 32 * kHeadDim * 4, TN = 32 * WAVES, ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM), LANES = ROW / 16;  // lanes a row of values
+    static_assert(32 * ROWB <= PITCH, "the values of a tile fit where the sums go");
+    extern __shared__ __align__(16) unsigned char smem[];
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+    const int head = blockIdx.x % a.Hkv;
+    Block blk;
+    int split;
+    if (!find_unit<true>(a, blockIdx.x / a.Hkv, 32, TN, blk, split)) return;
+    Drafted drafted;
+    if (TREE) {
+        drafted.init(a, blk, blk.rows0 + l32);
+        blk.all_hi = max(drafted.base, 0);
+    }
+    const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
+    const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
+    auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
+
+    State<DT> st;
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * PITCH;
+    typename E::Addr ad;
+    ad.init(lane);
+
+    // the kv head's codes and scales, and the lane's places in them
+    const int64_t head_at = head * a.k_head;
+    const unsigned char *k_codes = a.k + code_bytes<FMT>(head_at) + half * (ROW / 2), *k_scales = a.k_scales + head_at / ILRE_KV_BLOCK;
+    const unsigned char *v_codes = a.v + code_bytes<FMT>(head_at), *v_scales = a.v_scales + head_at / ILRE_KV_BLOCK;
+    const int token_bytes = (int)code_bytes<FMT>(a.k_token), token_scales = (int)(a.k_token / ILRE_KV_BLOCK);
+    const int v_row = lane / LANES, v_piece = lane % LANES;  // of a piece of values: its row and place in it
+    const int page_mask = (1 << a.page_shift) - 1;
+    struct Pages {
+        int id[2];
+    };
+    auto lookup = [&](int i) {
+        const int t = token_of(i);
+        return Pages{{page_of(a, blk, t), page_of(a, blk, t + 16)}};
+    };
+    // 16 tokens from `tok` on, in channels from the kv head's first page on
+    auto place = [&](int tok, int page) { return (int64_t)max(page, 0) * a.k_page + (int64_t)(tok & page_mask) * a.k_token; };
+    auto fetch_keys = [&](int i, const Pages &p, K &c) {
+        const int tok = token_of(i);
+        const int64_t p0 = place(tok, p.id[0]), p1 = place(tok + 16, p.id[1]), at = (l32 < 16 ? p0 : p1) + (int64_t)(l32 & 15) * a.k_token;
+        const unsigned char *from = k_codes + code_bytes<FMT>(at);
+#pragma unroll
+        for (int j = 0; j < K::N; ++j) c.w[j] = ((const u32x4 *)from)[j];
+        c.scales = *(const unsigned *)(k_scales + at / ILRE_KV_BLOCK);
+    };
+    auto fetch_values = [&](int i, const Pages &p, V &c) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int tok = token_of(i) + 16 * g, n = p.id[g] < 0 ? 0 : clamp_to(blk.hi - tok, 0, 16);
+            const int64_t at = place(tok, p.id[g]);
+            auto buffer = [&](const unsigned char *from, int step, int row) {
+                const uint64_t u = (uint64_t)from;
+                const uint64_t base = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
+                return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * step + row : 0), 0x00020000);
+            };
+            const __amdgpu_buffer_rsrc_t codes = buffer(v_codes + code_bytes<FMT>(at), token_bytes, ROW), scales = buffer(v_scales + at / ILRE_KV_BLOCK, token_scales, 4);
+            const bool gap = __builtin_amdgcn_readfirstlane(tok < blk.lo && tok + 16 > blk.sink);
+#pragma unroll
+            for (int j = 0; j < V::N / 2; ++j) {
+                const int row = j * V::ROWS + v_row, t = tok + row;
+                int from = row * token_bytes + v_piece * 16, scale_from = row * token_scales + v_piece * 4 / LANES;
+                if (gap && t < blk.lo && t >= blk.sink) from = scale_from = -1;
+                c.w[g * (V::N / 2) + j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, from, 0, 0));
+                c.scale[g * (V::N / 2) + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_from, 0, 0);
+            }
+        }
+    };
+    constexpr int NX = FMT == ILRE_KV_FP8 ? DT == ILRE_BF16 ? 2 : 4 : DT == ILRE_BF16 ? 4 : 8;  // 16-byte pieces of numbers in one of codes
+    auto write_values = [&](const V &c) {
+#pragma unroll
+        for (int j = 0; j < V::N; ++j) {
+            u32x4 x[NX];
+            piece_to_numbers<DT, FMT>(c.w[j], scale_of(c.scale[j]), x);
+            const int r = j * V::ROWS + v_row;
+#pragma unroll
+            for (int k = 0; k < NX; ++k) lds_write16(lds0 + r * ROWB + (((NX * v_piece + k) ^ (r & 3) << 2) * 16), x[k]);
+        }
+    };
+    // Logits of the tile's 32 tokens: piece j of a lane holds channels 64 half + ROW / 2 / N j .. of its token.
+    auto logits = [&](f32x16 &s, const K &c) {
+        s = f32x16{};
+        const unsigned mine = c.scales >> (16 * half);
+        const float scale[2] = {scale_of(mine & 255), scale_of(mine >> 8 & 255)};
+#pragma unroll
+        for (int j = 0; j < K::N; ++j) {
+            u32x4 x[NX];
+            piece_to_numbers<DT, FMT>(c.w[j], scale[j * 2 / K::N], x);
+#pragma unroll
+            for (int k = 0; k < NX; ++k) {
+                if constexpr (DT == ILRE_BF16) {
+                    Elem<ILRE_BF16>::mma(s, x[k], st.q[j * NX + k]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[k][e]), __uint_as_float(st.q[j * NX + k][e]), s, 0, 0, 0);
+                }
+            }
+        }
+    };
+
+    K keys;
+    V values;
+    Pages now, next;
+    if (count > 0) {
+        now = lookup(0);
+        next = lookup(min(1, count - 1));
+        fetch_keys(0, now, keys);
+        fetch_values(0, now, values);
+    }
+    st.template load<true>(a, blk, head, blk.rows0, l32, half);  // behind the codes: they are on their way together
+    st.clear();
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        const bool more = i + 1 < count;
+        const int tok = token_of(i), absent = (now.id[0] < 0 ? 1 : 0) | (now.id[1] < 0 ? 2 : 0);
+        f32x16 s[1];
+        typename E::Weights w[1];
+        logits(s[0], keys);
+        write_values(values);
+        if (more) {
+            fetch_keys(i + 1, next, keys);
+            fetch_values(i + 1, next, values);
+        }
+        if (tok < blk.all_lo || tok + 32 > blk.all_hi || absent)  // an edge: what a row does not see is hidden
+            st.hide(s[0], tok, a.sink, half, absent, TREE ? drafted.bits(tok) : ~0u);
+        st.template weigh<1>(s, w, a.c);
+        E::values(st.o, w[0], ad, lds0);
+        if (more) {
+            now = next;
+            next = lookup(min(i + 2, count - 1));
+        }
+    }
+    join_waves<DT, WAVES, PITCH>(a, blk, st, smem, head, wave, l32, half, nsp == 1, split);
 }
 
 // ------------------------------------------------------------------------------------------------ merge of the ranges
@@ -1183,7 +1360,8 @@ hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 template <int DT, int WAVES, bool PAGED, int FMT, bool TREE>
 hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(attend_tokens<DT, WAVES, PAGED, FMT, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
+    if constexpr (FMT != kPlain) return launch(attend_codes<DT, WAVES, FMT, TREE>, p, WAVES * 64, codes_lds<DT>(WAVES), a, s);
+    return launch(attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
 template <bool PAGED, int FMT = kPlain, bool TREE = false>
