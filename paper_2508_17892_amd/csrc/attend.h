@@ -51,6 +51,12 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// The larger of a lane's and its partner's, 32 lanes on (a swap of registers' halves, where __shfl_xor goes by way of LDS).
+__device__ __forceinline__ float larger_of_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 __device__ __forceinline__ u32x4 lds_read16(unsigned at) { return *(const __attribute__((address_space(3))) u32x4 *)(size_t)at; }
 __device__ __forceinline__ float lds_read4(unsigned at) { return *(const __attribute__((address_space(3))) float *)(size_t)at; }
@@ -456,13 +462,13 @@ struct State {
         m = m == kFloor ? top : m;
     }
     // The logits of SUB x 32 tokens become weights; the running maximum is followed.
-    template <int SUB>
+    template <int SUB, bool SWAP = false>
     __device__ __forceinline__ void weigh(const f32x16 (&s)[SUB], typename E::Weights (&w)[SUB], float c)
     {
         float top = largest(s[0]);
 #pragma unroll
         for (int u = 1; u < SUB; ++u) top = fmaxf(top, largest(s[u]));
-        top = fmaxf(top, other_half(top));
+        top = SWAP ? larger_of_halves(top) : fmaxf(top, other_half(top));
         const float mnew = fmaxf(m, top * c);
         if (__ballot(mnew != m)) {
             const float f = exp2_fast(m - mnew);
@@ -1111,61 +1117,98 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
     typename E::Addr ad;
     ad.init(lane);
 
-    // the kv head's codes and scales, and the lane's places in them
+    // the kv head's codes and scales, and the lane's places in 32 tokens of them that follow each other
     const int64_t head_at = head * a.k_head;
-    const unsigned char *k_codes = a.k + code_bytes<FMT>(head_at) + half * (ROW / 2), *k_scales = a.k_scales + head_at / ILRE_KV_BLOCK;
+    const unsigned char *k_codes = a.k + code_bytes<FMT>(head_at), *k_scales = a.k_scales + head_at / ILRE_KV_BLOCK;
     const unsigned char *v_codes = a.v + code_bytes<FMT>(head_at), *v_scales = a.v_scales + head_at / ILRE_KV_BLOCK;
-    const int token_bytes = (int)code_bytes<FMT>(a.k_token), token_scales = (int)(a.k_token / ILRE_KV_BLOCK);
+    const unsigned token_bytes = (unsigned)code_bytes<FMT>(a.k_token), token_scales = (unsigned)(a.k_token / ILRE_KV_BLOCK);
+    // Pages of 32 tokens and more: a wavefront's tokens are on one.  Otherwise 16 at a time are.  (Offsets within 32 tokens fit 32 bits.)
+    const bool wide = a.page_shift >= 5;
+    const unsigned k_lane = l32 * token_bytes + half * (ROW / 2), k_lane_scales = l32 * token_scales;
     const int v_row = lane / LANES, v_piece = lane % LANES;  // of a piece of values: its row and place in it
+    unsigned v_lane[V::N], v_lane_scales[V::N];
+#pragma unroll
+    for (int j = 0; j < V::N; ++j) {
+        const unsigned row = j * V::ROWS + v_row;
+        v_lane[j] = row * token_bytes + v_piece * 16;
+        v_lane_scales[j] = row * token_scales + v_piece * 4 / LANES;
+    }
     const int page_mask = (1 << a.page_shift) - 1;
     struct Pages {
         int id[2];
     };
     auto lookup = [&](int i) {
-        const int t = token_of(i);
-        return Pages{{page_of(a, blk, t), page_of(a, blk, t + 16)}};
+        const int t = token_of(i), p = page_of(a, blk, t);
+        return Pages{{p, wide ? p : page_of(a, blk, t + 16)}};
     };
-    // 16 tokens from `tok` on, in channels from the kv head's first page on
+    // Where token `tok` lies, in channels from the kv head's first page on.
     auto place = [&](int tok, int page) { return (int64_t)max(page, 0) * a.k_page + (int64_t)(tok & page_mask) * a.k_token; };
     auto fetch_keys = [&](int i, const Pages &p, K &c) {
         const int tok = token_of(i);
-        const int64_t p0 = place(tok, p.id[0]), p1 = place(tok + 16, p.id[1]), at = (l32 < 16 ? p0 : p1) + (int64_t)(l32 & 15) * a.k_token;
-        const unsigned char *from = k_codes + code_bytes<FMT>(at);
+        const int64_t at = place(tok, p.id[0]);
+        const unsigned char *codes = k_codes + code_bytes<FMT>(at), *scales = k_scales + at / ILRE_KV_BLOCK;
+        if (!wide && l32 >= 16) {
+            const int64_t skip = place(tok + 16, p.id[1]) - 16 * a.k_token;
+            codes = k_codes + code_bytes<FMT>(skip);
+            scales = k_scales + skip / ILRE_KV_BLOCK;
+        }
 #pragma unroll
-        for (int j = 0; j < K::N; ++j) c.w[j] = ((const u32x4 *)from)[j];
-        c.scales = *(const unsigned *)(k_scales + at / ILRE_KV_BLOCK);
+        for (int j = 0; j < K::N; ++j) c.w[j] = *(const u32x4 *)(codes + k_lane + 16 * j);
+        c.scales = *(const unsigned *)(scales + k_lane_scales);
+    };
+    // Rows first .. of the tile, N of them at most, which follow each other in memory from `at` (of row 0) on.
+    auto fetch_rows = [&](int i, int page, int64_t at, auto begin, auto end, V &c) {
+        const int tok = token_of(i), n = page < 0 ? 0 : clamp_to(blk.hi - tok, 0, end.value * V::ROWS);
+        auto buffer = [&](const unsigned char *from, unsigned step, unsigned row) {
+            const uint64_t u = (uint64_t)from;
+            const uint64_t base = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
+            return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (int)((n - 1) * step + row) : 0), 0x00020000);
+        };
+        const __amdgpu_buffer_rsrc_t codes = buffer(v_codes + code_bytes<FMT>(at), token_bytes, ROW), scales = buffer(v_scales + at / ILRE_KV_BLOCK, token_scales, 4);
+        const bool gap = __builtin_amdgcn_readfirstlane(tok < blk.lo && tok + 32 > blk.sink);
+#pragma unroll
+        for (int j = begin.value; j < end.value; ++j) {
+            unsigned from = v_lane[j], scale_from = v_lane_scales[j];
+            if (gap) {
+                const int t = tok + j * V::ROWS + v_row;
+                if (t < blk.lo && t >= blk.sink) from = scale_from = ~0u;
+            }
+            c.w[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)from, 0, 0));
+            c.scale[j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_from, 0, 0);
+        }
     };
     auto fetch_values = [&](int i, const Pages &p, V &c) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int tok = token_of(i) + 16 * g, n = p.id[g] < 0 ? 0 : clamp_to(blk.hi - tok, 0, 16);
-            const int64_t at = place(tok, p.id[g]);
-            auto buffer = [&](const unsigned char *from, int step, int row) {
-                const uint64_t u = (uint64_t)from;
-                const uint64_t base = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
-                return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * step + row : 0), 0x00020000);
-            };
-            const __amdgpu_buffer_rsrc_t codes = buffer(v_codes + code_bytes<FMT>(at), token_bytes, ROW), scales = buffer(v_scales + at / ILRE_KV_BLOCK, token_scales, 4);
-            const bool gap = __builtin_amdgcn_readfirstlane(tok < blk.lo && tok + 16 > blk.sink);
-#pragma unroll
-            for (int j = 0; j < V::N / 2; ++j) {
-                const int row = j * V::ROWS + v_row, t = tok + row;
-                int from = row * token_bytes + v_piece * 16, scale_from = row * token_scales + v_piece * 4 / LANES;
-                if (gap && t < blk.lo && t >= blk.sink) from = scale_from = -1;
-                c.w[g * (V::N / 2) + j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, from, 0, 0));
-                c.scale[g * (V::N / 2) + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_from, 0, 0);
-            }
+        constexpr std::integral_constant<int, 0> none{};
+        constexpr std::integral_constant<int, V::N / 2> middle{};
+        constexpr std::integral_constant<int, V::N> all{};
+        const int tok = token_of(i);
+        if (wide) {
+            fetch_rows(i, p.id[0], place(tok, p.id[0]), none, all, c);
+        } else {
+            fetch_rows(i, p.id[0], place(tok, p.id[0]), none, middle, c);
+            fetch_rows(i, p.id[1], place(tok + 16, p.id[1]) - 16 * a.k_token, middle, all, c);
         }
     };
     constexpr int NX = FMT == ILRE_KV_FP8 ? DT == ILRE_BF16 ? 2 : 4 : DT == ILRE_BF16 ? 4 : 8;  // 16-byte pieces of numbers in one of codes
+    // Eight lanes write together; so that they reach all banks, a lane's pieces go out in an order of its own: piece k ^ turn.
+    const int turn = NX == 2 ? v_piece >> 2 : LANES == 8 ? v_piece >> 1 : NX == 4 ? v_piece >> 1 | (v_row & 1) << 1 : v_piece << 1;
+    unsigned v_to[NX];
+#pragma unroll
+    for (int k = 0; k < NX; ++k) v_to[k] = lds0 + v_row * ROWB + (((NX * v_piece + (k ^ turn)) ^ (v_row & 3) << 2) * 16);
     auto write_values = [&](const V &c) {
 #pragma unroll
         for (int j = 0; j < V::N; ++j) {
-            u32x4 x[NX];
-            piece_to_numbers<DT, FMT>(c.w[j], scale_of(c.scale[j]), x);
-            const int r = j * V::ROWS + v_row;
+            u32x4 w = c.w[j], x[NX];
+            if (NX == 2) {
+                w = turn ? u32x4{w[2], w[3], w[0], w[1]} : w;
+            } else {
+                const int q = NX == 8 ? turn >> 1 : turn;
+                w = q & 1 ? u32x4{w[1], w[0], w[3], w[2]} : w;
+                w = q & 2 ? u32x4{w[2], w[3], w[0], w[1]} : w;
+            }
+            piece_to_numbers<DT, FMT>(w, scale_of(c.scale[j]), x);
 #pragma unroll
-            for (int k = 0; k < NX; ++k) lds_write16(lds0 + r * ROWB + (((NX * v_piece + k) ^ (r & 3) << 2) * 16), x[k]);
+            for (int k = 0; k < NX; ++k) lds_write16(v_to[k] + j * V::ROWS * ROWB, x[k]);
         }
     };
     // Logits of the tile's 32 tokens: piece j of a lane holds channels 64 half + ROW / 2 / N j .. of its token.
@@ -1214,7 +1257,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
         }
         if (tok < blk.all_lo || tok + 32 > blk.all_hi || absent)  // an edge: what a row does not see is hidden
             st.hide(s[0], tok, a.sink, half, absent, TREE ? drafted.bits(tok) : ~0u);
-        st.template weigh<1>(s, w, a.c);
+        st.template weigh<1, true>(s, w, a.c);
         E::values(st.o, w[0], ad, lds0);
         if (more) {
             now = next;
