@@ -1267,6 +1267,238 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
     join_waves<DT, WAVES, PITCH>(a, blk, st, smem, head, wave, l32, half, nsp == 1, split);
 }
 
+// Up to 16 rows, bf16 states: the matrix instructions of 16 rows, as half of the logits, exponentials and sums above would be nobody's.  Lane l has query l % 16; tokens 16 b + 4 (l / 16) + i of
+// logits, i = 0..3, b = 0, 1; channels 16 db + 4 (l / 16) + i of sums.  Of keys it has a quarter of the codes, one block of a scale, of tokens l % 16 and 16 + l % 16.  With fewer
+// registers and half the LDS three or four workgroups fit a compute unit.
+template <int FMT, int WAVES, bool TREE>
+__global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) void attend_codes16(const AttnArgs a)
+{
+    using V = ValueCodes<FMT>;
+    constexpr int ROWB = 256, PITCH = 32 * ROWB, TN = 32 * WAVES, ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM), LANES = ROW / 16, KN = ROW / 64;  // KN: 16-byte pieces of a quarter of a token
+    extern __shared__ __align__(16) unsigned char smem[];
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int head = blockIdx.x % a.Hkv;
+    Block blk;
+    int split;
+    if (!find_unit<true>(a, blockIdx.x / a.Hkv, 16, TN, blk, split)) return;
+    Drafted drafted;
+    if (TREE) {
+        drafted.init(a, blk, blk.rows0 + l16);
+        blk.all_hi = max(drafted.base, 0);
+    }
+    const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
+    const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
+    auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
+
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * PITCH;
+    // the kv head's codes and scales, and the lane's places in 16 or 32 tokens of them that follow each other
+    const int64_t head_at = head * a.k_head;
+    const unsigned char *k_codes = a.k + code_bytes<FMT>(head_at), *k_scales = a.k_scales + head_at / ILRE_KV_BLOCK;
+    const unsigned char *v_codes = a.v + code_bytes<FMT>(head_at), *v_scales = a.v_scales + head_at / ILRE_KV_BLOCK;
+    const unsigned token_bytes = (unsigned)code_bytes<FMT>(a.k_token), token_scales = (unsigned)(a.k_token / ILRE_KV_BLOCK);
+    const bool wide = a.page_shift >= 5;  // a wavefront's 32 tokens are on one page
+    const unsigned k_lane = l16 * token_bytes + g * (ROW / 4), k_lane_scales = l16 * token_scales + g;
+    const int v_row = lane / LANES, v_piece = lane % LANES;
+    const unsigned v_lane = v_row * token_bytes + v_piece * 16, v_lane_scales = v_row * token_scales + v_piece * 4 / LANES;
+    const int page_mask = (1 << a.page_shift) - 1;
+    struct Pages {
+        int id[2];
+    };
+    auto lookup = [&](int i) {
+        const int t = token_of(i), p = page_of(a, blk, t);
+        return Pages{{p, wide ? p : page_of(a, blk, t + 16)}};
+    };
+    auto place = [&](int tok, int page) { return (int64_t)max(page, 0) * a.k_page + (int64_t)(tok & page_mask) * a.k_token; };
+    struct K {
+        u32x4 w[2][KN];
+        unsigned char scale[2];
+    };
+    auto fetch_keys = [&](int i, const Pages &p, K &c) {
+        const int tok = token_of(i);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int64_t at = place(tok + 16 * b, p.id[b]);
+            const unsigned char *codes = k_codes + code_bytes<FMT>(at), *scales = k_scales + at / ILRE_KV_BLOCK;
+#pragma unroll
+            for (int j = 0; j < KN; ++j) c.w[b][j] = *(const u32x4 *)(codes + k_lane + 16 * j);
+            c.scale[b] = scales[k_lane_scales];
+        }
+    };
+    auto fetch_values = [&](int i, const Pages &p, V &c) {
+        const int tok = token_of(i);
+        const bool gap = __builtin_amdgcn_readfirstlane(tok < blk.lo && tok + 32 > blk.sink);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int t0 = tok + 16 * b, n = p.id[b] < 0 ? 0 : clamp_to(blk.hi - t0, 0, 16);
+            const int64_t at = place(t0, p.id[b]);
+            auto buffer = [&](const unsigned char *from, unsigned step, unsigned row) {
+                const uint64_t u = (uint64_t)from;
+                const uint64_t base = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
+                return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (int)((n - 1) * step + row) : 0), 0x00020000);
+            };
+            const __amdgpu_buffer_rsrc_t codes = buffer(v_codes + code_bytes<FMT>(at), token_bytes, ROW), scales = buffer(v_scales + at / ILRE_KV_BLOCK, token_scales, 4);
+#pragma unroll
+            for (int j = 0; j < V::N / 2; ++j) {
+                unsigned from = v_lane + j * V::ROWS * token_bytes, scale_from = v_lane_scales + j * V::ROWS * token_scales;
+                if (gap) {
+                    const int t = t0 + j * V::ROWS + v_row;
+                    if (t < blk.lo && t >= blk.sink) from = scale_from = ~0u;
+                }
+                c.w[b * (V::N / 2) + j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)from, 0, 0));
+                c.scale[b * (V::N / 2) + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_from, 0, 0);
+            }
+        }
+    };
+    // Values in LDS: 16-byte chunk c of row r at place c ^ 2 (r % 4), for the transposing read of 4 rows and 16 channels by 16 lanes; a lane's chunks are written in an order of its own, k ^ turn,
+    // so that eight lanes reach all banks.
+    constexpr int NX = FMT == ILRE_KV_FP8 ? 2 : 4;
+    const int turn = FMT == ILRE_KV_FP8 ? v_piece >> 2 : v_piece >> 1;
+    unsigned v_to[NX], v_from[4];
+#pragma unroll
+    for (int k = 0; k < NX; ++k) v_to[k] = lds0 + v_row * ROWB + (((NX * v_piece + (k ^ turn)) ^ (v_row & 3) << 1) * 16);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) v_from[d] = lds0 + (4 * g + (l16 >> 2)) * ROWB + (d ^ (l16 >> 2)) * 32 + (l16 & 3) * 8;
+    auto write_values = [&](const V &c) {
+#pragma unroll
+        for (int j = 0; j < V::N; ++j) {
+            u32x4 w = c.w[j], x[NX];
+            w = turn ? (NX == 2 ? u32x4{w[2], w[3], w[0], w[1]} : u32x4{w[1], w[0], w[3], w[2]}) : w;
+            piece_to_numbers<ILRE_BF16, FMT>(w, scale_of(c.scale[j]), x);
+#pragma unroll
+            for (int k = 0; k < NX; ++k) lds_write16(v_to[k] + j * V::ROWS * ROWB, x[k]);
+        }
+    };
+    auto mma = [](f32x4 &acc, const u32x4 &x, const u32x4 &y) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+    };
+
+    K keys;
+    V values;
+    Pages now, next;
+    if (count > 0) {
+        now = lookup(0);
+        next = lookup(min(1, count - 1));
+        fetch_keys(0, now, keys);
+        fetch_values(0, now, values);
+    }
+    // the lane's query: channels 32 g + 8 st .. of row rows0 + l16; past the last row zeros, which see what the last one sees and are written nowhere
+    u32x4 q[4];
+    int lo, hi;
+    {
+        const int want = blk.rows0 + l16, r = min(want, blk.nrows - 1), i = r / a.G;
+        const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head * a.G + r - i * a.G) * a.q_head + g * 64;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = want == r ? *(const u32x4 *)(src + k * 16) : u32x4{};
+        const int p = max(blk.kv - blk.q_len + i, -1);
+        hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
+        lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
+    }
+    f32x4 o[8];
+#pragma unroll
+    for (int db = 0; db < 8; ++db) o[db] = f32x4{};
+    float m = kFloor, z = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        const bool more = i + 1 < count;
+        const int tok = token_of(i), absent = (now.id[0] < 0 ? 1 : 0) | (now.id[1] < 0 ? 2 : 0);
+        f32x4 s[2] = {f32x4{}, f32x4{}};
+#pragma unroll
+        for (int j = 0; j < KN; ++j) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                u32x4 x[NX];
+                piece_to_numbers<ILRE_BF16, FMT>(keys.w[b][j], scale_of(keys.scale[b]), x);
+#pragma unroll
+                for (int k = 0; k < NX; ++k) mma(s[b], x[k], q[j * NX + k]);
+            }
+        }
+        write_values(values);
+        if (more) {
+            fetch_keys(i + 1, next, keys);
+            fetch_values(i + 1, next, values);
+        }
+        if (tok < blk.all_lo || tok + 32 > blk.all_hi || absent) {  // an edge: what a row does not see is hidden
+            unsigned bits = first_bits(hi - tok) & (~first_bits(lo - tok) | first_bits(a.sink - tok)) & (TREE ? drafted.bits(tok) : ~0u);
+            bits &= ~((absent & 1 ? 0xFFFFu : 0u) | (absent & 2 ? 0xFFFF0000u : 0u));
+            bits >>= 4 * g;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[b][k] = bits >> (16 * b + k) & 1 ? s[b][k] : -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) top = fmaxf(top, s[k / 4][k % 4]);
+        top = larger_of_halves(top);
+        {
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        }
+        const float mnew = fmaxf(m, top * a.c);
+        if (__ballot(mnew != m)) {
+            const float f = exp2_fast(m - mnew);
+#pragma unroll
+            for (int db = 0; db < 8; ++db) o[db] *= f;
+            z *= f;
+            m = mnew;
+        }
+        float p[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) p[k] = exp2_fast(fmaf(s[k / 4][k % 4], a.c, -m));
+        z += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        const u32x4 w = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            const u32x2 x = lds_read_tr(v_from[db & 3] + (db >> 2) * 128), y = lds_read_tr(v_from[db & 3] + (db >> 2) * 128 + 16 * ROWB);
+            mma(o[db], u32x4{x[0], x[1], y[0], y[1]}, w);
+        }
+        if (more) {
+            now = next;
+            next = lookup(min(i + 2, count - 1));
+        }
+    }
+    // What the wavefronts have, added up: sums where the values were, 16-byte piece of row l16 at place piece ^ l16 % 8, references and sums of weights behind all of them; then a thread
+    // has eight channels of a row.
+    static_assert(16 * kHeadDim * 4 <= PITCH && WAVES * 64 == 256, "sums of 16 rows; 16 threads a row");
+    z += __shfl_xor(z, 16);
+    z += __shfl_xor(z, 32);
+    float2 *stats = (float2 *)(smem + WAVES * PITCH);  // [WAVES][16]
+    auto piece = [&](int w, int row, int at) { return (f32x4 *)(smem + w * PITCH + row * kHeadDim * 4 + (at ^ (row & 7)) * 16); };
+#pragma unroll
+    for (int db = 0; db < 8; ++db) *piece(wave, l16, db * 4 + g) = o[db];
+    if (g == 0) stats[wave * 16 + l16] = make_float2(m, z);
+    __syncthreads();
+    const int row = tid >> 4, part = tid & 15;
+    float2 ms[WAVES];
+    float top = kFloor, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        ms[w] = stats[w * 16 + row];
+        top = fmaxf(top, ms[w].x);
+    }
+    f32x4 x[2] = {f32x4{}, f32x4{}};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const float f = exp2_fast(ms[w].x - top);
+        sum = fmaf(ms[w].y, f, sum);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) x[k] += *piece(w, row, 2 * part + k) * f;
+    }
+    const Target t = target_of(a, blk, head, blk.rows0 + row, nsp == 1, split, top, sum);
+    if (!t.real) return;
+    x[0] *= t.f;
+    x[1] *= t.f;
+    if (t.direct) {
+        *(uint4 *)(t.out + part * 16) = make_uint4(pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]), pack_bf16(x[1][2], x[1][3]));
+    } else {
+        f32x4 *to = (f32x4 *)(a.part_o + t.row * kHeadDim + part * 8);
+        to[0] = x[0];
+        to[1] = x[1];
+    }
+    store_sum(a, t, part);
+}
+
 // ------------------------------------------------------------------------------------------------ merge of the ranges
 
 // What is read here has just been written: latency.  16 lanes a row (token, head), 8 channels each: out = sum_s 2^(e_s - E) o_s / sum_s 2^(e_s - E), E the largest e_s.  WIDE: a workgroup a row, its 16 groups
@@ -1412,6 +1644,12 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
     hipError_t e;
     if (p.dtype == ILRE_BF16) {
+        if constexpr (FMT != kPlain) {
+            if (p.rows == 16) {
+                e = launch(attend_codes16<FMT, 4, TREE>, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s);
+                return e != hipSuccess || p.nsplit == 1 ? e : launch_merge<ILRE_BF16, PAGED>(p, a, s);
+            }
+        }
         if (p.rows == 32)
             e = launch_tokens<ILRE_BF16, 4, PAGED, FMT, TREE>(p, a, s);
         else if (p.rows == 128)

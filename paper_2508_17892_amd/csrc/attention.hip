@@ -13,7 +13,7 @@ namespace ilre {
 //     11.7; 30000 tokens, 8/2 heads: 17.7 and 15.7).  More rows: 12 tiles of 64 tokens at least, and 4 while the merge has little to do (32/8 heads, 4096 tokens: 16
 //     new ones 18.4 us with 4, 25.2 with 12, 64 29.7 and 35.7, 200 51.9 and 40.3), 2 of 32 in fp32 (prompts of 77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6,
 //     6 74).
-AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
+AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
 {
     AttnPlan p{};
     p.dtype = dtype;
@@ -30,7 +30,9 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
         if (window <= 0) return all;
         return std::min(all, (std::min((int64_t)sink, kv) + p.tile - 1) / p.tile + (window + (p.rows + G - 1) / G) / p.tile + 2);
     };
-    if (rows <= 32) {
+    if (rows <= 16 && dtype == ILRE_BF16 && format != kPlain) {
+        cut(16, 128);
+    } else if (rows <= 32) {
         cut(32, 128);
     } else if (dtype == ILRE_F32) {
         cut(128, 32);
@@ -41,8 +43,8 @@ AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q,
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
     const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);
-    const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
-    const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
+    const int64_t places = p.rows == 16 ? (format == ILRE_KV_FP4 ? 4 : 3) * kNumCU : (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
+    const int64_t least = p.rows <= 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
     const int64_t per = std::max<int64_t>((work + places - 1) / places, least);
     int64_t n = (most + per - 1) / per;
     const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);

@@ -296,7 +296,7 @@ struct AttnArgs {
     int tree_words;
 };
 
-// How a call is cut up: blocks of `rows` query rows a kv head (32: attend_tokens, otherwise attend_rows), tiles of `tile` tokens, up to nsplit ranges of
+// How a call is cut up: blocks of `rows` query rows a kv head (16: attend_codes16, 32: attend_tokens or attend_codes, otherwise attend_rows), tiles of `tile` tokens, up to nsplit ranges of
 // split_tiles tiles a block.
 struct AttnPlan {
     int dtype, rows, tile, nblocks, nsplit, split_tiles;
@@ -306,7 +306,12 @@ struct AttnPlan {
 // Most workgroups of a launch (a dimension counts threads in 32 bits, and no workgroup here has more than 512).
 constexpr int64_t kMaxUnits = (int64_t)1 << 22;
 
-AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
+AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
+// The same for a cache of the states' own type.
+inline AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
+{
+    return make_attn_plan(dtype, kPlain, T, n_seq, Hq, Hkv, max_q, max_kv, total_kv, sink, window, workspace);
+}
 hipError_t launch_attention(const AttnPlan &p, AttnArgs a, int format, void *workspace, hipStream_t s);
 // The kernels by kind of call; `a` has its plan already.
 hipError_t launch_attention_fp8(const AttnPlan &p, const AttnArgs &a, hipStream_t s);
