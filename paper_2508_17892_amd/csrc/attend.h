@@ -204,7 +204,7 @@ __device__ __forceinline__ void copy_offsets(int (&voff)[ROWS * ROWB / 1024], in
 // ------------------------------------------------------------------------------------------------ tiles of a quantised cache
 
 // Eight tokens of a kv head at a time: lane l has channels 16 (l % 8) .. + 15 of token l / 8, as codes in registers until they are written to LDS as numbers of the states' type,
-// where and as copy_rows would have put them.  Tokens that no row of the block sees are zeros here too (codes and scales past the end of a buffer read as zero).
+// where copy_rows would have put them.  Tokens that no row of the block sees are zeros here too (codes and scales past the end of a buffer read as zero).
 template <int FMT>
 struct Codes {
     static constexpr int W = FMT == ILRE_KV_FP8 ? 4 : 2;  // words of 16 channels
@@ -212,84 +212,115 @@ struct Codes {
     unsigned char scale;
 };
 
+// Where a kv head's codes and scales of keys and values lie, and a lane's place in eight tokens of them.
+template <int FMT>
 struct QuantSource {
-    const unsigned char *codes, *scales;  // of the kv head
-    int64_t page, token;                  // channels
-    template <int FMT>
-    static __device__ __forceinline__ QuantSource of(const unsigned char *codes, const unsigned char *scales, int64_t head, int64_t page, int64_t token)
+    const unsigned char *codes[2], *scales[2];
+    unsigned token_bytes, token_scales, from, scale_from;
+    __device__ __forceinline__ void init(const AttnArgs &a, int head, int lane)
     {
-        return {codes + code_bytes<FMT>(head), scales + head / ILRE_KV_BLOCK, page, token};
+        const int64_t at = head * a.k_head;
+        codes[0] = a.k + code_bytes<FMT>(at), codes[1] = a.v + code_bytes<FMT>(at);
+        scales[0] = a.k_scales + at / ILRE_KV_BLOCK, scales[1] = a.v_scales + at / ILRE_KV_BLOCK;
+        token_bytes = (unsigned)code_bytes<FMT>(a.k_token);
+        token_scales = (unsigned)(a.k_token / ILRE_KV_BLOCK);
+        from = (lane >> 3) * token_bytes + (lane & 7) * (unsigned)code_bytes<FMT>(16);
+        scale_from = (lane >> 3) * token_scales + (lane & 7) / 2;
     }
 };
 
+// Keys and values of tokens tok .. tok + 7, which are on one page.
 template <int FMT>
-__device__ __forceinline__ void fetch_codes(const AttnArgs &a, const Block &b, const QuantSource &src, int tok, int page, Codes<FMT> &c, int lane)
+__device__ __forceinline__ void fetch_codes(const AttnArgs &a, const Block &b, const QuantSource<FMT> &src, int tok, int page, Codes<FMT> (&c)[2], int lane)
 {
     const int n = page < 0 ? 0 : clamp_to(b.hi - tok, 0, 8);
-    const int64_t at = (int64_t)max(page, 0) * src.page + (int64_t)(tok & ((1 << a.page_shift) - 1)) * src.token;
-    constexpr int ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM);
-    const int token_bytes = (int)code_bytes<FMT>(src.token), token_scales = (int)(src.token / ILRE_KV_BLOCK);
-    auto buffer = [&](const unsigned char *p, int step, int row) {
+    const int64_t at = (int64_t)max(page, 0) * a.k_page + (int64_t)(tok & ((1 << a.page_shift) - 1)) * a.k_token;
+    const int codes_end = n > 0 ? (int)((n - 1) * src.token_bytes + code_bytes<FMT>(ILRE_HEAD_DIM)) : 0;
+    const int scales_end = n > 0 ? (int)((n - 1) * src.token_scales + ILRE_HEAD_DIM / ILRE_KV_BLOCK) : 0;
+    auto buffer = [](const unsigned char *p, int end) {
         const uint64_t u = (uint64_t)p;
         const uint64_t base = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
-        return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * step + row : 0), 0x00020000);
+        return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, __builtin_amdgcn_readfirstlane(end), 0x00020000);
     };
-    const __amdgpu_buffer_rsrc_t codes = buffer(src.codes + code_bytes<FMT>(at), token_bytes, ROW),
-                                 scales = buffer(src.scales + at / ILRE_KV_BLOCK, token_scales, ILRE_HEAD_DIM / ILRE_KV_BLOCK);
-    const int row = lane >> 3, u = lane & 7, t = tok + row;
-    const bool gap = t < b.lo && t >= b.sink;
-    const int from = gap ? -1 : row * token_bytes + u * (ROW / 8), scale_from = gap ? -1 : row * token_scales + u / 2;
-    if constexpr (FMT == ILRE_KV_FP8) {
-        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, from, 0, 0));
-        c.w[0] = x[0], c.w[1] = x[1], c.w[2] = x[2], c.w[3] = x[3];
-    } else {
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, from, 0, 0));
-        c.w[0] = x[0], c.w[1] = x[1];
+    unsigned from = src.from, scale_from = src.scale_from;
+    if (__builtin_amdgcn_readfirstlane(tok < b.lo && tok + 8 > b.sink)) {
+        const int t = tok + (lane >> 3);
+        if (t < b.lo && t >= b.sink) from = scale_from = ~0u;
     }
-    c.scale = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_from, 0, 0);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        const __amdgpu_buffer_rsrc_t codes = buffer(src.codes[v] + code_bytes<FMT>(at), codes_end), scales = buffer(src.scales[v] + at / ILRE_KV_BLOCK, scales_end);
+        if constexpr (FMT == ILRE_KV_FP8) {
+            const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)from, 0, 0));
+            c[v].w[0] = x[0], c[v].w[1] = x[1], c[v].w[2] = x[2], c[v].w[3] = x[3];
+        } else {
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, (int)from, 0, 0));
+            c[v].w[0] = x[0], c[v].w[1] = x[1];
+        }
+        c[v].scale = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_from, 0, 0);
+    }
 }
 
 __device__ __forceinline__ void lds_write16(unsigned at, const u32x4 &x) { *(__attribute__((address_space(3))) u32x4 *)(size_t)at = x; }
 
-// The eight tokens to rows first_row .. of a tile of rows at LDS address `to`.  (first_row a multiple of 8.)
+// Eight tokens to rows first_row .. of a tile in LDS (first_row a multiple of 8).  Eight lanes, the pieces of one row, write together: so that they reach all banks, a lane's 16-byte
+// pieces go out in an order of its own, piece k ^ turn.
 template <int DT, int FMT, bool VALUES>
-__device__ __forceinline__ void write_codes(const Codes<FMT> &c, unsigned to, int first_row, int lane)
-{
-    const float scale = scale_of(c.scale);
-    const int r = first_row + (lane >> 3), u = lane & 7, swap = VALUES ? (r & 3) << 2 : r & 15;
-    constexpr int ROWB = DT == ILRE_BF16 ? 256 : 512;
-    const unsigned row = to + r * ROWB;
-    if constexpr (DT == ILRE_BF16) {
-        unsigned x[8];
-        if constexpr (FMT == ILRE_KV_FP8) {
+struct CodeRows {
+    static constexpr int ROWB = DT == ILRE_BF16 ? 256 : 512, N = ROWB / 128;  // N: 16-byte pieces a lane
+    unsigned to[N];
+    static __device__ __forceinline__ int turn(int lane) { return DT == ILRE_BF16 ? (lane & 7) >> 2 : FMT == ILRE_KV_FP8 ? (lane & 7) >> 1 : (lane & 7) >> 1 & 2; }
+    __device__ __forceinline__ void init(unsigned tile, int first_row, int lane)
+    {
+        const int r = first_row + (lane >> 3), u = lane & 7, swap = VALUES ? (r & 3) << 2 : r & 15;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[2 * k] = bf16_pair<FMT, 0>(c.w[k], scale), x[2 * k + 1] = bf16_pair<FMT, 1>(c.w[k], scale);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                x[4 * k] = bf16_pair<FMT, 0>(c.w[k], scale), x[4 * k + 1] = bf16_pair<FMT, 1>(c.w[k], scale);
-                x[4 * k + 2] = bf16_pair<FMT, 2>(c.w[k], scale), x[4 * k + 3] = bf16_pair<FMT, 3>(c.w[k], scale);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) lds_write16(row + ((2 * u + k) ^ swap) * 16, u32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]});
-    } else {
-        float2 x[8];
-        if constexpr (FMT == ILRE_KV_FP8) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[2 * k] = f32_pair<FMT, 0>(c.w[k], scale), x[2 * k + 1] = f32_pair<FMT, 1>(c.w[k], scale);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                x[4 * k] = f32_pair<FMT, 0>(c.w[k], scale), x[4 * k + 1] = f32_pair<FMT, 1>(c.w[k], scale);
-                x[4 * k + 2] = f32_pair<FMT, 2>(c.w[k], scale), x[4 * k + 3] = f32_pair<FMT, 3>(c.w[k], scale);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            lds_write16(row + ((4 * u + k) ^ swap) * 16,
-                        u32x4{__float_as_uint(x[2 * k].x), __float_as_uint(x[2 * k].y), __float_as_uint(x[2 * k + 1].x), __float_as_uint(x[2 * k + 1].y)});
+        for (int k = 0; k < N; ++k) to[k] = tile + r * ROWB + (((N * u + (k ^ turn(lane))) ^ swap) * 16);
     }
+};
+
+// `slot`: the tile's distance from the one that CodeRows was made for.
+template <int DT, int FMT, bool VALUES>
+__device__ __forceinline__ void write_codes(const Codes<FMT> &c, const CodeRows<DT, FMT, VALUES> &rows, unsigned slot, int lane)
+{
+    constexpr int N = CodeRows<DT, FMT, VALUES>::N, PER = FMT == ILRE_KV_FP8 ? 2 : 4;  // PER: pairs of channels a word
+    const float scale = scale_of(c.scale);
+    const int turn = rows.turn(lane);
+    unsigned w[4] = {c.w[0], c.w[1], c.w[Codes<FMT>::W - 2], c.w[Codes<FMT>::W - 1]};
+    auto exchange = [](unsigned &p, unsigned &q, bool yes) {
+        const unsigned a = p, b = q;
+        p = yes ? b : a;
+        q = yes ? a : b;
+    };
+    if (FMT == ILRE_KV_FP4) {
+        exchange(w[0], w[1], turn != 0);
+    } else {
+        if (DT == ILRE_F32) {
+            exchange(w[0], w[1], turn & 1);
+            exchange(w[2], w[3], turn & 1);
+        }
+        exchange(w[0], w[2], DT == ILRE_F32 ? turn & 2 : turn);
+        exchange(w[1], w[3], DT == ILRE_F32 ? turn & 2 : turn);
+    }
+    unsigned x[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {  // channels 2i, 2i + 1 of what is written
+        const unsigned word = w[i / PER];
+        if constexpr (DT == ILRE_BF16) {
+            x[i] = i % PER == 0   ? bf16_pair<FMT, 0>(word, scale)
+                   : i % PER == 1 ? bf16_pair<FMT, 1>(word, scale)
+                   : i % PER == 2 ? bf16_pair<FMT, PER == 4 ? 2 : 0>(word, scale)
+                                  : bf16_pair<FMT, PER == 4 ? 3 : 0>(word, scale);
+        } else {
+            const float2 f = i % PER == 0   ? f32_pair<FMT, 0>(word, scale)
+                             : i % PER == 1 ? f32_pair<FMT, 1>(word, scale)
+                             : i % PER == 2 ? f32_pair<FMT, PER == 4 ? 2 : 0>(word, scale)
+                                            : f32_pair<FMT, PER == 4 ? 3 : 0>(word, scale);
+            x[2 * i] = __float_as_uint(f.x);
+            x[2 * i + 1] = __float_as_uint(f.y);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) lds_write16(rows.to[k] + slot, u32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]});
 }
 
 // ------------------------------------------------------------------------------------------------ products
@@ -586,8 +617,7 @@ __device__ __forceinline__ void store_sum(const AttnArgs &a, const Target &t, in
 // loop) the values of tile i - 1 are in use, and the copies of keys i + 2, i + 3 and values i + 1, i + 2 under way.  fp32 tiles have two buffers
 // each, so that two workgroups of four wavefronts fit a compute unit: with one wavefront a SIMD every wait for LDS is a hole between matrix instructions.
 //
-// Of a quantised cache (FMT) the next tiles' codes are in registers: the keys of tile i + 2 and the values of tile i + 1 are asked for when those of the tiles before them have been
-// written to LDS, a tile ahead of their use.
+// Of a quantised cache (FMT) the codes of tile i + 2 are on their way to registers while tile i is worked on; before, those of tile i + 1 have been converted and written to LDS.
 template <int DT, int WAVES, int TS, int TN, bool PAGED, int FMT = kPlain, bool TREE = false>
 __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
 {
@@ -633,12 +663,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     auto own_token = [&](int i) { return i < count ? token_of(i) + wave * CROWS : blk.hi; };
     // of a quantised cache: where the head lies, and the codes that are on their way
     constexpr int QF = FMT == kPlain ? ILRE_KV_FP8 : FMT;
-    const QuantSource qk = QuantSource::of<QF>(a.k, a.k_scales, head * a.k_head, a.k_page, a.k_token), qv = QuantSource::of<QF>(a.v, a.v_scales, head * a.v_head, a.v_page, a.v_token);
-    Codes<QF> key_codes, value_codes;
-    auto fetch_keys = [&](int i, int page) { fetch_codes<QF>(a, blk, qk, own_token(i), page, key_codes, lane); };
-    auto fetch_values = [&](int i, int page) { fetch_codes<QF>(a, blk, qv, own_token(i), page, value_codes, lane); };
-    auto write_keys = [&](int i) { write_codes<DT, QF, false>(key_codes, lds0 + i % RING * SLOT, wave * CROWS, lane); };
-    auto write_values = [&](int i) { write_codes<DT, QF, true>(value_codes, lds0 + (RING + i % RING) * SLOT, wave * CROWS, lane); };
+    QuantSource<QF> quant;
+    CodeRows<DT, QF, false> key_rows;
+    CodeRows<DT, QF, true> value_rows;
+    if (FMT != kPlain) {
+        quant.init(a, head, lane);
+        key_rows.init(lds0, wave * CROWS, lane);
+        value_rows.init(lds0 + RING * SLOT, wave * CROWS, lane);
+    }
+    Codes<QF> codes[2];  // of keys and values
+    auto fetch = [&](int i, int page) { fetch_codes<QF>(a, blk, quant, own_token(i), page, codes, lane); };
+    auto write = [&](int i) {
+        write_codes<DT, QF, false>(codes[0], key_rows, i % RING * SLOT, lane);
+        write_codes<DT, QF, true>(codes[1], value_rows, i % RING * SLOT, lane);
+    };
     int pages[2];  // of this wavefront's rows: of the last tile whose keys were asked for, and the next one
     auto lookup = [&](int i) {
         if (!PAGED) return 0;
@@ -654,15 +692,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     };
     auto begin = [&]() {
         if constexpr (FMT != kPlain) {
-            const int p0 = lookup(0);
-            fetch_keys(0, p0);
-            fetch_values(0, p0);
-            pages[0] = lookup(1);
-            if (RING != 2) {
-                write_keys(0);
-                fetch_keys(1, pages[0]);
-                pages[1] = lookup(2);
+            const int p0 = lookup(0), p1 = lookup(1);
+            fetch(0, p0);
+            if (RING == 2) {
+                pages[0] = p1;
+                return;
             }
+            write(0);
+            fetch(1, p1);
+            pages[0] = lookup(2);
             return;
         }
         if (RING == 2) {
@@ -684,18 +722,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     // Tile i's values and tile i + 1's keys (two buffers: tile i's) are there, everybody is done with tile i - 1, and the next copies are on their way.
     auto advance = [&](int i) {
         if constexpr (FMT != kPlain) {
-            write_keys(RING == 2 ? i : i + 1);
-            write_values(i);
-            if (RING == 2) {
-                fetch_keys(i + 1, pages[0]);
-                fetch_values(i + 1, pages[0]);
-                pages[0] = lookup(i + 2);
-            } else {
-                fetch_keys(i + 2, pages[1]);
-                fetch_values(i + 1, pages[0]);
-                pages[0] = pages[1];
-                pages[1] = lookup(i + 3);
-            }
+            constexpr int AHEAD = RING == 2 ? 0 : 1;  // with four buffers what is written now is for the next tile
+            write(i + AHEAD);
+            fetch(i + AHEAD + 1, pages[0]);
+            pages[0] = lookup(i + AHEAD + 2);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");

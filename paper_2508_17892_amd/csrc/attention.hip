@@ -13,6 +13,10 @@ namespace ilre {
 //     11.7; 30000 tokens, 8/2 heads: 17.7 and 15.7).  More rows: 12 tiles of 64 tokens at least, and 4 while the merge has little to do (32/8 heads, 4096 tokens: 16
 //     new ones 18.4 us with 4, 25.2 with 12, 64 29.7 and 35.7, 200 51.9 and 40.3), 2 of 32 in fp32 (prompts of 77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6,
 //     6 74).
+//   - Up to 16 rows over a quantised cache (tiles of 128 tokens): a workgroup a compute unit reads nearly as fast as HBM gives (32 requests of 1500 tokens, 8 kv heads 24.9 us whole, 25.5 in two),
+//     so that lists stay whole where the longest has no more tiles than a compute unit's share of all and what a merge costs, four, or five at most (128 requests of 1000 tokens: whole 56 us, in two
+//     63; one of 640: whole 9.4, single tiles 10.5; four of 1000: single tiles 10.7, whole 13.6). What is cut makes two ranges a compute unit (48 requests of 1 to 16384 tokens, 4 kv heads:
+//     ranges of 12 tiles 47.0 us, 10 53.0, 7 50.3; 65536 tokens, 8 kv heads: 8 33.7, 6 36.3; 262144: 32 102.7, 22 106.8).
 AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
 {
     AttnPlan p{};
@@ -43,9 +47,18 @@ AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
     const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);
-    const int64_t places = p.rows == 16 ? (format == ILRE_KV_FP4 ? 4 : 3) * kNumCU : (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
-    const int64_t least = p.rows <= 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
-    const int64_t per = std::max<int64_t>((work + places - 1) / places, least);
+    const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
+    const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
+    int64_t per = std::max<int64_t>((work + places - 1) / places, least);
+    if (p.rows == 16) {
+        const int64_t lists = blocks * Hkv, mean = tiles(total_kv / n_seq);
+        auto units = [&](int64_t x) { return most == mean ? lists * ((most + x - 1) / x) : lists * (2 * mean + x) / (2 * x); };  // lists of unlike lengths end with half a range each
+        per = std::max<int64_t>(work <= kNumCU ? 1 : 2, work / (2 * kNumCU));
+        if (most <= std::max<int64_t>(5, work / kNumCU + 4))
+            per = most;
+        else
+            while (per < most && units(per) > 2 * kNumCU) ++per;
+    }
     int64_t n = (most + per - 1) / per;
     const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);
     n = std::max<int64_t>(1, std::min({n, (int64_t)256, (int64_t)(workspace / (size_t)row_bytes), kMaxUnits / std::max<int64_t>(p.nblocks * (int64_t)Hkv, 1)}));
