@@ -33,6 +33,17 @@ struct Eight {  // channels, as they lie in memory
 #pragma unroll
         for (int i = 0; i < N; ++i) ((uint4 *)p)[i] = v[i];
     }
+    __device__ __forceinline__ void choose(bool mine, const Eight &o)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = make_uint4(mine ? v[i].x : o.v[i].x, mine ? v[i].y : o.v[i].y, mine ? v[i].z : o.v[i].z, mine ? v[i].w : o.v[i].w);
+    }
+    // What has been worked out from the channels so far is worked out again, not kept in registers.
+    __device__ __forceinline__ void forget()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i].x), "+v"(v[i].y), "+v"(v[i].z), "+v"(v[i].w));
+    }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
@@ -67,20 +78,75 @@ struct Eight {  // channels, as they lie in memory
     }
 };
 
+// Where pair j's sine and cosine lie: eight lanes read every eighth pair (every fourth) at a time, from different banks.
+__device__ __forceinline__ int spread(int j) { return j + (j >> 3); }
+
 template <int DT, int FMT, int PAIR, int WPT>
 __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
 {
     using Real = std::conditional_t<FMT == kPlain, float, double>;  // of keys
     struct Turn {
-        Real c, s;  // cosine and sine, times the magnitude
+        float c, s;  // cosine and sine, times the magnitude
+    };
+    struct KeyTurn {
+        Real c, s;
     };
     constexpr int ES = DT == ILRE_BF16 ? 2 : 4;
-    __shared__ Turn wheels[kThreads / 64][ILRE_HEAD_DIM / 2];
+    __shared__ Turn wheels[kThreads / 64][ILRE_HEAD_DIM / 2 + 8];
+    __shared__ KeyTurn key_wheels[FMT == kPlain ? 1 : kThreads / 64][FMT == kPlain ? 1 : ILRE_HEAD_DIM / 2 + 8];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const int token = (int)blockIdx.x * (kThreads / 64 / WPT) + wave / WPT;
     if (token >= a.T) return;
     const int u = lane & 7, slot = lane >> 3;
     Turn *wheel = wheels[wave];
+    KeyTurn *key_wheel = key_wheels[FMT == kPlain ? 0 : wave];
+
+    // of the lane's two runs of eight channels: where they begin, whether they are turned, their pairs, and where the others of these begin
+    const int half = a.rotary / 2;
+    int from[2], pair[2], other[2];
+    bool turned[2], first[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        from[s] = 64 * s + 8 * u;
+        turned[s] = PAIR == kSameLane || from[s] < a.rotary;
+        first[s] = PAIR == kSameLane ? s == 0 : from[s] < half;
+        pair[s] = PAIR == kNeighbour ? from[s] / 2 : first[s] ? from[s] : from[s] - half;
+        other[s] = !turned[s] ? from[s] : first[s] ? from[s] + half : from[s] - half;
+    }
+    // A head's channels, and the others of their pairs; likewise their weights.
+    struct Head {
+        Eight<DT> x[2], p[2];
+    };
+    auto fetch = [&](Head &h, const unsigned char *at) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            h.x[s].load(at + from[s] * ES);
+            if (PAIR == kElsewhere) h.p[s].load(at + other[s] * ES);
+        }
+    };
+    // Queries eight heads at a time, then keys and values as one list of heads; WPT wavefronts take turns.  What the first of a wavefront's steps needs is asked for at once, before it is
+    // known where the token stands, and each step's heads a step ahead.
+    const int nq = a.q ? a.Hq : 0, nk = a.k ? a.Hkv : 0, nv = a.v ? a.Hkv : 0;
+    const int steps_q = (nq + 7) / 8, steps = steps_q + (nk + nv + 7) / 8;
+    auto fetch_step = [&](Head &h, int step) {
+        if (step >= steps) return;
+        if (step < steps_q) {
+            fetch(h, a.q + (int64_t)token * a.q_token + min(step * 8 + slot, nq - 1) * a.q_head);
+        } else {
+            const int at = min((step - steps_q) * 8 + slot, nk + nv - 1);
+            fetch(h, at < nk ? a.k + (int64_t)token * a.k_token + at * a.k_head : a.v + (int64_t)token * a.v_token + (at - nk) * a.v_head);
+        }
+    };
+    int step = wave % WPT;
+    Head head, weight;
+    fetch_step(head, step);
+    auto fetch_weights = [&](bool norm, const unsigned char *w) {
+        if (norm && w) fetch(weight, w);
+    };
+    const bool queries = step < steps_q;
+    fetch_weights(queries ? a.q_norm : a.k_norm, queries ? a.q_weight : a.k_weight);
+    const double turns = lane < half ? a.turns[lane] : 0.0;
+    const int position = a.positions && lane < half ? a.positions[(int64_t)a.axes[lane] * a.T + token] : 0;
 
     // the token's place in its sequence, and where that is in the cache
     double place = (double)a.first_position + token;
@@ -105,99 +171,46 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
             if ((unsigned)page < (unsigned)a.num_pages) cell = page * a.page + (at & (((int64_t)1 << a.page_shift) - 1)) * a.token;
         }
     }
-    if (lane < a.rotary / 2) {
-        if (a.positions) place = a.positions[(int64_t)a.axes[lane] * a.T + token];
-        const double n = place * a.turns[lane], part = n - rint(n);
+    if (a.positions) place = position;
+    if (lane < half) {
+        const double n = place * turns, part = n - rint(n);
         if (FMT == kPlain) {
             const float upper = (float)part, lower = (float)(part - upper) * 6.283185307f, m = (float)a.magnitude;
             float s, c;
             sincospif(2.0f * upper, &s, &c);
-            wheel[lane].s = fmaf(c, lower, s) * m;
-            wheel[lane].c = fmaf(-s, lower, c) * m;
+            wheel[spread(lane)].s = fmaf(c, lower, s) * m;
+            wheel[spread(lane)].c = fmaf(-s, lower, c) * m;
         } else {
             double s, c;
             sincospi(2.0 * part, &s, &c);
-            wheel[lane].s = (Real)(s * a.magnitude);
-            wheel[lane].c = (Real)(c * a.magnitude);
+            s *= a.magnitude;
+            c *= a.magnitude;
+            key_wheel[spread(lane)] = KeyTurn{(Real)c, (Real)s};
+            wheel[spread(lane)] = Turn{(float)c, (float)s};
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 
-    // of the lane's two runs of eight channels: where they begin, whether they are turned, their pairs, and where the others of these begin
-    const int half = a.rotary / 2;
-    int from[2], pair[2], other[2];
-    bool turned[2], first[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        from[s] = 64 * s + 8 * u;
-        turned[s] = PAIR == kSameLane || from[s] < a.rotary;
-        first[s] = PAIR == kSameLane ? s == 0 : from[s] < half;
-        pair[s] = PAIR == kNeighbour ? from[s] / 2 : first[s] ? from[s] : from[s] - half;
-        other[s] = !turned[s] ? from[s] : first[s] ? from[s] + half : from[s] - half;
-    }
     // Channel e of run s: its pair's cosine and sine (with the sign that its part takes); what is not turned is multiplied with one and added to minus zero, which changes nothing.
-    auto turn_of = [&](int s, int e) {
-        Turn t;
-        if (PAIR == kNeighbour) {
-            t = wheel[(pair[s] + e / 2) & 63];
-            t.s = e & 1 ? t.s : -t.s;
-        } else {
-            t = wheel[(pair[s] + e) & 63];
-            t.s = first[s] ? -t.s : t.s;
-        }
-        if (!turned[s]) t.c = 1, t.s = -(Real)0;
+    auto turn_of = [&](auto *wheels, int s, int e) {
+        const int j = (pair[s] + (PAIR == kNeighbour ? e / 2 : e)) & 63;
+        auto t = wheels[spread(j)];
+        if (PAIR == kNeighbour ? !(e & 1) : first[s]) t.s = -t.s;
+        if (!turned[s]) t.c = 1, t.s = -(t.c * 0);
         return t;
     };
-    auto weights = [&](const unsigned char *w, int at, float (&f)[8]) {
-        if (!w) {
+    // The other channels of the pairs of run s (where it is turned), of states or weights.
+    auto other_channels = [&](const Head &h, int s, float (&p)[8]) {
+        if (PAIR == kSameLane) {
+            h.x[1 - s].get(p);
+        } else if (PAIR == kElsewhere) {
+            h.p[s].get(p);
+        } else {
+            float x[8];
+            h.x[s].get(x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = 1.f;
-            return;
-        }
-        Eight<DT> x;
-        x.load(w + at * ES);
-        x.get(f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] += a.offset;
-    };
-    // the weights of the lane's channels and of the others of their pairs
-    auto weights_of = [&](const unsigned char *w, float (&own)[2][8], float (&others)[2][8]) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) weights(w, from[s], own[s]);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (PAIR == kElsewhere) weights(w, other[s], others[s]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (PAIR == kSameLane) others[s][e] = own[1 - s][e];
-                if (PAIR == kNeighbour) others[s][e] = own[s][e ^ 1];
-            }
-        }
-    };
-    // A head's channels, and the others of their pairs (zeros where nothing is turned: an infinity there would not stay out).
-    struct Head {
-        Eight<DT> x[2], p[2];
-    };
-    auto fetch = [&](Head &h, const unsigned char *at) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            h.x[s].load(at + from[s] * ES);
-            if (PAIR == kElsewhere) h.p[s].load(at + other[s] * ES);
-        }
-    };
-    auto values = [&](const Head &h, float (&x)[2][8], float (&p)[2][8]) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) h.x[s].get(x[s]);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (PAIR == kElsewhere) h.p[s].get(p[s]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (PAIR == kSameLane) p[s][e] = x[1 - s][e];
-                if (PAIR == kNeighbour) p[s][e] = x[s][e ^ 1];
-                if (PAIR != kSameLane) p[s][e] = turned[s] ? p[s][e] : 0.f;
-            }
+            for (int e = 0; e < 8; ++e) p[e] = x[e ^ 1];
         }
     };
     // 1 / sqrt(mean + eps) of a head, the same for its eight lanes
@@ -209,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
             for (int e = 0; e < 8; ++e) sum = fmaf(x[s][e], x[s][e], sum);
 #pragma unroll
         for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
-        return 1.f / sqrtf(sum * (1.f / ILRE_HEAD_DIM) + (float)a.eps);
+        return rsqrtf(sum * (1.f / ILRE_HEAD_DIM) + (float)a.eps);
     };
     auto norm64 = [&](const float (&x)[2][8]) {
         double sum = 0.0;
@@ -221,43 +234,48 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
         for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
         return 1.0 / sqrt(sum * (1.0 / ILRE_HEAD_DIM) + a.eps);
     };
-    // fp32: coefficients of the token's heads, and a head from its place to another
+    // fp32: coefficients of the token's heads, and a head turned
     float A[2][8], B[2][8];
-    auto coefficients = [&](const unsigned char *w) {
-        float own[2][8], others[2][8];
-        weights_of(w, own, others);
+    auto coefficients = [&](bool norm, const unsigned char *w) {
+        const bool there = norm && w;
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s) {
+            float own[8], others[8];
+            weight.x[s].get(own);
+            other_channels(weight, s, others);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const Turn t = turn_of(s, e);
-                A[s][e] = own[s][e] * (float)t.c;
-                B[s][e] = turned[s] ? others[s][e] * (float)t.s : -0.f;
+                const Turn t = turn_of(wheel, s, e);
+                A[s][e] = (there ? own[e] + a.offset : 1.f) * t.c;
+                B[s][e] = turned[s] ? (there ? others[e] + a.offset : 1.f) * t.s : -0.f;
             }
+        }
     };
     auto turn32 = [&](Head &h, bool norm) {
         float x[2][8], p[2][8];
-        values(h, x, p);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            h.x[s].get(x[s]);
+            other_channels(h, s, p[s]);
+        }
         const float r = norm ? norm32(x) : 1.f;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[s][e] = fmaf(x[s][e], A[s][e], p[s][e] * B[s][e]) * r;
+            for (int e = 0; e < 8; ++e) {
+                const float q = turned[s] ? p[s][e] : 0.f;  // (an infinity where nothing is turned would not stay out)
+                x[s][e] = fmaf(x[s][e], A[s][e], q * B[s][e]) * r;
+            }
             h.x[s].put(x[s]);
         }
     };
 
-    // queries eight heads at a time, then keys and values as one list of heads
-    const int nq = a.q ? a.Hq : 0, nk = a.k ? a.Hkv : 0, nv = a.v ? a.Hkv : 0;
-    const int steps_q = (nq + 7) / 8, steps = steps_q + (nk + nv + 7) / 8;
-    int step = wave % WPT;
-    if (step < steps_q) coefficients(a.q_norm ? a.q_weight : nullptr);
+    if (queries) coefficients(a.q_norm, a.q_weight);
     for (; step < steps_q; step += WPT) {
-        const int h = step * 8 + slot;
-        const int at = min(h, nq - 1);
-        Head x;
-        fetch(x, a.q + (int64_t)token * a.q_token + at * a.q_head);
+        Head x = head;
+        fetch_step(head, step + WPT);
         turn32(x, a.q_norm);
+        const int h = step * 8 + slot;
         if (h < nq) {
             unsigned char *to = a.q_out + (int64_t)token * a.out_token + h * a.out_head;
 #pragma unroll
@@ -265,13 +283,13 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
         }
     }
     if (step >= steps || cell < 0) return;
-    const unsigned char *kw = a.k_norm ? a.k_weight : nullptr;
-    if (FMT == kPlain) coefficients(kw);
+    if (queries) fetch_weights(a.k_norm, a.k_weight);
+    if (FMT == kPlain) coefficients(a.k_norm, a.k_weight);
     for (; step < steps; step += WPT) {
-        const int h = (step - steps_q) * 8 + slot, at = min(h, nk + nv - 1);
-        const bool key = at < nk;
-        Head x;
-        fetch(x, key ? a.k + (int64_t)token * a.k_token + at * a.k_head : a.v + (int64_t)token * a.v_token + (at - nk) * a.v_head);
+        const int h = (step - steps_q) * 8 + slot;
+        const bool key = h < nk;
+        Head x = head;
+        fetch_step(head, step + WPT);
         const int64_t to = cell + (key ? h : h - nk) * a.head;
         if (FMT == kPlain) {
             Head y = x;
@@ -279,47 +297,70 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
             if (h < nk + nv) {
                 unsigned char *p = (key ? a.k_pages : a.v_pages) + to * ES;
 #pragma unroll
-                for (int s = 0; s < 2; ++s) (key ? y.x[s] : x.x[s]).store(p + from[s] * ES);
+                for (int s = 0; s < 2; ++s) {
+                    y.x[s].choose(key, x.x[s]);
+                    y.x[s].store(p + from[s] * ES);
+                }
             }
             continue;
         }
-        float f[2][8], p[2][8];
-        values(x, f, p);
-        if (__ballot(key)) {
-            const double r = a.k_norm ? norm64(f) : 1.0;
-            float own[2][8], others[2][8];
-            weights_of(kw, own, others);
-            float y[2][8];
+        const bool keys = __ballot(key);
+        double r = 1.0;
+        if (keys && a.k_norm) {
+            float f[2][8];
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s) x.x[s].get(f[s]);
+            r = norm64(f);
+        }
+        auto run = [&](auto number) {  // eight channels
+            constexpr int s = number.value;
+            float f[8];
+            x.x[s].get(f);
+            if (keys) {
+                float p[8], own[8], others[8];
+                other_channels(x, s, p);
+                weight.x[s].get(own);
+                other_channels(weight, s, others);
+                const bool there = a.k_norm && a.k_weight;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const Turn t = turn_of(s, e);
-                    y[s][e] = cut_off(((double)f[s][e] * own[s][e] * t.c + (double)p[s][e] * others[s][e] * t.s) * r);
+                    const KeyTurn t = turn_of(key_wheel, s, e);
+                    const float w = there ? own[e] + a.offset : 1.f, v = there ? others[e] + a.offset : 1.f, q = turned[s] ? p[e] : 0.f;
+                    const float y = cut_off(((double)f[e] * w * t.c + (double)q * v * t.s) * r);
+                    f[e] = key ? y : f[e];
                 }
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[s][e] = key ? y[s][e] : f[s][e];
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
+            }
             unsigned top = 0;  // the largest magnitude, as bits: a NaN's are larger than any number's
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[s][e]) & 0x7FFFFFFFu);
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
             top = max(top, (unsigned)__shfl_xor((int)top, 1));
             top = max(top, (unsigned)__shfl_xor((int)top, 2));
             const unsigned byte = scale_byte<FMT == kPlain ? ILRE_KV_FP8 : FMT>(__uint_as_float(top));
             const float inv = inverse_scale(byte);
             const int64_t channel = to + from[s];
-            if (h >= nk + nv) continue;
+            if (h >= nk + nv) return;
             unsigned char *codes = (key ? a.k_pages : a.v_pages) + (FMT == ILRE_KV_FP8 ? channel : channel / 2);
             if (FMT == ILRE_KV_FP8)
-                *(uint2 *)codes = byte == 255 ? make_uint2(0, 0) : to_fp8(f[s], inv);
+                *(uint2 *)codes = byte == 255 ? make_uint2(0, 0) : to_fp8(f, inv);
             else
-                *(unsigned *)codes = byte == 255 ? 0 : to_fp4(f[s], inv);
+                *(unsigned *)codes = byte == 255 ? 0 : to_fp4(f, inv);
             if ((u & 3) == 0) (key ? a.k_scales : a.v_scales)[channel / ILRE_KV_BLOCK] = (unsigned char)byte;
-        }
+        };
+        // (both at once, or numbers in fp64 and sines and cosines kept from one for the other, would take registers that a fourth wavefront can have)
+        auto forget = [&]() {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                x.x[s].forget();
+                weight.x[s].forget();
+                if (PAIR == kElsewhere) x.p[s].forget(), weight.p[s].forget();
+            }
+            asm volatile("" : "+v"(pair[1]));
+        };
+        forget();
+        run(std::integral_constant<int, 0>{});
+        forget();
+        run(std::integral_constant<int, 1>{});
     }
 }
 
@@ -358,16 +399,16 @@ __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int ro
 {
     constexpr int ES = DT == ILRE_BF16 ? 2 : 4;
     const int lane = threadIdx.x & 63, u = lane & 7;
-    const int64_t items = (int64_t)a.T * a.Hkv, first = (int64_t)blockIdx.x * (kThreads / 8 * kItems) + (threadIdx.x >> 6) * (8 * kItems) + (lane >> 3);
+    const unsigned items = (unsigned)a.T * a.Hkv, first = blockIdx.x * (kThreads / 8 * kItems) + (threadIdx.x >> 6) * (8 * kItems) + (lane >> 3);  // (2^30 at most)
     int row[kItems], head[kItems];
     bool real[kItems];
     int64_t cell[kItems];  // -1: zeros
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {  // rows or heads running fastest
-        const int64_t item = min(first + 8 * k, items - 1);
+        const unsigned item = min(first + 8 * k, items - 1), by = rows_first ? a.T : a.Hkv, quotient = item / by, rest = item - quotient * by;
         real[k] = first + 8 * k < items;
-        row[k] = (int)(rows_first ? item % a.T : item / a.Hkv);
-        head[k] = (int)(rows_first ? item / a.T : item % a.Hkv);
+        row[k] = (int)(rows_first ? rest : quotient);
+        head[k] = (int)(rows_first ? quotient : rest);
     }
     // the rows' sequences: the wavefront looks for its lowest row's, the others look on from there
     int lowest = __builtin_amdgcn_readfirstlane(row[0]), begin = a.n_seq;
