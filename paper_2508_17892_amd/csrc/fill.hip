@@ -391,28 +391,29 @@ hipError_t launch_format(const FillArgs &a, int format, int pairing, hipStream_t
 
 // ------------------------------------------------------------------------------------------------ reading a cache back
 
-// Rows (token, head) with eight lanes each, which have the channels that they have above; kItems rows a lane, whose loads are under way together.  One pass, HBM.
-constexpr int kItems = 4;
-
-template <int DT, int FMT>
+// Rows (token, head) with eight lanes each, which have the channels that they have above; ITEMS rows a lane, whose loads are under way together.  One pass, HBM.
+template <int DT, int FMT, int ITEMS>
 __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int rows_first)
 {
     constexpr int ES = DT == ILRE_BF16 ? 2 : 4;
     const int lane = threadIdx.x & 63, u = lane & 7;
-    const unsigned items = (unsigned)a.T * a.Hkv, first = blockIdx.x * (kThreads / 8 * kItems) + (threadIdx.x >> 6) * (8 * kItems) + (lane >> 3);  // (2^30 at most)
-    int row[kItems], head[kItems];
-    bool real[kItems];
-    int64_t cell[kItems];  // -1: zeros
+    const unsigned items = (unsigned)a.T * a.Hkv, first = blockIdx.x * (kThreads / 8 * ITEMS) + (threadIdx.x >> 6) * (8 * ITEMS) + (lane >> 3);  // (2^30 at most)
+    int row[ITEMS], head[ITEMS];
+    bool real[ITEMS];
+    int64_t cell[ITEMS];  // -1: zeros
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {  // rows or heads running fastest
+    for (int k = 0; k < ITEMS; ++k) {  // rows or heads running fastest
         const unsigned item = min(first + 8 * k, items - 1), by = rows_first ? a.T : a.Hkv, quotient = item / by, rest = item - quotient * by;
         real[k] = first + 8 * k < items;
         row[k] = (int)(rows_first ? rest : quotient);
         head[k] = (int)(rows_first ? quotient : rest);
     }
-    // the rows' sequences: the wavefront looks for its lowest row's, the others look on from there
-    int lowest = __builtin_amdgcn_readfirstlane(row[0]), begin = a.n_seq;
-    if (__ballot(row[0] < lowest || row[1] < lowest || row[2] < lowest || row[3] < lowest)) lowest = 0;  // on to the next head's rows
+    int token[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) token[k] = a.tokens ? a.tokens[row[k]] : 0;
+    // The rows' sequences: the wavefront looks for its first row's; the others look on from there, or from the beginning where the next head's rows begin.
+    const int lowest = __builtin_amdgcn_readfirstlane(row[0]);
+    int begin = a.n_seq;
     for (int base = 0; base < a.n_seq; base += 64) {
         const int s = base + lane;
         const unsigned long long past = __ballot(s < a.n_seq && a.cu_q[s + 1] > lowest);
@@ -421,17 +422,18 @@ __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int ro
             break;
         }
     }
-    static_assert(kItems == 4, "the rows named above");
+    int seq = begin, seen = lowest;
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        int seq = begin;
+    for (int k = 0; k < ITEMS; ++k) {
+        if (row[k] < seen) seq = 0;
+        seen = row[k];
         while (seq < a.n_seq && a.cu_q[seq + 1] <= row[k]) ++seq;
         cell[k] = -1;
         const int r0 = seq < a.n_seq ? max(a.cu_q[seq], 0) : 0x7FFFFFFF;
         real[k] = real[k] && row[k] >= r0;  // otherwise a row of no sequence
         if (!real[k]) continue;
         const int r1 = min(a.cu_q[seq + 1], a.T), len = a.kv_len[seq];
-        const int64_t at = a.tokens ? (int64_t)a.tokens[row[k]] : (int64_t)len - (r1 - r0) + (row[k] - r0);
+        const int64_t at = a.tokens ? (int64_t)token[k] : (int64_t)len - (r1 - r0) + (row[k] - r0);
         if (at < 0 || at >= min((int64_t)len, a.kv_limit)) continue;
         const int page = a.table[seq * a.table_stride + (at >> a.page_shift)];
         if ((unsigned)page < (unsigned)a.num_pages) cell[k] = page * a.page + (at & (((int64_t)1 << a.page_shift) - 1)) * a.token + head[k] * a.head;
@@ -484,33 +486,40 @@ __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int ro
         if (!out) continue;
         const unsigned char *pages = t ? a.v_pages : a.k_pages, *scales = t ? a.v_scales : a.k_scales;
         const int64_t out_token = t ? a.v_token : a.k_token, out_head = t ? a.v_head : a.k_head;
-        Run r[kItems][2];
+        Run r[ITEMS][2];
 #pragma unroll
-        for (int k = 0; k < kItems; ++k)
+        for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
             for (int s = 0; s < 2; ++s) fetch(r[k][s], pages, scales, cell[k] < 0 ? -1 : cell[k] + 64 * s + 8 * u);
 #pragma unroll
-        for (int k = 0; k < kItems; ++k)
+        for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
                 if (real[k]) store(r[k][s], out + row[k] * out_token + head[k] * out_head + (64 * s + 8 * u) * ES);
     }
 }
 
+template <int DT, int FMT>
+hipError_t launch_read_items(const ReadArgs &a, hipStream_t s)
+{
+    const int64_t items = (int64_t)a.T * a.Hkv;
+    const int rows_first = a.k_out ? a.k_token < a.k_head : a.v_token < a.v_head;
+    const int64_t each = kThreads / 8;
+    // Four rows a lane where there are many, one where what counts is how soon the first arrive (8 kv heads: 4100 tokens 10.4 -> 8.0 us with one, 16000 25.0 -> 24.4, 131072 158 -> 162, a
+    // million's keys 606 -> 854).
+    if (items <= 1 << 18)
+        hipLaunchKernelGGL((read_kernel<DT, FMT, 1>), dim3((unsigned)((items + each - 1) / each)), dim3(kThreads), 0, s, a, rows_first);
+    else
+        hipLaunchKernelGGL((read_kernel<DT, FMT, 4>), dim3((unsigned)((items + 4 * each - 1) / (4 * each))), dim3(kThreads), 0, s, a, rows_first);
+    return hipGetLastError();
+}
+
 template <int DT>
 hipError_t launch_read_format(const ReadArgs &a, int format, hipStream_t s)
 {
-    const int64_t items = (int64_t)a.T * a.Hkv;
-    const int64_t each = kThreads / 8 * kItems;
-    const dim3 grid((unsigned)((items + each - 1) / each));
-    const int rows_first = a.k_out ? a.k_token < a.k_head : a.v_token < a.v_head;
-    if (format == ILRE_KV_FP8)
-        hipLaunchKernelGGL((read_kernel<DT, ILRE_KV_FP8>), grid, dim3(kThreads), 0, s, a, rows_first);
-    else if (format == ILRE_KV_FP4)
-        hipLaunchKernelGGL((read_kernel<DT, ILRE_KV_FP4>), grid, dim3(kThreads), 0, s, a, rows_first);
-    else
-        hipLaunchKernelGGL((read_kernel<DT, kPlain>), grid, dim3(kThreads), 0, s, a, rows_first);
-    return hipGetLastError();
+    return format == ILRE_KV_FP8   ? launch_read_items<DT, ILRE_KV_FP8>(a, s)
+           : format == ILRE_KV_FP4 ? launch_read_items<DT, ILRE_KV_FP4>(a, s)
+                                   : launch_read_items<DT, kPlain>(a, s);
 }
 
 }  // namespace
