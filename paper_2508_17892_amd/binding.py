@@ -497,6 +497,12 @@ def _attn_ref(causal: int, sink: int, window: int, max_q: int, max_kv: int, tota
     return ctypes.byref(IlreAttn(ctypes.sizeof(IlreAttn), causal, sink, window, max_q, max_kv, total_kv))
 
 
+@functools.lru_cache(maxsize=4096)
+def _call_opts_ref(dtype: int, scale: float, workspace: int, workspace_bytes: int, stream: int):
+    """An ilre_opts of the operators around a recall to pass on (the library only reads it)."""
+    return ctypes.byref(IlreOpts(_OPTS_SIZE, dtype, 0, ILRE_SCORE_SUM, scale, 0, 0, 0, 0, 0, workspace, workspace_bytes, stream, 0, 0))
+
+
 def _like(name: str, out: Optional[torch.Tensor], ref: torch.Tensor):
     """(out, its token stride, its head stride): a new tensor, or the caller's of the same shape and element type."""
     if out is None:
@@ -651,12 +657,14 @@ def _turn_arguments(freqs: Optional[IlreRopeFreqs], positions: Optional[torch.Te
     return positions.data_ptr(), positions.shape[0], _axes_array(tuple(axes)), ctypes.byref(freqs)
 
 
-def _same_device(*tensors: Optional[torch.Tensor]) -> None:
-    """The library works on the current device: a tensor of another one would be reached over the link, or not at all, on a stream that does not wait for it."""
+def _stream_of(*tensors: Optional[torch.Tensor]) -> int:
+    """The current stream of the current device, on which the library works: a tensor of another device would be reached over the link, or not at all, on a stream that does not wait
+    for it, and is refused."""
     here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.get_device() not in (here, -1):
+        if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor on device {t.get_device()}, the current device is {here}")
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
 def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], cache: PagedKV, freqs: IlreRopeFreqs,
@@ -711,10 +719,9 @@ def ilre_norm_rope(x: torch.Tensor, freqs: Optional[IlreRopeFreqs], positions: O
     pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return out
-    _same_device(x, out, positions)
-    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(x, out, positions))
     _check(load().ilre_norm_rope(x.data_ptr(), out.data_ptr(), T, H, d, pos, n_axes, ax, int(first_position), fr, int(pairing),
-                                 None if norms is None else norms._ref, _strides_ref(x0, x1, o0, o1), ctypes.byref(o)))
+                                 None if norms is None else norms._ref, _strides_ref(x0, x1, o0, o1), o))
     return out
 
 
@@ -729,11 +736,10 @@ def ilre_norm_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optiona
     pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return q_out
-    _same_device(q, k, v, q_out, positions, cache.k_pages)
-    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(q, k, v, q_out, positions, cache.k_pages))
     _check(load().ilre_norm_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
                                         None if v is None else v.data_ptr(), T, Hq, d, pos, n_axes, ax, fr, int(pairing),
-                                        None if norms is None else norms._ref, cache._ref, st, ctypes.byref(o)))
+                                        None if norms is None else norms._ref, cache._ref, st, o))
     return q_out
 
 
@@ -765,10 +771,9 @@ def ilre_cache_read(cache: PagedKV, T: int, tokens: Optional[torch.Tensor] = Non
     if T == 0:
         return k_out, v_out
     at = None if tokens is None else _int32_vector("tokens", tokens, T)
-    _same_device(k_out, v_out, tokens, cache.k_pages)
-    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(k_out, v_out, tokens, cache.k_pages))
     _check(load().ilre_cache_read(None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(), T, 128, at,
-                                  cache._ref, _strides_ref(0, 0, 0, 0, k0, k1, v0, v1), ctypes.byref(o)))
+                                  cache._ref, _strides_ref(0, 0, 0, 0, k0, k1, v0, v1), o))
     return k_out, v_out
 
 
@@ -813,8 +818,8 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
         raise ValueError("workspace is a contiguous device tensor")
     at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
     st = _strides_ref(q0, q1, o0, o1)
-    o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
-    _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, at, cache._ref, st, ctypes.byref(o)))
+    o = _call_opts_ref(dt, float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _current_stream())
+    _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, at, cache._ref, st, o))
     return out, lse
 
 
@@ -842,10 +847,9 @@ def ilre_tree_attention(q: torch.Tensor, cache: PagedKV, tree: torch.Tensor, *, 
     elif not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace is a contiguous device tensor")
     at = _attn_ref(0, 0, 0, int(max_q), int(max_kv), int(total_kv))
-    _same_device(q, tree, out, lse, workspace, cache.k_pages)
-    o = _opts(dt, 0, scale, ILRE_SCORE_SUM, workspace)
+    o = _call_opts_ref(dt, float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(q, tree, out, lse, workspace, cache.k_pages))
     _check(load().ilre_tree_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, tree.data_ptr(), words, row, at, cache._ref,
-                                      _strides_ref(q0, q1, o0, o1), ctypes.byref(o)))
+                                      _strides_ref(q0, q1, o0, o1), o))
     return out, lse
 
 
