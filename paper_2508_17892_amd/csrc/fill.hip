@@ -82,8 +82,9 @@ struct Eight {  // channels, as they lie in memory
 __device__ __forceinline__ int spread(int j) { return j + (j >> 3); }
 
 template <int DT, int FMT, int PAIR, int WPT>
-__global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
+__global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(const FillArgs a)
 {
+    constexpr int WAVES = WPT > 4 ? WPT : kThreads / 64;
     using Real = std::conditional_t<FMT == kPlain, float, double>;  // of keys
     struct Turn {
         float c, s;  // cosine and sine, times the magnitude
@@ -92,10 +93,10 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
         Real c, s;
     };
     constexpr int ES = DT == ILRE_BF16 ? 2 : 4;
-    __shared__ Turn wheels[kThreads / 64][ILRE_HEAD_DIM / 2 + 8];
-    __shared__ KeyTurn key_wheels[FMT == kPlain ? 1 : kThreads / 64][FMT == kPlain ? 1 : ILRE_HEAD_DIM / 2 + 8];
+    __shared__ Turn wheels[WAVES][ILRE_HEAD_DIM / 2 + 8];
+    __shared__ KeyTurn key_wheels[FMT == kPlain ? 1 : WAVES][FMT == kPlain ? 1 : ILRE_HEAD_DIM / 2 + 8];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    const int token = (int)blockIdx.x * (kThreads / 64 / WPT) + wave / WPT;
+    const int token = (int)blockIdx.x * (WAVES / WPT) + wave / WPT;
     if (token >= a.T) return;
     const int u = lane & 7, slot = lane >> 3;
     Turn *wheel = wheels[wave];
@@ -367,7 +368,11 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(const FillArgs a)
 template <int DT, int FMT, int PAIR>
 hipError_t launch(const FillArgs &a, hipStream_t s)
 {
-    if (a.T < 4096)
+    // A token's heads go to several wavefronts while there are not tokens for all of them: eight up to 512 tokens (32/8 heads, 8 bits; a step of 8 heads each: 8 tokens 6.4 -> 5.4 us, 512 8.5 -> 7.9,
+    // but 1028 12.2 -> 15.8), four up to a few thousand; many tokens have one each, so that sines and weights are worked out once.
+    if (a.T <= 512)
+        hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 8>), dim3((unsigned)a.T), dim3(512), 0, s, a);
+    else if (a.T < 4096)
         hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 4>), dim3((unsigned)a.T), dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 1>), dim3((unsigned)((a.T + 3) / 4)), dim3(kThreads), 0, s, a);
