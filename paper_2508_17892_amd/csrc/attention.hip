@@ -13,11 +13,14 @@ namespace ilre {
 //     11.7; 30000 tokens, 8/2 heads: 17.7 and 15.7).  More rows: 12 tiles of 64 tokens at least, and 4 while the merge has little to do (32/8 heads, 4096 tokens: 16
 //     new ones 18.4 us with 4, 25.2 with 12, 64 29.7 and 35.7, 200 51.9 and 40.3), 2 of 32 in fp32 (prompts of 77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6,
 //     6 74).
+//   - Trees, and more than 16 rows over a quantised cache: a range leaves 32 rows behind for the merge, a quarter to half of what a tile of 128 tokens is. A range a compute unit, two from twelve tiles each
+//     on, and whole where that is a merge's worth longer at most (8 drafted tokens, 32/8 heads: contexts of 4105, 9009, 7 and 300 26.1 -> 20.8 us, eight of 3000 28.3 -> 26.9, one of 30000 33.9 -> 31.7,
+//     sixteen of 900 22.0 -> 19.8; in 8 bits 24.3 -> 18.8, 22.1 -> 20.4, 23.3 -> 21.7, 20.2 -> 16.8).
 //   - Up to 16 rows over a quantised cache (tiles of 128 tokens): a workgroup a compute unit reads nearly as fast as HBM gives (32 requests of 1500 tokens, 8 kv heads 24.9 us whole, 25.5 in two),
 //     so that lists stay whole where the longest has no more tiles than a compute unit's share of all and what a merge costs, four, or five at most (128 requests of 1000 tokens: whole 56 us, in two
 //     63; one of 640: whole 9.4, single tiles 10.5; four of 1000: single tiles 10.7, whole 13.6). What is cut makes two ranges a compute unit (48 requests of 1 to 16384 tokens, 4 kv heads:
 //     ranges of 12 tiles 47.0 us, 10 53.0, 7 50.3; 65536 tokens, 8 kv heads: 8 33.7, 6 36.3; 262144: 32 102.7, 22 106.8).
-AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
+AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
 {
     AttnPlan p{};
     p.dtype = dtype;
@@ -50,7 +53,10 @@ AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv
     const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
     const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
     int64_t per = std::max<int64_t>((work + places - 1) / places, least);
-    if (p.rows == 16) {
+    if (p.rows == 32 && dtype == ILRE_BF16 && (format != kPlain || tree)) {
+        per = work / (2 * kNumCU) >= 12 ? per : std::max<int64_t>((work + kNumCU - 1) / kNumCU, work <= kNumCU ? 1 : 2);
+        if (most <= (work < kNumCU ? 3 : work / kNumCU + 4)) per = most;
+    } else if (p.rows == 16) {
         const int64_t lists = blocks * Hkv, mean = tiles(total_kv / n_seq);
         auto units = [&](int64_t x) { return most == mean ? lists * ((most + x - 1) / x) : lists * (2 * mean + x) / (2 * x); };  // lists of unlike lengths end with half a range each
         per = std::max<int64_t>(work <= kNumCU ? 1 : 2, work / (2 * kNumCU));

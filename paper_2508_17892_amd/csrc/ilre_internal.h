@@ -306,11 +306,11 @@ struct AttnPlan {
 // Most workgroups of a launch (a dimension counts threads in 32 bits, and no workgroup here has more than 512).
 constexpr int64_t kMaxUnits = (int64_t)1 << 22;
 
-AttnPlan make_attn_plan(int dtype, int format, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
-// The same for a cache of the states' own type.
+AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
+// The same for a cache of the states' own type and no tree.
 inline AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
 {
-    return make_attn_plan(dtype, kPlain, T, n_seq, Hq, Hkv, max_q, max_kv, total_kv, sink, window, workspace);
+    return make_attn_plan(dtype, kPlain, false, T, n_seq, Hq, Hkv, max_q, max_kv, total_kv, sink, window, workspace);
 }
 hipError_t launch_attention(const AttnPlan &p, AttnArgs a, int format, void *workspace, hipStream_t s);
 // The kernels by kind of call; `a` has its plan already.
