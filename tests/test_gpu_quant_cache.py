@@ -65,13 +65,22 @@ class Quant(Paged):
 
 # ------------------------------------------------------------------------------------------------ attention over a quantised cache
 
-@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
-@pytest.mark.parametrize("q_lens,kv_lens,Hq,Hkv,page,layout,dtype,mask", CASES + [
+ATTENTION = CASES + [
     ([300], [900], 64, 8, 16, "head", "bf16", {}),                             # 256 rows a workgroup
     ([1024, 700], [3000, 700], 32, 8, 64, "head", "bf16", {}),
     ([600], [600], 64, 8, 32, "token", "bf16", dict(sink=4, window=200)),
     ([1], [70001], 8, 1, 64, "head", "bf16", {}),
-])
+    ([7, 5], [3000, 900], 8, 2, 16, "head", "bf16", {}),                       # 32 rows
+    ([7], [3000], 8, 2, 64, "token", "bf16", dict(sink=4, window=700)),
+    ([2100], [2100], 32, 8, 64, "head", "bf16", dict(sink=4, window=128)),     # 256 rows, whole
+    ([2, 3], [60, 40], 8, 2, 16, "head", "f32", {}),
+    ([3], [900], 8, 2, 32, "head", "f32", dict(sink=4, window=100)),
+    ([40], [40], 8, 2, 16, "head", "f32", {}),
+]
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("q_lens,kv_lens,Hq,Hkv,page,layout,dtype,mask", ATTENTION)
 def test_attention(fmt, q_lens, kv_lens, Hq, Hkv, page, layout, dtype, mask):
     _announce(f"quantised {fmt} {q_lens} of {kv_lens} {Hq}/{Hkv} page {page} {layout} {dtype} {mask}")
     x = Quant(fmt, q_lens, kv_lens, Hq, Hkv, page, dtype, layout, seed=sum(kv_lens) + Hq)
@@ -213,6 +222,11 @@ TREES = [
     ([12, 6], [5, 2], 8, 2, 16, "head", "bf16"),             # more drafted tokens than the cache holds
     ([8, 3], [500, 3], 8, 2, 32, "head", "f32"),
     ([60], [300], 8, 2, 16, "token", "f32"),
+    ([20], [3000], 8, 2, 16, "head", "bf16"),                # 128 rows, cut
+    ([64] * 32, [80] * 32, 32, 8, 16, "head", "bf16"),       # 256 rows, whole
+    ([4, 3], [3000, 700], 8, 2, 16, "head", "bf16"),         # 16 rows
+    ([2], [30], 8, 2, 16, "head", "f32"),
+    ([20], [30], 8, 2, 16, "head", "f32"),
 ]
 
 
@@ -641,3 +655,57 @@ def test_another_device_is_refused():
         il.ilre_tree_attention(q, x.cache(), _i32(1)[None], max_q=1, max_kv=5)
     with pytest.raises(il.IlreError):
         il.ilre_tree_attention(x.dev["q"], x.cache(), _i32(1)[None], max_q=33, max_kv=5)
+
+
+def test_a_request_over_a_quantised_cache():
+    """Chunks of a context are normed, turned along three axes, stored in 8 bits and attended to; the keys are read back for the recall, the kept tokens stored in 4 bits, and a draft attends
+    to them: every stage against the oracle on what the stage before should have left."""
+    _announce("a request, every operator")
+    L, HQ, HKV, P = 620, 8, 2, 16
+    g = torch.Generator().manual_seed(31)
+    states = torch.randn(L, HQ + 2 * HKV, 128, generator=g).bfloat16()
+    qw, kw = _weights("bf16", 31, 0)
+    f = il.ilre_rope_frequencies(128, 500000.0)
+    pos = np.stack((np.arange(L), np.arange(L) // 7, np.arange(L) % 7))
+    pages = -(-L // P)
+    blank = lambda width: torch.full((pages + 1, HKV, P, width), 255, dtype=torch.uint8, device="cuda")  # noqa: E731
+    kp, vp, ks, vs = blank(128).view(torch.float8_e4m3fn), blank(128).view(torch.float8_e4m3fn), blank(4), blank(4)
+    table = torch.randperm(pages + 1, generator=g)[:pages].int().cuda()[None]
+    kv_len, cu = _i32(0), _i32(0, 0)
+    cache = il.QuantKV(kp, vp, ks, vs, table, kv_len, cu)
+    norms = il.HeadNorms(qw.cuda(), kw.cuda())
+    dev = states.cuda()
+    want_k = oq.read(*oq.store(_turned(states[:, HQ:HQ + HKV], kw, pos, AXES3[64], f, "half", 0), "fp8"), "fp8")
+    want_v = oq.read(*oq.store(_f64(states[:, HQ + HKV:]), "fp8"), "fp8")
+    at = 0
+    for n in (204, 200, 200, 16):
+        s = dev[at:at + n]
+        kv_len.fill_(at + n)
+        cu[1] = n
+        q = il.ilre_norm_rope_append(s[:, :HQ], s[:, HQ:HQ + HKV], s[:, HQ + HKV:], cache, f, torch.from_numpy(pos[:, at:at + n].copy()).int().cuda(), norms=norms, axes=AXES3[64])
+        out, lse = il.ilre_paged_attention(q, cache, max_q=n, max_kv=at + n, sink=4, window=128)
+        _check(out, lse, *oa.attend(_f64(q), want_k[:at + n], want_v[:at + n], sink=4, window=128), at + n, "bf16", f"chunk at {at}")
+        at += n
+    # the last chunk's queries recall, over the keys as they come out of the cache
+    cu[1] = L
+    key_cache = torch.empty(HKV, L, 128, dtype=torch.bfloat16, device="cuda")
+    il.ilre_cache_read(cache, L, k_out=key_cache.transpose(0, 1))
+    assert np.array_equal(_f64(key_cache.transpose(0, 1)), want_k)
+    idx, _ = il.ilre_recall(q.transpose(0, 1), key_cache, 90, (1, 3, 7), sink=4)
+    assert len(idx) == 94
+    cu[1] = len(idx)
+    k, v = il.ilre_cache_read(cache, len(idx), idx)
+    kept = idx.cpu().numpy()
+    assert np.array_equal(_f64(k), want_k[kept]) and np.array_equal(_f64(v), want_v[kept])
+    # kept tokens and a draft of six in 4 bits (the keys are turned already)
+    n, m = 6, len(idx) + 6
+    k, v = torch.cat((k, dev[:n, HQ:HQ + HKV])), torch.cat((v, dev[:n, HQ + HKV:]))
+    code, scale = torch.zeros(8, HKV, P, 64, dtype=torch.uint8, device="cuda"), torch.zeros(8, HKV, P, 4, dtype=torch.uint8, device="cuda")
+    code2, scale2 = torch.zeros_like(code), torch.zeros_like(scale)
+    short = il.QuantKV(code, code2, scale, scale2, _i32(6, 1, 4, 2, 7, 0, 3)[None], _i32(m), _i32(0, m))
+    il.ilre_norm_rope_append(None, k, v, short, None)
+    short.cu_q[1] = n
+    words = _tree([n], 5)
+    out, lse = il.ilre_tree_attention(q[:n].contiguous(), short, _dev(words), max_q=n, max_kv=m)
+    k4, v4 = (oq.read(*oq.store(_f64(t), "fp4"), "fp4") for t in (k, v))
+    _check(out, lse, *oq.attend_seen(_f64(q[:n]), k4, v4, oq.tree_seen(words, n, m)), m, "bf16", "draft")
