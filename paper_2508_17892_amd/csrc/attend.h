@@ -1112,6 +1112,20 @@ __device__ __forceinline__ void piece_to_numbers(const u32x4 &w, float scale, u3
     }
 }
 
+// Workgroups go to the XCDs in turn.  With 4 bits the kv heads of a unit go to the same one: where a token's heads lie side by side, two heads' codes share a cache line, which then comes to one
+// L2 and not to two (a million tokens in that layout 369 -> 261 us, 48 requests 38.5 -> 31.2; with a layout by heads 197 either way).  8-bit codes fill their lines, and a kv head an XCD is the better
+// way (444 us, together 465; 48 requests 48.3 and 48.8).
+template <int FMT>
+__device__ __forceinline__ int head_of_block(const AttnArgs &a)
+{
+    return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD % a.Hkv : blockIdx.x % a.Hkv;
+}
+template <int FMT>
+__device__ __forceinline__ int unit_of_block(const AttnArgs &a)
+{
+    return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD / a.Hkv * kNumXCD + blockIdx.x % kNumXCD : blockIdx.x / a.Hkv;
+}
+
 template <int DT>
 constexpr size_t codes_lds(int waves)
 {
@@ -1129,10 +1143,10 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % a.Hkv;
+    const int head = head_of_block<FMT>(a);
     Block blk;
     int split;
-    if (!find_unit<true>(a, blockIdx.x / a.Hkv, 32, TN, blk, split)) return;
+    if (!find_unit<true>(a, unit_of_block<FMT>(a), 32, TN, blk, split)) return;
     Drafted drafted;
     if (TREE) {
         drafted.init(a, blk, blk.rows0 + l32);
@@ -1308,10 +1322,10 @@ __global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) vo
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g = lane >> 4;
-    const int head = blockIdx.x % a.Hkv;
+    const int head = head_of_block<FMT>(a);
     Block blk;
     int split;
-    if (!find_unit<true>(a, blockIdx.x / a.Hkv, 16, TN, blk, split)) return;
+    if (!find_unit<true>(a, unit_of_block<FMT>(a), 16, TN, blk, split)) return;
     Drafted drafted;
     if (TREE) {
         drafted.init(a, blk, blk.rows0 + l16);
@@ -1647,12 +1661,14 @@ hipError_t raise_lds_limit_once(const void *kernel)
     return e;
 }
 
+// units_step: the number of units is rounded up to a multiple of it.
 template <typename K>
-hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const AttnArgs &a, hipStream_t s)
+hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const AttnArgs &a, hipStream_t s, unsigned units_step = 1)
 {
     const hipError_t e = raise_lds_limit_once((const void *)kernel);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p.nsplit * p.nblocks * a.Hkv), dim3(threads), lds, s, a);
+    const unsigned units = ((unsigned)p.nsplit * p.nblocks + units_step - 1) / units_step * units_step;
+    hipLaunchKernelGGL(kernel, dim3(units * a.Hkv), dim3(threads), lds, s, a);
     return hipGetLastError();
 }
 
@@ -1665,7 +1681,7 @@ hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 template <int DT, int WAVES, bool PAGED, int FMT, bool TREE>
 hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    if constexpr (FMT != kPlain) return launch(attend_codes<DT, WAVES, FMT, TREE>, p, WAVES * 64, codes_lds<DT>(WAVES), a, s);
+    if constexpr (FMT != kPlain) return launch(attend_codes<DT, WAVES, FMT, TREE>, p, WAVES * 64, codes_lds<DT>(WAVES), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
     return launch(attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
@@ -1676,7 +1692,7 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
     if (p.dtype == ILRE_BF16) {
         if constexpr (FMT != kPlain) {
             if (p.rows == 16) {
-                e = launch(attend_codes16<FMT, 4, TREE>, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s);
+                e = launch(attend_codes16<FMT, 4, TREE>, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
                 return e != hipSuccess || p.nsplit == 1 ? e : launch_merge<ILRE_BF16, PAGED>(p, a, s);
             }
         }
