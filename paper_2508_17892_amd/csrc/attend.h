@@ -203,7 +203,7 @@ __device__ __forceinline__ void copy_offsets(int (&voff)[ROWS * ROWB / 1024], in
 
 // ------------------------------------------------------------------------------------------------ tiles of a quantised cache
 
-// Eight tokens of a kv head at a time: lane l has channels 16 (l % 8) .. + 15 of token l / 8, as codes in registers until they are written to LDS as numbers of the states' type,
+// Eight tokens of a kv head at a time: lane l has channels 16 (l % 8) .. + 15 of token l / 8, as codes in registers until they are written to LDS as bf16,
 // where copy_rows would have put them.  Tokens that no row of the block sees are zeros here too (codes and scales past the end of a buffer read as zero).
 template <int FMT>
 struct Codes {
@@ -265,62 +265,39 @@ __device__ __forceinline__ void lds_write16(unsigned at, const u32x4 &x) { *(__a
 
 // Eight tokens to rows first_row .. of a tile in LDS (first_row a multiple of 8).  Eight lanes, the pieces of one row, write together: so that they reach all banks, a lane's 16-byte
 // pieces go out in an order of its own, piece k ^ turn.
-template <int DT, int FMT, bool VALUES>
+template <bool VALUES>
 struct CodeRows {
-    static constexpr int ROWB = DT == ILRE_BF16 ? 256 : 512, N = ROWB / 128;  // N: 16-byte pieces a lane
-    unsigned to[N];
-    static __device__ __forceinline__ int turn(int lane) { return DT == ILRE_BF16 ? (lane & 7) >> 2 : FMT == ILRE_KV_FP8 ? (lane & 7) >> 1 : (lane & 7) >> 1 & 2; }
+    unsigned to[2];
+    static __device__ __forceinline__ int turn(int lane) { return (lane & 7) >> 2; }
     __device__ __forceinline__ void init(unsigned tile, int first_row, int lane)
     {
         const int r = first_row + (lane >> 3), u = lane & 7, swap = VALUES ? (r & 3) << 2 : r & 15;
 #pragma unroll
-        for (int k = 0; k < N; ++k) to[k] = tile + r * ROWB + (((N * u + (k ^ turn(lane))) ^ swap) * 16);
+        for (int k = 0; k < 2; ++k) to[k] = tile + r * 256 + (((2 * u + (k ^ turn(lane))) ^ swap) * 16);
     }
 };
 
 // `slot`: the tile's distance from the one that CodeRows was made for.
-template <int DT, int FMT, bool VALUES>
-__device__ __forceinline__ void write_codes(const Codes<FMT> &c, const CodeRows<DT, FMT, VALUES> &rows, unsigned slot, int lane)
+template <int FMT, bool VALUES>
+__device__ __forceinline__ void write_codes(const Codes<FMT> &c, const CodeRows<VALUES> &rows, unsigned slot, int lane)
 {
-    constexpr int N = CodeRows<DT, FMT, VALUES>::N, PER = FMT == ILRE_KV_FP8 ? 2 : 4;  // PER: pairs of channels a word
     const float scale = scale_of(c.scale);
-    const int turn = rows.turn(lane);
-    unsigned w[4] = {c.w[0], c.w[1], c.w[Codes<FMT>::W - 2], c.w[Codes<FMT>::W - 1]};
-    auto exchange = [](unsigned &p, unsigned &q, bool yes) {
-        const unsigned a = p, b = q;
-        p = yes ? b : a;
-        q = yes ? a : b;
-    };
-    if (FMT == ILRE_KV_FP4) {
-        exchange(w[0], w[1], turn != 0);
+    const bool turn = rows.turn(lane);
+    unsigned x[8];
+    if constexpr (FMT == ILRE_KV_FP8) {
+        const unsigned w[4] = {turn ? c.w[2] : c.w[0], turn ? c.w[3] : c.w[1], turn ? c.w[0] : c.w[2], turn ? c.w[1] : c.w[3]};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[2 * k] = bf16_pair<FMT, 0>(w[k], scale), x[2 * k + 1] = bf16_pair<FMT, 1>(w[k], scale);
     } else {
-        if (DT == ILRE_F32) {
-            exchange(w[0], w[1], turn & 1);
-            exchange(w[2], w[3], turn & 1);
-        }
-        exchange(w[0], w[2], DT == ILRE_F32 ? turn & 2 : turn);
-        exchange(w[1], w[3], DT == ILRE_F32 ? turn & 2 : turn);
-    }
-    unsigned x[16];
+        const unsigned w[2] = {turn ? c.w[1] : c.w[0], turn ? c.w[0] : c.w[1]};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {  // channels 2i, 2i + 1 of what is written
-        const unsigned word = w[i / PER];
-        if constexpr (DT == ILRE_BF16) {
-            x[i] = i % PER == 0   ? bf16_pair<FMT, 0>(word, scale)
-                   : i % PER == 1 ? bf16_pair<FMT, 1>(word, scale)
-                   : i % PER == 2 ? bf16_pair<FMT, PER == 4 ? 2 : 0>(word, scale)
-                                  : bf16_pair<FMT, PER == 4 ? 3 : 0>(word, scale);
-        } else {
-            const float2 f = i % PER == 0   ? f32_pair<FMT, 0>(word, scale)
-                             : i % PER == 1 ? f32_pair<FMT, 1>(word, scale)
-                             : i % PER == 2 ? f32_pair<FMT, PER == 4 ? 2 : 0>(word, scale)
-                                            : f32_pair<FMT, PER == 4 ? 3 : 0>(word, scale);
-            x[2 * i] = __float_as_uint(f.x);
-            x[2 * i + 1] = __float_as_uint(f.y);
+        for (int k = 0; k < 2; ++k) {
+            x[4 * k] = bf16_pair<FMT, 0>(w[k], scale), x[4 * k + 1] = bf16_pair<FMT, 1>(w[k], scale);
+            x[4 * k + 2] = bf16_pair<FMT, 2>(w[k], scale), x[4 * k + 3] = bf16_pair<FMT, 3>(w[k], scale);
         }
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) lds_write16(rows.to[k] + slot, u32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]});
+    for (int k = 0; k < 2; ++k) lds_write16(rows.to[k] + slot, u32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]});
 }
 
 // ------------------------------------------------------------------------------------------------ products
@@ -625,7 +602,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     constexpr int ROWB = E::ROWB, SLOT = TN * ROWB, GROUPS = WAVES / TS, ROWS = GROUPS * 32, SUB = TN / 32 / TS, RING = E::RING;
     constexpr int CROWS = TN / WAVES, COPIES = CROWS * ROWB / 1024;  // a wavefront's rows and copies of a tile
     static_assert(CROWS <= 16 && CROWS * ROWB % 1024 == 0 && TN % 32 == 0, "a wavefront's rows lie on one page");
-    static_assert(FMT == kPlain || (PAGED && CROWS == 8), "a wavefront has eight rows of codes of a tile");
+    static_assert(FMT == kPlain || (PAGED && DT == ILRE_BF16 && CROWS == 8), "a wavefront has eight rows of codes of a tile");
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
@@ -664,8 +641,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     // of a quantised cache: where the head lies, and the codes that are on their way
     constexpr int QF = FMT == kPlain ? ILRE_KV_FP8 : FMT;
     QuantSource<QF> quant;
-    CodeRows<DT, QF, false> key_rows;
-    CodeRows<DT, QF, true> value_rows;
+    CodeRows<false> key_rows;
+    CodeRows<true> value_rows;
     if (FMT != kPlain) {
         quant.init(a, head, lane);
         key_rows.init(lds0, wave * CROWS, lane);
@@ -674,8 +651,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     Codes<QF> codes[2];  // of keys and values
     auto fetch = [&](int i, int page) { fetch_codes<QF>(a, blk, quant, own_token(i), page, codes, lane); };
     auto write = [&](int i) {
-        write_codes<DT, QF, false>(codes[0], key_rows, i % RING * SLOT, lane);
-        write_codes<DT, QF, true>(codes[1], value_rows, i % RING * SLOT, lane);
+        write_codes<QF, false>(codes[0], key_rows, i % RING * SLOT, lane);
+        write_codes<QF, true>(codes[1], value_rows, i % RING * SLOT, lane);
     };
     int pages[2];  // of this wavefront's rows: of the last tile whose keys were asked for, and the next one
     auto lookup = [&](int i) {
@@ -694,10 +671,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         if constexpr (FMT != kPlain) {
             const int p0 = lookup(0), p1 = lookup(1);
             fetch(0, p0);
-            if (RING == 2) {
-                pages[0] = p1;
-                return;
-            }
             write(0);
             fetch(1, p1);
             pages[0] = lookup(2);
@@ -722,10 +695,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
     // Tile i's values and tile i + 1's keys (two buffers: tile i's) are there, everybody is done with tile i - 1, and the next copies are on their way.
     auto advance = [&](int i) {
         if constexpr (FMT != kPlain) {
-            constexpr int AHEAD = RING == 2 ? 0 : 1;  // with four buffers what is written now is for the next tile
-            write(i + AHEAD);
-            fetch(i + AHEAD + 1, pages[0]);
-            pages[0] = lookup(i + AHEAD + 2);
+            write(i + 1);
+            fetch(i + 2, pages[0]);
+            pages[0] = lookup(i + 3);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
@@ -1085,30 +1057,16 @@ struct ValueCodes {
     unsigned char scale[N];
 };
 
-// Two channels (word i of a piece, pair k of the word) as the states' type.
-template <int DT, int FMT>
-__device__ __forceinline__ void piece_to_numbers(const u32x4 &w, float scale, u32x4 (&x)[FMT == ILRE_KV_FP8 ? DT == ILRE_BF16 ? 2 : 4 : DT == ILRE_BF16 ? 4 : 8])
+// A piece as bf16, 16 bytes at a time.
+template <int FMT>
+__device__ __forceinline__ void piece_to_numbers(const u32x4 &w, float scale, u32x4 (&x)[FMT == ILRE_KV_FP8 ? 2 : 4])
 {
-    constexpr int PER = FMT == ILRE_KV_FP8 ? 2 : 4;  // pairs a word
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const int at = i * PER + k;
-            if constexpr (DT == ILRE_BF16) {
-                x[at / 4][at % 4] = k == 0   ? bf16_pair<FMT, 0>(w[i], scale)
-                                    : k == 1 ? bf16_pair<FMT, 1>(w[i], scale)
-                                    : k == 2 ? bf16_pair<FMT, PER == 4 ? 2 : 0>(w[i], scale)
-                                             : bf16_pair<FMT, PER == 4 ? 3 : 0>(w[i], scale);
-            } else {
-                const float2 f = k == 0   ? f32_pair<FMT, 0>(w[i], scale)
-                                 : k == 1 ? f32_pair<FMT, 1>(w[i], scale)
-                                 : k == 2 ? f32_pair<FMT, PER == 4 ? 2 : 0>(w[i], scale)
-                                          : f32_pair<FMT, PER == 4 ? 3 : 0>(w[i], scale);
-                x[at / 2][at % 2 * 2] = __float_as_uint(f.x);
-                x[at / 2][at % 2 * 2 + 1] = __float_as_uint(f.y);
-            }
-        }
+        if constexpr (FMT == ILRE_KV_FP8)
+            x[i / 2][i % 2 * 2] = bf16_pair<FMT, 0>(w[i], scale), x[i / 2][i % 2 * 2 + 1] = bf16_pair<FMT, 1>(w[i], scale);
+        else
+            x[i] = u32x4{bf16_pair<FMT, 0>(w[i], scale), bf16_pair<FMT, 1>(w[i], scale), bf16_pair<FMT, 2>(w[i], scale), bf16_pair<FMT, 3>(w[i], scale)};
     }
 }
 
@@ -1126,16 +1084,10 @@ __device__ __forceinline__ int unit_of_block(const AttnArgs &a)
     return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD / a.Hkv * kNumXCD + blockIdx.x % kNumXCD : blockIdx.x / a.Hkv;
 }
 
-template <int DT>
-constexpr size_t codes_lds(int waves)
+template <int FMT, int WAVES, bool TREE>
+__global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
 {
-    return waves * (32 * kHeadDim * 4 + 32 * sizeof(float2));
-}
-
-template <int DT, int WAVES, int FMT, bool TREE>
-__global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_codes(const AttnArgs a)
-{
-    using E = Elem<DT>;
+    using E = Elem<ILRE_BF16>;
     using K = KeyCodes<FMT>;
     using V = ValueCodes<FMT>;
     constexpr int ROWB = E::ROWB, PITCH = 32 * kHeadDim * 4, TN = 32 * WAVES, ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM), LANES = ROW / 16;  // lanes a row of values
@@ -1156,7 +1108,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
     auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
 
-    State<DT> st;
+    State<ILRE_BF16> st;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * PITCH;
     typename E::Addr ad;
     ad.init(lane);
@@ -1233,9 +1185,9 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
             fetch_rows(i, p.id[1], place(tok + 16, p.id[1]) - 16 * a.k_token, middle, all, c);
         }
     };
-    constexpr int NX = FMT == ILRE_KV_FP8 ? DT == ILRE_BF16 ? 2 : 4 : DT == ILRE_BF16 ? 4 : 8;  // 16-byte pieces of numbers in one of codes
+    constexpr int NX = FMT == ILRE_KV_FP8 ? 2 : 4;  // 16-byte pieces of numbers in one of codes
     // Eight lanes write together; so that they reach all banks, a lane's pieces go out in an order of its own: piece k ^ turn.
-    const int turn = NX == 2 ? v_piece >> 2 : LANES == 8 ? v_piece >> 1 : NX == 4 ? v_piece >> 1 | (v_row & 1) << 1 : v_piece << 1;
+    const int turn = NX == 2 ? v_piece >> 2 : v_piece >> 1 | (v_row & 1) << 1;
     unsigned v_to[NX];
 #pragma unroll
     for (int k = 0; k < NX; ++k) v_to[k] = lds0 + v_row * ROWB + (((NX * v_piece + (k ^ turn)) ^ (v_row & 3) << 2) * 16);
@@ -1246,11 +1198,10 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
             if (NX == 2) {
                 w = turn ? u32x4{w[2], w[3], w[0], w[1]} : w;
             } else {
-                const int q = NX == 8 ? turn >> 1 : turn;
-                w = q & 1 ? u32x4{w[1], w[0], w[3], w[2]} : w;
-                w = q & 2 ? u32x4{w[2], w[3], w[0], w[1]} : w;
+                w = turn & 1 ? u32x4{w[1], w[0], w[3], w[2]} : w;
+                w = turn & 2 ? u32x4{w[2], w[3], w[0], w[1]} : w;
             }
-            piece_to_numbers<DT, FMT>(w, scale_of(c.scale[j]), x);
+            piece_to_numbers<FMT>(w, scale_of(c.scale[j]), x);
 #pragma unroll
             for (int k = 0; k < NX; ++k) lds_write16(v_to[k] + j * V::ROWS * ROWB, x[k]);
         }
@@ -1263,16 +1214,9 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
 #pragma unroll
         for (int j = 0; j < K::N; ++j) {
             u32x4 x[NX];
-            piece_to_numbers<DT, FMT>(c.w[j], scale[j * 2 / K::N], x);
+            piece_to_numbers<FMT>(c.w[j], scale[j * 2 / K::N], x);
 #pragma unroll
-            for (int k = 0; k < NX; ++k) {
-                if constexpr (DT == ILRE_BF16) {
-                    Elem<ILRE_BF16>::mma(s, x[k], st.q[j * NX + k]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[k][e]), __uint_as_float(st.q[j * NX + k][e]), s, 0, 0, 0);
-                }
-            }
+            for (int k = 0; k < NX; ++k) E::mma(s, x[k], st.q[j * NX + k]);
         }
     };
 
@@ -1308,15 +1252,35 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_co
             next = lookup(min(i + 2, count - 1));
         }
     }
-    join_waves<DT, WAVES, PITCH>(a, blk, st, smem, head, wave, l32, half, nsp == 1, split);
+    join_waves<ILRE_BF16, WAVES, PITCH>(a, blk, st, smem, head, wave, l32, half, nsp == 1, split);
 }
 
-// Up to 16 rows, bf16 states: the matrix instructions of 16 rows, as half of the logits, exponentials and sums above would be nobody's.  Lane l has query l % 16; tokens 16 b + 4 (l / 16) + i of
+// Up to 16 rows: the matrix instructions of 16 rows, as half of the logits, exponentials and sums above would be nobody's.  Lane l has query l % 16; tokens 16 b + 4 (l / 16) + i of
 // logits, i = 0..3, b = 0, 1; channels 16 db + 4 (l / 16) + i of sums.  Of keys it has a quarter of the codes, one block of a scale, of tokens l % 16 and 16 + l % 16.  With fewer
 // registers and half the LDS three or four workgroups fit a compute unit.
-template <int FMT, int WAVES, bool TREE>
-__global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) void attend_codes16(const AttnArgs a)
+//
+// Keys and values are exact in bf16, so that fp32 states take the bf16 matrix instructions too: queries and weights go in as three parts, each the rest rounded to nearest, which hold 24 bits
+// (the fp32 matrix instructions are a sixteenth as fast).
+__device__ __forceinline__ void split_parts(const float (&x)[8], u32x4 (&part)[3])
 {
+    float rest[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) rest[k] = x[k];
+#pragma unroll
+    for (int n = 0; n < 3; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned u = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+            part[n][k] = u;
+            rest[2 * k] -= __uint_as_float(u << 16);
+            rest[2 * k + 1] -= __uint_as_float(u & 0xFFFF0000u);
+        }
+}
+
+template <int DT, int FMT, int WAVES, bool TREE>
+__global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) void attend_codes16(const AttnArgs a)
+{
+    constexpr int PARTS = DT == ILRE_F32 ? 3 : 1;  // of queries and weights
     using V = ValueCodes<FMT>;
     constexpr int ROWB = 256, PITCH = 32 * ROWB, TN = 32 * WAVES, ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM), LANES = ROW / 16, KN = ROW / 64;  // KN: 16-byte pieces of a quarter of a token
     extern __shared__ __align__(16) unsigned char smem[];
@@ -1408,7 +1372,7 @@ __global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) vo
         for (int j = 0; j < V::N; ++j) {
             u32x4 w = c.w[j], x[NX];
             w = turn ? (NX == 2 ? u32x4{w[2], w[3], w[0], w[1]} : u32x4{w[1], w[0], w[3], w[2]}) : w;
-            piece_to_numbers<ILRE_BF16, FMT>(w, scale_of(c.scale[j]), x);
+            piece_to_numbers<FMT>(w, scale_of(c.scale[j]), x);
 #pragma unroll
             for (int k = 0; k < NX; ++k) lds_write16(v_to[k] + j * V::ROWS * ROWB, x[k]);
         }
@@ -1427,13 +1391,22 @@ __global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) vo
         fetch_values(0, now, values);
     }
     // the lane's query: channels 32 g + 8 st .. of row rows0 + l16; past the last row zeros, which see what the last one sees and are written nowhere
-    u32x4 q[4];
+    u32x4 q[4][PARTS];
     int lo, hi;
     {
         const int want = blk.rows0 + l16, r = min(want, blk.nrows - 1), i = r / a.G;
-        const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head * a.G + r - i * a.G) * a.q_head + g * 64;
+        const unsigned char *src = a.q + (int64_t)(blk.q0 + i) * a.q_token + (int64_t)(head * a.G + r - i * a.G) * a.q_head + g * (DT == ILRE_F32 ? 128 : 64);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = want == r ? *(const u32x4 *)(src + k * 16) : u32x4{};
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (DT == ILRE_F32) {
+                const f32x4 x = ((const f32x4 *)src)[2 * k], y = ((const f32x4 *)src)[2 * k + 1];
+                const bool real = want == r;
+                const float f[8] = {real ? x[0] : 0.f, real ? x[1] : 0.f, real ? x[2] : 0.f, real ? x[3] : 0.f, real ? y[0] : 0.f, real ? y[1] : 0.f, real ? y[2] : 0.f, real ? y[3] : 0.f};
+                split_parts(f, q[k]);
+            } else {
+                q[k][0] = want == r ? *(const u32x4 *)(src + k * 16) : u32x4{};
+            }
+        }
         const int p = max(blk.kv - blk.q_len + i, -1);
         hi = a.causal ? min(p + 1, blk.kv) : blk.kv;
         lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
@@ -1452,9 +1425,11 @@ __global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) vo
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 u32x4 x[NX];
-                piece_to_numbers<ILRE_BF16, FMT>(keys.w[b][j], scale_of(keys.scale[b]), x);
+                piece_to_numbers<FMT>(keys.w[b][j], scale_of(keys.scale[b]), x);
 #pragma unroll
-                for (int k = 0; k < NX; ++k) mma(s[b], x[k], q[j * NX + k]);
+                for (int k = 0; k < NX; ++k)
+#pragma unroll
+                    for (int n = PARTS - 1; n >= 0; --n) mma(s[b], x[k], q[j * NX + k][n]);
             }
         }
         write_values(values);
@@ -1491,11 +1466,16 @@ __global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) vo
 #pragma unroll
         for (int k = 0; k < 8; ++k) p[k] = exp2_fast(fmaf(s[k / 4][k % 4], a.c, -m));
         z += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        const u32x4 w = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+        u32x4 w[PARTS];
+        if constexpr (DT == ILRE_F32)
+            split_parts(p, w);
+        else
+            w[0] = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
             const u32x2 x = lds_read_tr(v_from[db & 3] + (db >> 2) * 128), y = lds_read_tr(v_from[db & 3] + (db >> 2) * 128 + 16 * ROWB);
-            mma(o[db], u32x4{x[0], x[1], y[0], y[1]}, w);
+#pragma unroll
+            for (int n = PARTS - 1; n >= 0; --n) mma(o[db], u32x4{x[0], x[1], y[0], y[1]}, w[n]);
         }
         if (more) {
             now = next;
@@ -1533,10 +1513,10 @@ __global__ __launch_bounds__(WAVES * 64, FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) vo
     if (!t.real) return;
     x[0] *= t.f;
     x[1] *= t.f;
-    if (t.direct) {
+    if (t.direct && DT == ILRE_BF16) {
         *(uint4 *)(t.out + part * 16) = make_uint4(pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]), pack_bf16(x[1][2], x[1][3]));
     } else {
-        f32x4 *to = (f32x4 *)(a.part_o + t.row * kHeadDim + part * 8);
+        f32x4 *to = (f32x4 *)(t.direct ? (float *)t.out : a.part_o + t.row * kHeadDim) + part * 2;
         to[0] = x[0];
         to[1] = x[1];
     }
@@ -1681,32 +1661,39 @@ hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 template <int DT, int WAVES, bool PAGED, int FMT, bool TREE>
 hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    if constexpr (FMT != kPlain) return launch(attend_codes<DT, WAVES, FMT, TREE>, p, WAVES * 64, codes_lds<DT>(WAVES), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
-    return launch(attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
+    if constexpr (FMT != kPlain)
+        return launch(attend_codes<FMT, WAVES, TREE>, p, WAVES * 64, WAVES * (32 * kHeadDim * 4 + 32 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
+    else
+        return launch(attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
 template <bool PAGED, int FMT = kPlain, bool TREE = false>
 hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
     hipError_t e;
-    if (p.dtype == ILRE_BF16) {
-        if constexpr (FMT != kPlain) {
-            if (p.rows == 16) {
-                e = launch(attend_codes16<FMT, 4, TREE>, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
-                return e != hipSuccess || p.nsplit == 1 ? e : launch_merge<ILRE_BF16, PAGED>(p, a, s);
-            }
+    if constexpr (FMT != kPlain) {
+        if (p.rows == 16) {
+            constexpr size_t lds = 4 * (32 * 256 + 16 * sizeof(float2));
+            constexpr unsigned step = FMT == ILRE_KV_FP4 ? kNumXCD : 1;
+            e = p.dtype == ILRE_BF16 ? launch(attend_codes16<ILRE_BF16, FMT, 4, TREE>, p, 256, lds, a, s, step) : launch(attend_codes16<ILRE_F32, FMT, 4, TREE>, p, 256, lds, a, s, step);
+            if (e != hipSuccess || p.nsplit == 1) return e;
+            return p.dtype == ILRE_BF16 ? launch_merge<ILRE_BF16, PAGED>(p, a, s) : launch_merge<ILRE_F32, PAGED>(p, a, s);
         }
+    }
+    if (p.dtype == ILRE_BF16) {
         if (p.rows == 32)
             e = launch_tokens<ILRE_BF16, 4, PAGED, FMT, TREE>(p, a, s);
         else if (p.rows == 128)
             e = launch_rows<ILRE_BF16, 8, 2, 64, PAGED, FMT, TREE>(p, a, s);
         else
             e = launch_rows<ILRE_BF16, 8, 1, 64, PAGED, FMT, TREE>(p, a, s);
-    } else {
+    } else if constexpr (FMT == kPlain) {
         if (p.rows == 32)
             e = launch_tokens<ILRE_F32, 4, PAGED, FMT, TREE>(p, a, s);
         else
             e = launch_rows<ILRE_F32, 4, 1, 32, PAGED, FMT, TREE>(p, a, s);
+    } else {
+        e = hipErrorInvalidValue;  // (fp32 states over a quantised cache are cut into 16 rows)
     }
     if (e != hipSuccess || p.nsplit == 1) return e;
     return p.dtype == ILRE_BF16 ? launch_merge<ILRE_BF16, PAGED>(p, a, s) : launch_merge<ILRE_F32, PAGED>(p, a, s);

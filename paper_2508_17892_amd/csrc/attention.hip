@@ -13,6 +13,8 @@ namespace ilre {
 //     11.7; 30000 tokens, 8/2 heads: 17.7 and 15.7).  More rows: 12 tiles of 64 tokens at least, and 4 while the merge has little to do (32/8 heads, 4096 tokens: 16
 //     new ones 18.4 us with 4, 25.2 with 12, 64 29.7 and 35.7, 200 51.9 and 40.3), 2 of 32 in fp32 (prompts of 77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6,
 //     6 74).
+//   - fp32 states over a quantised cache: 16 rows a workgroup however many there are, as only that kernel splits them into parts for the bf16 matrix instructions (32/8 heads, 8 bits: one token over 131072
+//     234 us with the fp32 instructions, 59 so; 8 over 30000 69 and 28, 100 over 9000 247 and 77, 1024 over 33000 5150 and 1800).
 //   - Trees, and more than 16 rows over a quantised cache: a range leaves 32 rows behind for the merge, a quarter to half of what a tile of 128 tokens is. A range a compute unit, two from twelve tiles each
 //     on, and whole where that is a merge's worth longer at most (8 drafted tokens, 32/8 heads: contexts of 4105, 9009, 7 and 300 26.1 -> 20.8 us, eight of 3000 28.3 -> 26.9, one of 30000 33.9 -> 31.7,
 //     sixteen of 900 22.0 -> 19.8; in 8 bits 24.3 -> 18.8, 22.1 -> 20.4, 23.3 -> 21.7, 20.2 -> 16.8).
@@ -37,7 +39,7 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
         if (window <= 0) return all;
         return std::min(all, (std::min((int64_t)sink, kv) + p.tile - 1) / p.tile + (window + (p.rows + G - 1) / G) / p.tile + 2);
     };
-    if (rows <= 16 && dtype == ILRE_BF16 && format != kPlain) {
+    if (format != kPlain && (rows <= 16 || dtype == ILRE_F32)) {
         cut(16, 128);
     } else if (rows <= 32) {
         cut(32, 128);

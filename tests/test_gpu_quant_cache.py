@@ -227,6 +227,7 @@ TREES = [
     ([4, 3], [3000, 700], 8, 2, 16, "head", "bf16"),         # 16 rows
     ([2], [30], 8, 2, 16, "head", "f32"),
     ([20], [30], 8, 2, 16, "head", "f32"),
+    ([5, 9], [2000, 900], 8, 2, 16, "token", "f32"),
 ]
 
 
