@@ -270,12 +270,13 @@ typedef struct {
 } ilre_quant_kv;
 
 /* Norms of queries and keys, each head by itself, before the rotation: y = x / sqrt(mean(x^2) + eps) * (weight + offset).  Sums are fp32 (fp64 for keys of a quantised cache), the
-   result is not rounded before it is turned.  (offset 1: weights that are kept as differences from one.) */
+   result is not rounded before it is turned.  (offset 1: weights that are kept as differences from one.  A head whose squares add up to more than fp32 holds, magnitudes of 2^60 and more, comes
+   out as zeros where the sum is fp32.) */
 typedef struct {
     int32_t struct_size;      /* sizeof(ilre_head_norms) */
     int32_t q_norm, k_norm;   /* 1: normed, 0: as they are */
     float offset;
-    double eps;               /* >= 0 */
+    double eps;               /* 0, or at least 2^-126 */
     const void *q_weight, *k_weight; /* dev, d elements of opts->dtype, 16-byte aligned; NULL: weight + offset is one */
 } ilre_head_norms;
 
@@ -359,7 +360,7 @@ int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t
 /* Attention of the new tokens of n_seq sequences over a paged cache that holds them already: one token each, a chunk of a prompt, or any mixture.
    out[i,h,:] = sum_t softmax_t(q[i,h,:] . K[g(h),t,:] * scale) V[g(h),t,:] over the tokens that ilre_attn lets row i see; consecutive query heads share a kv
    head as in Eq. 4.  Rows that see nothing give zeros and lse = -inf.  Logits, softmax and sums are fp32, weights are rounded to opts->dtype for the
-   product with V (their sum is taken before that).  Values and keys that some row of the call sees have to be finite, and its logits below 2^30 in magnitude: fp32
+   product with V (their sum is taken before that).  Over a quantised cache keys and values are the numbers that codes and scales stand for, exactly.  Values and keys that some row of the call sees have to be finite, and its logits below 2^30 in magnitude: fp32
    holds a logit and its row's reference to 2^-24 of themselves, and beyond that the exponential of what is left overflows.  What no row sees may hold anything.
    q, out     dev  [T, Hq, d] (strides->q_*, out_*); out must not overlap q
    lse        dev  [T, Hq] float, the natural logarithm of each row's sum of exponentials; may be NULL
