@@ -78,6 +78,58 @@ struct Eight {  // channels, as they lie in memory
     }
 };
 
+// What lane l ^ 1, l ^ 2 and (where every four lanes hold the same already) l ^ 4 has.
+template <int CTRL>
+__device__ __forceinline__ unsigned from_lane(unsigned x)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kXor4 = 0x141;  // quad permutations 1 0 3 2 and 2 3 0 1; a mirrored half row
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) { return __uint_as_float(from_lane<CTRL>(__float_as_uint(x))); }
+template <int CTRL>
+__device__ __forceinline__ double from_lane(double x)
+{
+    const unsigned long long u = (unsigned long long)__double_as_longlong(x);
+    const unsigned lo = from_lane<CTRL>((unsigned)u), hi = from_lane<CTRL>((unsigned)(u >> 32));
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+// Over a head's eight lanes.
+template <typename T>
+__device__ __forceinline__ T sum_of_eight(T x)
+{
+    x += from_lane<kXor1>(x);
+    x += from_lane<kXor2>(x);
+    return x + from_lane<kXor4>(x);
+}
+
+// Sine and cosine of `part` turns, |part| <= 1/2: to the nearest quarter turn, then the series of both up to x^15 and x^16, whose rests are below 2^-54 for |x| <= pi / 4.
+__device__ __forceinline__ void sine_and_cosine(double part, double &s, double &c)
+{
+    const double quarter = rint(4.0 * part), x = fma(quarter, -0.25, part) * 6.283185307179586476925, y = x * x;
+    double p = -1.0 / 1307674368000.0, q = 1.0 / 20922789888000.0;
+    p = fma(p, y, 1.0 / 6227020800.0);
+    p = fma(p, y, -1.0 / 39916800.0);
+    p = fma(p, y, 1.0 / 362880.0);
+    p = fma(p, y, -1.0 / 5040.0);
+    p = fma(p, y, 1.0 / 120.0);
+    p = fma(p, y, -1.0 / 6.0);
+    p = fma(p * y, x, x);
+    q = fma(q, y, -1.0 / 87178291200.0);
+    q = fma(q, y, 1.0 / 479001600.0);
+    q = fma(q, y, -1.0 / 3628800.0);
+    q = fma(q, y, 1.0 / 40320.0);
+    q = fma(q, y, -1.0 / 720.0);
+    q = fma(q, y, 1.0 / 24.0);
+    q = fma(q, y, -0.5);
+    q = fma(q, y, 1.0);
+    const int k = (int)quarter;  // -2 .. 2
+    s = k & 1 ? q : p;
+    c = k & 1 ? p : q;
+    if (k & 2) s = -s;
+    if ((k + 1) & 2) c = -c;
+}
+
 // Where pair j's sine and cosine lie: eight lanes read every eighth pair (every fourth) at a time, from different banks.
 __device__ __forceinline__ int spread(int j) { return j + (j >> 3); }
 
@@ -183,7 +235,7 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
             wheel[spread(lane)].c = fmaf(-s, lower, c) * m;
         } else {
             double s, c;
-            sincospi(2.0 * part, &s, &c);
+            sine_and_cosine(part, s, c);
             s *= a.magnitude;
             c *= a.magnitude;
             key_wheel[spread(lane)] = KeyTurn{(Real)c, (Real)s};
@@ -221,9 +273,7 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fmaf(x[s][e], x[s][e], sum);
-#pragma unroll
-        for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
-        return rsqrtf(sum * (1.f / ILRE_HEAD_DIM) + (float)a.eps);
+        return rsqrtf(sum_of_eight(sum) * (1.f / ILRE_HEAD_DIM) + (float)a.eps);
     };
     auto norm64 = [&](const float (&x)[2][8]) {
         double sum = 0.0;
@@ -231,9 +281,7 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fma((double)x[s][e], (double)x[s][e], sum);
-#pragma unroll
-        for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
-        return 1.0 / sqrt(sum * (1.0 / ILRE_HEAD_DIM) + a.eps);
+        return 1.0 / sqrt(sum_of_eight(sum) * (1.0 / ILRE_HEAD_DIM) + a.eps);
     };
     // fp32: coefficients of the token's heads, and a head turned
     float A[2][8], B[2][8];
@@ -313,29 +361,51 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
             for (int s = 0; s < 2; ++s) x.x[s].get(f[s]);
             r = norm64(f);
         }
+        const bool weighted = a.k_norm && a.k_weight;
+        auto weight64 = [&](float w) { return weighted ? (double)w + a.offset : 1.0; };
+        float y[2][8];
+        if (PAIR == kSameLane && keys) {  // both channels of a pair at once
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float f[2][8], w[2][8];
+#pragma unroll
+                for (int s = 0; s < 2; ++s) x.x[s].get(f[s]), weight.x[s].get(w[s]);
+                const KeyTurn t = turn_of(key_wheel, 1, e);
+                const double m = f[0][e] * weight64(w[0][e]) * r, n = f[1][e] * weight64(w[1][e]) * r;
+                y[0][e] = cut_off(m * t.c - n * t.s);
+                y[1][e] = cut_off(n * t.c + m * t.s);
+                if (e == 3) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) x.x[s].forget(), weight.x[s].forget();
+                }
+            }
+        }
         auto run = [&](auto number) {  // eight channels
             constexpr int s = number.value;
             float f[8];
             x.x[s].get(f);
-            if (keys) {
+            if (PAIR == kSameLane) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = key ? y[s][e] : f[e];
+            } else if (keys) {
                 float p[8], own[8], others[8];
                 other_channels(x, s, p);
                 weight.x[s].get(own);
                 other_channels(weight, s, others);
-                const bool there = a.k_norm && a.k_weight;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const KeyTurn t = turn_of(key_wheel, s, e);
-                    const float w = there ? own[e] + a.offset : 1.f, v = there ? others[e] + a.offset : 1.f, q = turned[s] ? p[e] : 0.f;
-                    const float y = cut_off(((double)f[e] * w * t.c + (double)q * v * t.s) * r);
-                    f[e] = key ? y : f[e];
+                    const float q = turned[s] ? p[e] : 0.f;
+                    const float z = cut_off((f[e] * weight64(own[e]) * t.c + q * weight64(others[e]) * t.s) * r);
+                    f[e] = key ? z : f[e];
                 }
             }
             unsigned top = 0;  // the largest magnitude, as bits: a NaN's are larger than any number's
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
-            top = max(top, (unsigned)__shfl_xor((int)top, 1));
-            top = max(top, (unsigned)__shfl_xor((int)top, 2));
+            top = max(top, from_lane<kXor1>(top));
+            top = max(top, from_lane<kXor2>(top));
             const unsigned byte = scale_byte<FMT == kPlain ? ILRE_KV_FP8 : FMT>(__uint_as_float(top));
             const float inv = inverse_scale(byte);
             const int64_t channel = to + from[s];
