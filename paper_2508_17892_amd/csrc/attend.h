@@ -302,6 +302,12 @@ __device__ __forceinline__ void write_codes(const Codes<FMT> &c, const CodeRows<
 
 // ------------------------------------------------------------------------------------------------ products
 
+// Two 16-bit halves, each kept where its bit (0, 1) is set.
+__device__ __forceinline__ unsigned keep_halves(unsigned x, unsigned bits)
+{
+    return x & ((bits & 1 ? 0xFFFFu : 0u) | (bits & 2 ? 0xFFFF0000u : 0u));
+}
+
 template <int DT>
 struct Elem;
 
@@ -354,6 +360,19 @@ struct Elem<ILRE_BF16> {
                 mma(o[db], u32x4{x[0], x[1], y[0], y[1]}, w.p[ks]);
             }
     }
+    // The same with zeros for the values of tokens whose bit in `keep` is not set.
+    static __device__ __forceinline__ void values(f32x16 (&o)[4], const Weights &w, const Addr &ad, unsigned vat, unsigned keep, int half)
+    {
+        keep >>= 4 * half;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                const u32x2 x = lds_read_tr(ad.v[db] + vat + ks * 16 * ROWB), y = lds_read_tr(ad.v[db] + vat + (ks * 16 + 8) * ROWB);
+                const unsigned b = keep >> (16 * ks);
+                mma(o[db], u32x4{keep_halves(x[0], b), keep_halves(x[1], b >> 2), keep_halves(y[0], b >> 8), keep_halves(y[1], b >> 10)}, w.p[ks]);
+            }
+    }
 };
 
 // fp32 states: the fp32 matrix instructions (a sixteenth of the bf16 rate), nothing is rounded on the way.
@@ -398,6 +417,17 @@ struct Elem<ILRE_F32> {
                 // chunk (8 db + l32 / 4) ^ (i % 4 << 2): the upper bit of the XOR picks another channel block
                 const float v = lds_read4(ad.v[i & 3] + vat + (i >> 2) * 8 * ROWB + (db ^ ((i & 3) >> 1)) * 128);
                 o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.p[i], o[db], 0, 0, 0);
+            }
+    }
+    static __device__ __forceinline__ void values(f32x16 (&o)[4], const Weights &w, const Addr &ad, unsigned vat, unsigned keep, int half)
+    {
+        keep >>= 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                const float v = lds_read4(ad.v[i & 3] + vat + (i >> 2) * 8 * ROWB + (db ^ ((i & 3) >> 1)) * 128);
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(keep >> (8 * (i >> 2) + (i & 3)) & 1 ? v : 0.f, w.p[i], o[db], 0, 0, 0);
             }
     }
 };
@@ -509,7 +539,20 @@ struct State {
     }
 };
 
-// What a row sees of a tree of drafted tokens, which are the tokens from `base` on (it may lie in front of the sequence).
+// The bits that some lane has.
+__device__ __forceinline__ unsigned of_any_lane(unsigned x)
+{
+    auto from = [](auto ctrl, unsigned y) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)y, ctrl.value, 0xF, 0xF, true); };
+    x |= from(std::integral_constant<int, 0xB1>{}, x);   // quad permutation 1 0 3 2
+    x |= from(std::integral_constant<int, 0x4E>{}, x);   // 2 3 0 1
+    x |= from(std::integral_constant<int, 0x141>{}, x);  // half rows mirrored
+    x |= from(std::integral_constant<int, 0x140>{}, x);  // rows of 16 mirrored
+    return (unsigned)(__builtin_amdgcn_readlane((int)x, 0) | __builtin_amdgcn_readlane((int)x, 16) | __builtin_amdgcn_readlane((int)x, 32) | __builtin_amdgcn_readlane((int)x, 48));
+}
+
+// What a row sees of a tree of drafted tokens, which are the tokens from `base` on (it may lie in front of the sequence).  A drafted token that no row of the wavefront sees may hold
+// anything, and stands in the middle of others that are seen: its values are made zeros, as a weight of zero times a NaN is a NaN (attend_rows, whose wavefronts share tiles: on the way from LDS to the
+// matrix instruction; the others: in LDS).
 struct Drafted {
     const uint32_t *words;
     int base, n;
@@ -530,6 +573,18 @@ struct Drafted {
         return (unsigned)(((unsigned long long)hi << 32 | lo) >> (j & 31));
     }
 };
+
+// Zeros for those of a wavefront's 32 rows of values in LDS whose bit is not set.
+template <int ROWB>
+__device__ __forceinline__ void keep_rows(unsigned tile, unsigned keep, int lane)
+{
+    for (unsigned gone = ~keep; gone; gone &= gone - 1) {
+        const unsigned row = tile + (unsigned)__builtin_ctz(gone) * ROWB;
+#pragma unroll
+        for (int at = 0; at < ROWB; at += 256) *(__attribute__((address_space(3))) unsigned *)(size_t)(row + at + lane * 4) = 0;
+    }
+    __builtin_amdgcn_wave_barrier();
+}
 
 // Where a row's results go: where all of its tokens were in this workgroup's range, out and the logarithm of the sum; otherwise the quotient in
 // fp32 and the base-2 logarithm for the merge.
@@ -729,6 +784,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
         const int tok = token_of(i) + part;
         f32x16 s[SUB];
         typename E::Weights w[SUB];
+        unsigned seen[SUB];
 #pragma unroll
         for (int sub = 0; sub < SUB; ++sub) E::logits(s[sub], st.q, ad, keys_at(i, sub));
         int absent = 0;
@@ -736,7 +792,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
             for (int k = 0; k < SUB * 2; ++k) absent |= (page_of(a, blk, tok + 16 * k) < 0 ? 1 : 0) << k;
         }
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) st.hide(s[sub], tok + 32 * sub, a.sink, half, absent >> (2 * sub), TREE ? drafted.bits(tok + 32 * sub) : ~0u);
+        for (int sub = 0; sub < SUB; ++sub) {
+            seen[sub] = TREE ? drafted.bits(tok + 32 * sub) : ~0u;
+            st.hide(s[sub], tok + 32 * sub, a.sink, half, absent >> (2 * sub), seen[sub]);
+        }
         if (kept.value) {
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) st.weigh_kept(s[sub], w[sub], a.c);
@@ -744,7 +803,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_rows(const AttnArgs a)
             st.template weigh<SUB>(s, w, a.c);
         }
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) E::values(st.o, w[sub], ad, values_at(i, sub));
+        for (int sub = 0; sub < SUB; ++sub) {
+            if constexpr (TREE)
+                E::values(st.o, w[sub], ad, values_at(i, sub), of_any_lane(seen[sub]), half);
+            else
+                E::values(st.o, w[sub], ad, values_at(i, sub));
+        }
     };
 
     // Tiles g1 .. g2 - 1, which all rows see whole, against the references that the tiles before have left.  32 tokens are a step, and a step holds three
@@ -1018,12 +1082,14 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         E::logits(s[0], st.q, ad, lds0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads are done before the buffer is written again
         if (more) copy_keys(i + 1, next);
-        st.hide(s[0], token_of(i), a.sink, half, absent, TREE ? drafted.bits(token_of(i)) : ~0u);
+        const unsigned seen = TREE ? drafted.bits(token_of(i)) : ~0u;
+        st.hide(s[0], token_of(i), a.sink, half, absent, seen);
         st.template weigh<1>(s, w, a.c);
         if (more)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (TREE && __builtin_amdgcn_readfirstlane(token_of(i) + 32 > drafted.base)) keep_rows<E::ROWB>(lds0 + SLOT, of_any_lane(seen), lane);
         E::values(st.o, w[0], ad, lds0 + SLOT);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) {
@@ -1243,8 +1309,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
             fetch_keys(i + 1, next, keys);
             fetch_values(i + 1, next, values);
         }
-        if (tok < blk.all_lo || tok + 32 > blk.all_hi || absent)  // an edge: what a row does not see is hidden
-            st.hide(s[0], tok, a.sink, half, absent, TREE ? drafted.bits(tok) : ~0u);
+        if (tok < blk.all_lo || tok + 32 > blk.all_hi || absent) {  // an edge: what a row does not see is hidden
+            const unsigned seen = TREE ? drafted.bits(tok) : ~0u;
+            if (TREE) keep_rows<ROWB>(lds0, of_any_lane(seen), lane);
+            st.hide(s[0], tok, a.sink, half, absent, seen);
+        }
         st.template weigh<1, true>(s, w, a.c);
         E::values(st.o, w[0], ad, lds0);
         if (more) {
@@ -1438,7 +1507,9 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4
             fetch_values(i + 1, next, values);
         }
         if (tok < blk.all_lo || tok + 32 > blk.all_hi || absent) {  // an edge: what a row does not see is hidden
-            unsigned bits = first_bits(hi - tok) & (~first_bits(lo - tok) | first_bits(a.sink - tok)) & (TREE ? drafted.bits(tok) : ~0u);
+            const unsigned seen = TREE ? drafted.bits(tok) : ~0u;
+            if (TREE) keep_rows<ROWB>(lds0, of_any_lane(seen), lane);
+            unsigned bits = first_bits(hi - tok) & (~first_bits(lo - tok) | first_bits(a.sink - tok)) & seen;
             bits &= ~((absent & 1 ? 0xFFFFu : 0u) | (absent & 2 ? 0xFFFF0000u : 0u));
             bits >>= 4 * g;
 #pragma unroll

@@ -261,6 +261,35 @@ def test_tree_attention(fmt, q_lens, kv_lens, Hq, Hkv, page, layout, dtype):
     assert torch.equal(out, got) and torch.equal(lse, lse3)
 
 
+@pytest.mark.parametrize("fmt", ["plain", "fp8", "fp4"])
+@pytest.mark.parametrize("q_lens,kv_lens,Hq,Hkv,page,layout,dtype", TREES)
+def test_drafted_tokens_that_nobody_sees_hold_anything(fmt, q_lens, kv_lens, Hq, Hkv, page, layout, dtype):
+    """Drafted tokens that were given up, or never filled in, between others that are seen."""
+    _announce(f"tree, unseen drafts, {fmt} {q_lens} of {kv_lens} {Hq}/{Hkv} page {page} {layout} {dtype}")
+    args = (q_lens, kv_lens, Hq, Hkv, page, dtype, layout)
+    x = Paged(*args, seed=sum(kv_lens)) if fmt == "plain" else Quant(fmt, *args, seed=sum(kv_lens))
+    words = _tree(q_lens, sum(q_lens))
+    row = 0
+    for s, (n, kv) in enumerate(zip(q_lens, kv_lens)):
+        for j in range(1, n, 3):
+            words[row:row + n, j // 32] &= np.uint32(~(1 << (j % 32)) & 0xFFFFFFFF)
+            at = kv - n + j
+            if at < 0:
+                continue
+            where = (int(x.table[s, at // page]), slice(None), at % page)
+            for p in (x.kp, x.vp):
+                if fmt == "plain":
+                    p[where] = float("nan") if j % 2 else float("inf")
+                else:
+                    p.view(torch.uint8)[where] = 0x7F
+            if fmt != "plain":
+                x.ks[where] = x.vs[where] = 255
+        row += n
+    out, lse = il.ilre_tree_attention(x.dev["q"], x.cache(), _dev(words), max_q=max(q_lens), max_kv=max(kv_lens), total_kv=sum(kv_lens))
+    torch.cuda.synchronize()
+    _check_tree(x, words, out, lse)
+
+
 def test_more_drafted_tokens_than_bits():
     """A sequence longer than max_q promised: what has no bit is not seen."""
     _announce("tree, too few words")
