@@ -271,12 +271,12 @@ typedef struct {
 
 /* Norms of queries and keys, each head by itself, before the rotation: y = x / sqrt(mean(x^2) + eps) * (weight + offset).  Sums are fp32 (fp64 for keys of a quantised cache), the
    result is not rounded before it is turned.  (offset 1: weights that are kept as differences from one.  A head whose squares add up to more than fp32 holds, magnitudes of 2^60 and more, comes
-   out as zeros where the sum is fp32.) */
+   out as zeros where the sum is fp32; with eps 0 one whose squares fall below what fp32 holds, magnitudes of 2^-60 and less, as infinities or NaN.) */
 typedef struct {
     int32_t struct_size;      /* sizeof(ilre_head_norms) */
     int32_t q_norm, k_norm;   /* 1: normed, 0: as they are */
     float offset;
-    double eps;               /* 0, or at least 2^-126 */
+    double eps;               /* 0, or 2^-126 .. FLT_MAX */
     const void *q_weight, *k_weight; /* dev, d elements of opts->dtype, 16-byte aligned; NULL: weight + offset is one */
 } ilre_head_norms;
 

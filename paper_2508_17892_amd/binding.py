@@ -609,6 +609,8 @@ class QuantKV(PagedKV):
                 raise ValueError(f"{name} must have the layout of the codes (a {scale}th of their strides)")
         if any(s == 0 and n > 1 for s, n in zip(k_pages.stride(), k_pages.shape)):
             raise ValueError("pages expanded over a dimension are not supported")
+        if any(t is not None and t.get_device() != k_pages.get_device() for t in (v_pages, k_scales, v_scales, page_table, kv_len, cu_q)):
+            raise ValueError("pages, scales, page_table, kv_len and cu_q are on one device")
         self.dtype = None  # of the states: any
         self.k_scales, self.v_scales = k_scales, v_scales
         q = self.quant = IlreQuantKv()
@@ -635,6 +637,10 @@ class HeadNorms:
         self.c = IlreHeadNorms(ctypes.sizeof(IlreHeadNorms), 0 if q_weight is None else 1, 0 if k_weight is None else 1, float(offset), float(eps),
                                None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
         self._ref = ctypes.byref(self.c)
+
+
+def _weights_of(norms: Optional[HeadNorms]):
+    return () if norms is None else (norms.q_weight, norms.k_weight)
 
 
 @functools.lru_cache(maxsize=256)
@@ -719,7 +725,7 @@ def ilre_norm_rope(x: torch.Tensor, freqs: Optional[IlreRopeFreqs], positions: O
     pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return out
-    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(x, out, positions))
+    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(x, out, positions, *_weights_of(norms)))
     _check(load().ilre_norm_rope(x.data_ptr(), out.data_ptr(), T, H, d, pos, n_axes, ax, int(first_position), fr, int(pairing),
                                  None if norms is None else norms._ref, _strides_ref(x0, x1, o0, o1), o))
     return out
@@ -736,7 +742,7 @@ def ilre_norm_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optiona
     pos, n_axes, ax, fr = _turn_arguments(freqs, positions, axes, T)
     if T == 0:
         return q_out
-    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(q, k, v, q_out, positions, cache.k_pages))
+    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(q, k, v, q_out, positions, cache.k_pages, *_weights_of(norms)))
     _check(load().ilre_norm_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
                                         None if v is None else v.data_ptr(), T, Hq, d, pos, n_axes, ax, fr, int(pairing),
                                         None if norms is None else norms._ref, cache._ref, st, o))

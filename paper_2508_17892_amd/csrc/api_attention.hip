@@ -1,5 +1,6 @@
 // C ABI of libilre, the operators around a recall: rotary positions, fill of a paged cache, attention.  Host code only; the kernels live in rope.hip and
 // attention.hip.
+#include <float.h>
 #include <math.h>
 
 #include "ilre_internal.h"
@@ -61,7 +62,7 @@ int check_norms(const ilre_head_norms *n)
     if (n->struct_size != (int32_t)sizeof(ilre_head_norms)) return fail(ILRE_EINVAL, "norms->struct_size %d != %zu", n->struct_size, sizeof(ilre_head_norms));
     if ((n->q_norm != 0 && n->q_norm != 1) || (n->k_norm != 0 && n->k_norm != 1)) return fail(ILRE_EINVAL, "q_norm and k_norm must be 0 or 1");
     if (!(n->eps >= 0.0) || !isfinite(n->eps)) return fail(ILRE_EINVAL, "eps must be finite and non-negative");
-    if (n->eps > 0.0 && n->eps < 1.1754943508222875e-38) return fail(ILRE_EINVAL, "eps must be 0 or at least 2^-126 (fp32 takes it for 0)");
+    if (n->eps > 0.0 && (n->eps < FLT_MIN || n->eps > FLT_MAX)) return fail(ILRE_EINVAL, "eps must be 0 or from 2^-126 to FLT_MAX (sums are fp32)");
     if (!isfinite(n->offset)) return fail(ILRE_EINVAL, "offset is not finite");
     if (((uintptr_t)n->q_weight & 15) || ((uintptr_t)n->k_weight & 15)) return fail(ILRE_EINVAL, "q_weight and k_weight must be 16-byte aligned");
     return ILRE_OK;

@@ -685,6 +685,13 @@ def test_another_device_is_refused():
         il.ilre_tree_attention(q, x.cache(), _i32(1)[None], max_q=1, max_kv=5)
     with pytest.raises(il.IlreError):
         il.ilre_tree_attention(x.dev["q"], x.cache(), _i32(1)[None], max_q=33, max_kv=5)
+    with pytest.raises(ValueError, match="device"):
+        il.ilre_norm_rope(x.dev["q"], None, norms=il.HeadNorms(torch.ones(128, dtype=torch.bfloat16, device="cuda").as_subclass(Elsewhere)))
+    for name in ("ks", "vs", "vp"):
+        x = Quant("fp8", [1], [5], 8, 2, 16, "bf16")
+        setattr(x, name, getattr(x, name).as_subclass(Elsewhere))
+        with pytest.raises(ValueError, match="device"):
+            x.cache()
 
 
 def test_a_request_over_a_quantised_cache():

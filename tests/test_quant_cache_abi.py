@@ -101,7 +101,7 @@ def test_cache_description(kw, status):
 
 
 def test_norms_axes_and_positions():
-    for kw in (dict(norms=_norms(struct_size=8)), dict(norms=_norms(q_norm=2)), dict(norms=_norms(k_norm=-1)), dict(norms=_norms(eps=-1e-6)), dict(norms=_norms(eps=float("nan"))), dict(norms=_norms(eps=1e-40)),
+    for kw in (dict(norms=_norms(struct_size=8)), dict(norms=_norms(q_norm=2)), dict(norms=_norms(k_norm=-1)), dict(norms=_norms(eps=-1e-6)), dict(norms=_norms(eps=float("nan"))), dict(norms=_norms(eps=1e-40)), dict(norms=_norms(eps=1e39)),
                dict(norms=_norms(eps=float("inf"))), dict(norms=_norms(offset=float("inf"))), dict(norms=_norms(q_weight=FAKE + 8)), dict(norms=_norms(k_weight=FAKE + 2)),
                dict(n_axes=0), dict(n_axes=-1), dict(n_axes=3), dict(n_axes=3, positions=FAKE), dict(n_axes=3, axes=_axes(*[0] * 32)),
                dict(n_axes=3, positions=FAKE, axes=_axes(*[0] * 31, 3)), dict(axes=_axes(1, *[0] * 31)), dict(positions=FAKE + 2),
