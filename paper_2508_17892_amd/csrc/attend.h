@@ -1136,6 +1136,18 @@ __device__ __forceinline__ void piece_to_numbers(const u32x4 &w, float scale, u3
     }
 }
 
+// 16 bytes of codes.  LAST: nobody reads their cache line again (the instruction's lanes take it whole, or what is left of it), so that it need not stay in L2.
+template <bool LAST>
+__device__ __forceinline__ u32x4 load_codes(const unsigned char *p)
+{
+    return LAST ? __builtin_nontemporal_load((const u32x4 *)p) : *(const u32x4 *)p;
+}
+template <bool LAST>
+__device__ __forceinline__ u32x4 load_codes(__amdgpu_buffer_rsrc_t from, unsigned at)
+{
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, LAST ? 2 : 0));
+}
+
 // Workgroups go to the XCDs in turn.  With 4 bits the kv heads of a unit go to the same one: where a token's heads lie side by side, two heads' codes share a cache line, which then comes to one
 // L2 and not to two (a million tokens in that layout 369 -> 261 us, 48 requests 38.5 -> 31.2; with a layout by heads 197 either way).  8-bit codes fill their lines, and a kv head an XCD is the better
 // way (444 us, together 465; 48 requests 48.3 and 48.8).
@@ -1150,7 +1162,9 @@ __device__ __forceinline__ int unit_of_block(const AttnArgs &a)
     return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD / a.Hkv * kNumXCD + blockIdx.x % kNumXCD : blockIdx.x / a.Hkv;
 }
 
-template <int FMT, int WAVES, bool TREE>
+// ONCE: one workgroup reads a cache line of codes, and no other does: there is one block of rows, and no line holds codes of two heads.  Without a place in L2 for each of them, one token over a million in 8 bits
+// 359 -> 323 us, in 4 198 -> 186; 48 requests, heads side by side, 48.4 -> 43.8 in 8 bits.  In 4 bits such heads share lines, which then have to stay: 261 us, with ONCE 283.
+template <int FMT, int WAVES, bool TREE, bool ONCE>
 __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
 {
     using E = Elem<ILRE_BF16>;
@@ -1215,7 +1229,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
             scales = k_scales + skip / ILRE_KV_BLOCK;
         }
 #pragma unroll
-        for (int j = 0; j < K::N; ++j) c.w[j] = *(const u32x4 *)(codes + k_lane + 16 * j);
+        for (int j = 0; j < K::N; ++j) c.w[j] = j < K::N - 1 ? load_codes<false>(codes + k_lane + 16 * j) : load_codes<ONCE>(codes + k_lane + 16 * j);
         c.scales = *(const unsigned *)(scales + k_lane_scales);
     };
     // Rows first .. of the tile, N of them at most, which follow each other in memory from `at` (of row 0) on.
@@ -1235,7 +1249,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
                 const int t = tok + j * V::ROWS + v_row;
                 if (t < blk.lo && t >= blk.sink) from = scale_from = ~0u;
             }
-            c.w[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)from, 0, 0));
+            c.w[j] = load_codes<ONCE>(codes, from);
             c.scale[j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_from, 0, 0);
         }
     };
@@ -1346,7 +1360,7 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], u32x4 (&part)[3
         }
 }
 
-template <int DT, int FMT, int WAVES, bool TREE>
+template <int DT, int FMT, int WAVES, bool TREE, bool ONCE>
 __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) void attend_codes16(const AttnArgs a)
 {
     constexpr int PARTS = DT == ILRE_F32 ? 3 : 1;  // of queries and weights
@@ -1398,7 +1412,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4
             const int64_t at = place(tok + 16 * b, p.id[b]);
             const unsigned char *codes = k_codes + code_bytes<FMT>(at), *scales = k_scales + at / ILRE_KV_BLOCK;
 #pragma unroll
-            for (int j = 0; j < KN; ++j) c.w[b][j] = *(const u32x4 *)(codes + k_lane + 16 * j);
+            for (int j = 0; j < KN; ++j) c.w[b][j] = j < KN - 1 ? load_codes<false>(codes + k_lane + 16 * j) : load_codes<ONCE>(codes + k_lane + 16 * j);
             c.scale[b] = scales[k_lane_scales];
         }
     };
@@ -1422,7 +1436,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4
                     const int t = t0 + j * V::ROWS + v_row;
                     if (t < blk.lo && t >= blk.sink) from = scale_from = ~0u;
                 }
-                c.w[b * (V::N / 2) + j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)from, 0, 0));
+                c.w[b * (V::N / 2) + j] = load_codes<ONCE>(codes, from);
                 c.scale[b * (V::N / 2) + j] = __builtin_amdgcn_raw_buffer_load_b8(scales, (int)scale_from, 0, 0);
             }
         }
@@ -1729,13 +1743,28 @@ hipError_t launch_rows(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
     return launch(attend_rows<DT, WAVES, TS, TN, PAGED, FMT, TREE>, p, WAVES * 64, 2 * Elem<DT>::RING * TN * Elem<DT>::ROWB + 16 + (TS == 2 ? WAVES * 32 * sizeof(float2) : 0), a, s);
 }
 
+// Whether a workgroup is the only reader of the cache lines that it reads codes from.  (bf16 states come to the kernels for few rows with one block of rows a sequence.)
+template <int DT, int FMT>
+bool read_once(const AttnPlan &p, const AttnArgs &a)
+{
+    return (DT == ILRE_BF16 || p.one_block) && (FMT == ILRE_KV_FP8 || a.k_token == ILRE_HEAD_DIM);
+}
+
 template <int DT, int WAVES, bool PAGED, int FMT, bool TREE>
 hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
     if constexpr (FMT != kPlain)
-        return launch(attend_codes<FMT, WAVES, TREE>, p, WAVES * 64, WAVES * (32 * kHeadDim * 4 + 32 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
+        return launch(read_once<DT, FMT>(p, a) ? attend_codes<FMT, WAVES, TREE, true> : attend_codes<FMT, WAVES, TREE, FMT == ILRE_KV_FP8>, p, WAVES * 64,
+                      WAVES * (32 * kHeadDim * 4 + 32 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
     else
         return launch(attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
+}
+
+template <int DT, int FMT, bool TREE>
+hipError_t launch_codes16(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
+{
+    return launch(read_once<DT, FMT>(p, a) ? attend_codes16<DT, FMT, 4, TREE, true> : attend_codes16<DT, FMT, 4, TREE, DT == ILRE_BF16 && FMT == ILRE_KV_FP8>, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s,
+                  FMT == ILRE_KV_FP4 ? kNumXCD : 1);
 }
 
 template <bool PAGED, int FMT = kPlain, bool TREE = false>
@@ -1744,9 +1773,7 @@ hipError_t launch_kernels(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
     hipError_t e;
     if constexpr (FMT != kPlain) {
         if (p.rows == 16) {
-            constexpr size_t lds = 4 * (32 * 256 + 16 * sizeof(float2));
-            constexpr unsigned step = FMT == ILRE_KV_FP4 ? kNumXCD : 1;
-            e = p.dtype == ILRE_BF16 ? launch(attend_codes16<ILRE_BF16, FMT, 4, TREE>, p, 256, lds, a, s, step) : launch(attend_codes16<ILRE_F32, FMT, 4, TREE>, p, 256, lds, a, s, step);
+            e = p.dtype == ILRE_BF16 ? launch_codes16<ILRE_BF16, FMT, TREE>(p, a, s) : launch_codes16<ILRE_F32, FMT, TREE>(p, a, s);
             if (e != hipSuccess || p.nsplit == 1) return e;
             return p.dtype == ILRE_BF16 ? launch_merge<ILRE_BF16, PAGED>(p, a, s) : launch_merge<ILRE_F32, PAGED>(p, a, s);
         }

@@ -49,6 +49,7 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
         cut(256, 64);
         if (rows <= 128 || ((int64_t)p.nblocks * Hkv < kNumCU && tiles(max_kv) <= 24)) cut(128, 64);
     }
+    p.one_block = rows <= p.rows;
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
     const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);

@@ -300,6 +300,7 @@ struct AttnArgs {
 // split_tiles tiles a block.
 struct AttnPlan {
     int dtype, rows, tile, nblocks, nsplit, split_tiles;
+    bool one_block;  // of rows a sequence, as promised
     size_t bytes;  // of workspace
 };
 
