@@ -179,7 +179,7 @@ int run(ilre::AttnArgs &a, int format, const ilre_attn *t, const ilre_opts *o)
     if (o->workspace && ((uintptr_t)o->workspace & 255)) return fail(ILRE_EINVAL, "workspace must be 256-byte aligned");
     if (a.T == 0) return ILRE_OK;
     const ilre::AttnPlan p = ilre::make_attn_plan(o->dtype, format, a.tree != nullptr, a.T, a.n_seq, a.Hq, a.Hkv, t->max_q, t->max_kv, t->total_kv, t->sink, t->window,
-                                                  o->workspace ? o->workspace_bytes : 0);
+                                                  o->workspace ? o->workspace_bytes : 0, format != ilre::kPlain && a.k_head == ILRE_HEAD_DIM && a.k_token > ILRE_HEAD_DIM);
     if ((int64_t)p.nblocks * a.Hkv > ilre::kMaxUnits) return fail(ILRE_EUNSUPPORTED, "too many query rows");
     const hipError_t e = ilre::launch_attention(p, a, format, o->workspace, (hipStream_t)o->stream);
     return e == hipSuccess ? ILRE_OK : hip_fail(e, "attention launch");
@@ -454,8 +454,10 @@ int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t
     if ((int64_t)Hq * T > 0x3FFFFFFF) return fail(ILRE_EUNSUPPORTED, "too many query rows");
     *out_bytes = 0;
     for (int format : {ilre::kPlain, (int)ILRE_KV_FP8, (int)ILRE_KV_FP4}) {
-        const size_t n = T == 0 ? 0 : ilre::make_attn_plan(dtype, format, false, T, n_seq, Hq, Hkv, max_q, max_kv, total_kv, 0, 0, (size_t)1 << 62).bytes;
-        if (n > *out_bytes) *out_bytes = n;
+        for (bool beside : {false, true}) {
+            const size_t n = T == 0 ? 0 : ilre::make_attn_plan(dtype, format, false, T, n_seq, Hq, Hkv, max_q, max_kv, total_kv, 0, 0, (size_t)1 << 62, beside).bytes;
+            if (n > *out_bytes) *out_bytes = n;
+        }
     }
     return ILRE_OK;
 }

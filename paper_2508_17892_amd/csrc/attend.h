@@ -1152,14 +1152,14 @@ __device__ __forceinline__ u32x4 load_codes(__amdgpu_buffer_rsrc_t from, unsigne
 // L2 and not to two (a million tokens in that layout 369 -> 261 us, 48 requests 38.5 -> 31.2; with a layout by heads 197 either way).  8-bit codes fill their lines, and a kv head an XCD is the better
 // way (444 us, together 465; 48 requests 48.3 and 48.8).
 template <int FMT>
-__device__ __forceinline__ int head_of_block(const AttnArgs &a)
+__device__ __forceinline__ int head_of_block(int heads)
 {
-    return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD % a.Hkv : blockIdx.x % a.Hkv;
+    return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD % heads : blockIdx.x % heads;
 }
 template <int FMT>
-__device__ __forceinline__ int unit_of_block(const AttnArgs &a)
+__device__ __forceinline__ int unit_of_block(int heads)
 {
-    return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD / a.Hkv * kNumXCD + blockIdx.x % kNumXCD : blockIdx.x / a.Hkv;
+    return FMT == ILRE_KV_FP4 ? blockIdx.x / kNumXCD / heads * kNumXCD + blockIdx.x % kNumXCD : blockIdx.x / heads;
 }
 
 // ONCE: one workgroup reads a cache line of codes, and no other does: there is one block of rows, and no line holds codes of two heads.  Without a place in L2 for each of them, one token over a million in 8 bits
@@ -1175,10 +1175,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    const int head = head_of_block<FMT>(a);
+    const int head = head_of_block<FMT>(a.Hkv);
     Block blk;
     int split;
-    if (!find_unit<true>(a, unit_of_block<FMT>(a), 32, TN, blk, split)) return;
+    if (!find_unit<true>(a, unit_of_block<FMT>(a.Hkv), 32, TN, blk, split)) return;
     Drafted drafted;
     if (TREE) {
         drafted.init(a, blk, blk.rows0 + l32);
@@ -1340,7 +1340,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
 
 // Up to 16 rows: the matrix instructions of 16 rows, as half of the logits, exponentials and sums above would be nobody's.  Lane l has query l % 16; tokens 16 b + 4 (l / 16) + i of
 // logits, i = 0..3, b = 0, 1; channels 16 db + 4 (l / 16) + i of sums.  Of keys it has a quarter of the codes, one block of a scale, of tokens l % 16 and 16 + l % 16.  With fewer
-// registers and half the LDS three or four workgroups fit a compute unit.
+// registers and half the LDS three or four workgroups fit a compute unit.  HEADS: kv heads a workgroup, whose wavefronts then share out the tokens of WAVES / HEADS x 32 between those of a head.
+//
+// Bound: HBM.  One token over a million (32/8 heads) 322 us in 8 bits, 6.5 TB/s, and 186 in 4, 6.0; heads side by side 350 and 227; over 4097, 8 bits, 6.8 us and 3.6 for the merge.
 //
 // Keys and values are exact in bf16, so that fp32 states take the bf16 matrix instructions too: queries and weights go in as three parts, each the rest rounded to nearest, which hold 24 bits
 // (the fp32 matrix instructions are a sixteenth as fast).
@@ -1360,19 +1362,19 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], u32x4 (&part)[3
         }
 }
 
-template <int DT, int FMT, int WAVES, bool TREE, bool ONCE>
+template <int DT, int FMT, int WAVES, bool TREE, bool ONCE, int HEADS>
 __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4 && !TREE ? 4 : 3) void attend_codes16(const AttnArgs a)
 {
     constexpr int PARTS = DT == ILRE_F32 ? 3 : 1;  // of queries and weights
     using V = ValueCodes<FMT>;
-    constexpr int ROWB = 256, PITCH = 32 * ROWB, TN = 32 * WAVES, ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM), LANES = ROW / 16, KN = ROW / 64;  // KN: 16-byte pieces of a quarter of a token
+    constexpr int ROWB = 256, PITCH = 32 * ROWB, SHARE = WAVES / HEADS, TN = 32 * SHARE, ROW = (int)code_bytes<FMT>(ILRE_HEAD_DIM), LANES = ROW / 16, KN = ROW / 64;  // KN: 16-byte pieces of a quarter of a token
     extern __shared__ __align__(16) unsigned char smem[];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g = lane >> 4;
-    const int head = head_of_block<FMT>(a);
+    const int head0 = head_of_block<FMT>(a.Hkv / HEADS) * HEADS, head = head0 + wave / SHARE;
     Block blk;
     int split;
-    if (!find_unit<true>(a, unit_of_block<FMT>(a), 16, TN, blk, split)) return;
+    if (!find_unit<true>(a, unit_of_block<FMT>(a.Hkv / HEADS), 16, TN, blk, split)) return;
     Drafted drafted;
     if (TREE) {
         drafted.init(a, blk, blk.rows0 + l16);
@@ -1380,7 +1382,7 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4
     }
     const int nsp = ranges_of(blk.nt, a.split_tiles, a.nsplit);
     const int first = split * a.split_tiles, count = (split == nsp - 1 ? blk.nt : first + a.split_tiles) - first;
-    auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave * 32; };
+    auto token_of = [&](int i) { return tile_token(blk, first + i, TN) + wave % SHARE * 32; };
 
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * PITCH;
     // the kv head's codes and scales, and the lane's places in 16 or 32 tokens of them that follow each other
@@ -1579,33 +1581,36 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_F32 ? 2 : FMT == ILRE_KV_FP4
     if (g == 0) stats[wave * 16 + l16] = make_float2(m, z);
     __syncthreads();
     const int row = tid >> 4, part = tid & 15;
-    float2 ms[WAVES];
-    float top = kFloor, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        ms[w] = stats[w * 16 + row];
-        top = fmaxf(top, ms[w].x);
-    }
-    f32x4 x[2] = {f32x4{}, f32x4{}};
+    for (int h = 0; h < HEADS; ++h) {
+        float2 ms[SHARE];
+        float top = kFloor, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        const float f = exp2_fast(ms[w].x - top);
-        sum = fmaf(ms[w].y, f, sum);
+        for (int w = 0; w < SHARE; ++w) {
+            ms[w] = stats[(h * SHARE + w) * 16 + row];
+            top = fmaxf(top, ms[w].x);
+        }
+        f32x4 x[2] = {f32x4{}, f32x4{}};
 #pragma unroll
-        for (int k = 0; k < 2; ++k) x[k] += *piece(w, row, 2 * part + k) * f;
+        for (int w = 0; w < SHARE; ++w) {
+            const float f = exp2_fast(ms[w].x - top);
+            sum = fmaf(ms[w].y, f, sum);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) x[k] += *piece(h * SHARE + w, row, 2 * part + k) * f;
+        }
+        const Target t = target_of(a, blk, head0 + h, blk.rows0 + row, nsp == 1, split, top, sum);
+        if (!t.real) return;
+        x[0] *= t.f;
+        x[1] *= t.f;
+        if (t.direct && DT == ILRE_BF16) {
+            *(uint4 *)(t.out + part * 16) = make_uint4(pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]), pack_bf16(x[1][2], x[1][3]));
+        } else {
+            f32x4 *to = (f32x4 *)(t.direct ? (float *)t.out : a.part_o + t.row * kHeadDim) + part * 2;
+            to[0] = x[0];
+            to[1] = x[1];
+        }
+        store_sum(a, t, part);
     }
-    const Target t = target_of(a, blk, head, blk.rows0 + row, nsp == 1, split, top, sum);
-    if (!t.real) return;
-    x[0] *= t.f;
-    x[1] *= t.f;
-    if (t.direct && DT == ILRE_BF16) {
-        *(uint4 *)(t.out + part * 16) = make_uint4(pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]), pack_bf16(x[1][0], x[1][1]), pack_bf16(x[1][2], x[1][3]));
-    } else {
-        f32x4 *to = (f32x4 *)(t.direct ? (float *)t.out : a.part_o + t.row * kHeadDim) + part * 2;
-        to[0] = x[0];
-        to[1] = x[1];
-    }
-    store_sum(a, t, part);
 }
 
 // ------------------------------------------------------------------------------------------------ merge of the ranges
@@ -1728,12 +1733,12 @@ hipError_t raise_lds_limit_once(const void *kernel)
 
 // units_step: the number of units is rounded up to a multiple of it.
 template <typename K>
-hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const AttnArgs &a, hipStream_t s, unsigned units_step = 1)
+hipError_t launch(K kernel, const AttnPlan &p, int threads, size_t lds, const AttnArgs &a, hipStream_t s, unsigned units_step = 1, int heads = 1)
 {
     const hipError_t e = raise_lds_limit_once((const void *)kernel);
     if (e != hipSuccess) return e;
     const unsigned units = ((unsigned)p.nsplit * p.nblocks + units_step - 1) / units_step * units_step;
-    hipLaunchKernelGGL(kernel, dim3(units * a.Hkv), dim3(threads), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(units * (a.Hkv / heads)), dim3(threads), lds, s, a);
     return hipGetLastError();
 }
 
@@ -1763,8 +1768,12 @@ hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 template <int DT, int FMT, bool TREE>
 hipError_t launch_codes16(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
 {
-    return launch(read_once<DT, FMT>(p, a) ? attend_codes16<DT, FMT, 4, TREE, true> : attend_codes16<DT, FMT, 4, TREE, DT == ILRE_BF16 && FMT == ILRE_KV_FP8>, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s,
-                  FMT == ILRE_KV_FP4 ? kNumXCD : 1);
+    auto go = [&](auto kernel, int heads) { return launch(kernel, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1, heads); };
+    if constexpr (DT == ILRE_BF16 && !TREE) {
+        if (p.heads == 4) return go(attend_codes16<DT, FMT, 4, TREE, FMT == ILRE_KV_FP8, 4>, 4);
+        if (FMT == ILRE_KV_FP8 && p.heads == 2) return go(attend_codes16<DT, ILRE_KV_FP8, 4, TREE, true, 2>, 2);
+    }
+    return read_once<DT, FMT>(p, a) ? go(attend_codes16<DT, FMT, 4, TREE, true, 1>, 1) : go(attend_codes16<DT, FMT, 4, TREE, DT == ILRE_BF16 && FMT == ILRE_KV_FP8, 1>, 1);
 }
 
 template <bool PAGED, int FMT = kPlain, bool TREE = false>

@@ -22,10 +22,12 @@ namespace ilre {
 //     so that lists stay whole where the longest has no more tiles than a compute unit's share of all and what a merge costs, four, or five at most (128 requests of 1000 tokens: whole 56 us, in two
 //     63; one of 640: whole 9.4, single tiles 10.5; four of 1000: single tiles 10.7, whole 13.6). What is cut makes two ranges a compute unit (48 requests of 1 to 16384 tokens, 4 kv heads:
 //     ranges of 12 tiles 47.0 us, 10 53.0, 7 50.3; 65536 tokens, 8 kv heads: 8 33.7, 6 36.3; 262144: 32 102.7, 22 106.8).
-AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
+AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace,
+                        bool beside)
 {
     AttnPlan p{};
     p.dtype = dtype;
+    p.heads = 1;
     const int64_t G = Hq / Hkv, rows = (int64_t)max_q * G;
     if (total_kv <= 0) total_kv = (int64_t)n_seq * max_kv;
     auto cut = [&](int block, int tile) {
@@ -41,6 +43,12 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
     };
     if (format != kPlain && (rows <= 16 || dtype == ILRE_F32)) {
         cut(16, 128);
+        // Heads that lie side by side: a workgroup takes two or four of them, as 128 bytes here and there are read more slowly than what follows each other (one token, 8 kv heads, 8 bits: 131072
+        // tokens 67 us with one, 61 with two, 60 with four, 524288 231, 203 and 190; 4 bits 524288 142, 137 and 128, 131072 44, 44 and 44).  It cuts sequences into more ranges: not where a
+        // workgroup's share is short (8 bits, 16384 tokens 17.3, 18.0 and 20.9) or few lists are cut into very many ranges (131072 tokens of 4 kv heads 35.9, 37.5 and 38.3).
+        const int64_t lists = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq)) * Hkv, share = lists * tiles(total_kv / n_seq) / (2 * kNumCU);
+        if (beside && dtype == ILRE_BF16 && !tree) p.heads = share >= 32 && Hkv % 4 == 0 && lists >= 8 ? 4 : format == ILRE_KV_FP8 && share >= 8 && Hkv % 2 == 0 && lists >= 8 ? 2 : 1;
+        cut(16, 128 / p.heads);
     } else if (rows <= 32) {
         cut(32, 128);
     } else if (dtype == ILRE_F32) {
@@ -52,7 +60,7 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
     p.one_block = rows <= p.rows;
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
-    const int64_t work = std::max<int64_t>(blocks * Hkv * tiles(total_kv / n_seq), 1);
+    const int64_t work = std::max<int64_t>(blocks * (Hkv / p.heads) * tiles(total_kv / n_seq), 1);
     const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
     const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
     int64_t per = std::max<int64_t>((work + places - 1) / places, least);
@@ -60,7 +68,7 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
         per = work / (2 * kNumCU) >= 12 ? per : std::max<int64_t>((work + kNumCU - 1) / kNumCU, work <= kNumCU ? 1 : 2);
         if (most <= (work < kNumCU ? 3 : work / kNumCU + 4)) per = most;
     } else if (p.rows == 16) {
-        const int64_t lists = blocks * Hkv, mean = tiles(total_kv / n_seq);
+        const int64_t lists = blocks * (Hkv / p.heads), mean = tiles(total_kv / n_seq);
         auto units = [&](int64_t x) { return most == mean ? lists * ((most + x - 1) / x) : lists * (2 * mean + x) / (2 * x); };  // lists of unlike lengths end with half a range each
         per = std::max<int64_t>(work <= kNumCU ? 1 : 2, work / (2 * kNumCU));
         if (most <= std::max<int64_t>(5, work / kNumCU + 4))

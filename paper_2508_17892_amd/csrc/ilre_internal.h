@@ -301,13 +301,15 @@ struct AttnArgs {
 struct AttnPlan {
     int dtype, rows, tile, nblocks, nsplit, split_tiles;
     bool one_block;  // of rows a sequence, as promised
+    int heads;       // kv heads a workgroup
     size_t bytes;  // of workspace
 };
 
 // Most workgroups of a launch (a dimension counts threads in 32 bits, and no workgroup here has more than 512).
 constexpr int64_t kMaxUnits = (int64_t)1 << 22;
 
-AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace);
+AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace,
+                        bool beside = false);  // beside: a token's kv heads follow each other in memory
 // The same for a cache of the states' own type and no tree.
 inline AttnPlan make_attn_plan(int dtype, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace)
 {

@@ -93,6 +93,41 @@ def test_attention(fmt, q_lens, kv_lens, Hq, Hkv, page, layout, dtype, mask):
         x.check(*x.attend(workspace=ws, **mask), **mask)
 
 
+# Heads side by side, and so much work (as promised; it goes into how a call is cut up, not into what comes out) that a workgroup takes several.
+BESIDE = [
+    # format (1: 8 bits), q_lens, kv_lens, Hq, Hkv, page, mask, longest and total promised, heads a workgroup
+    (1, [1], [5000], 8, 8, 64, {}, 70000, 70000, 2),
+    (1, [2, 1, 0, 4], [700, 1031, 9, 64], 16, 4, 16, {}, 300000, 300000, 2),
+    (1, [1, 3] * 64, [500, 100, 45, 3] * 32, 16, 8, 32, dict(sink=4, window=300), 700, 128 * 700, 2),
+    (1, [1] * 70, [300, 17, 1, 0, 95, 512, 33] * 10, 12, 6, 16, {}, 512, 400000, 2),           # whole
+    (1, [1], [9000], 32, 8, 64, {}, 1000000, 1000000, 4),
+    (1, [2, 1, 0, 4], [700, 1031, 9, 64], 16, 4, 16, {}, 1000000, 4000000, 4),
+    (1, [1] * 150, [300, 17, 1] * 50, 16, 8, 16, {}, 300, 300 * 1000, 4),
+    (2, [1], [9000], 32, 8, 64, {}, 1000000, 1000000, 4),
+    (2, [3, 1, 0, 4], [700, 1031, 9, 64], 12, 4, 16, {}, 1000000, 4000000, 4),
+    (2, [1] * 150, [300, 17, 1] * 50, 16, 8, 16, {}, 300, 300 * 1000, 4),
+]
+
+
+@pytest.mark.parametrize("fmt,q_lens,kv_lens,Hq,Hkv,page,mask,most,total,heads", BESIDE)
+def test_several_heads_a_workgroup(fmt, q_lens, kv_lens, Hq, Hkv, page, mask, most, total, heads):
+    _announce(f"quantised, {heads} heads a workgroup, format {fmt} {len(q_lens)} sequences {Hq}/{Hkv} page {page} {mask}")
+    x = Quant({1: "fp8", 2: "fp4"}[fmt], q_lens, kv_lens, Hq, Hkv, page, "bf16", "token", seed=sum(kv_lens))
+    run = lambda **kw: il.ilre_paged_attention(x.dev["q"], x.cache(), max_q=max(q_lens), max_kv=most, total_kv=total, **mask, **kw)  # noqa: E731
+    out, lse = run()
+    torch.cuda.synchronize()
+    x.check(out, lse, **mask)
+    again, lse2 = run()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    x.check(*run(workspace=torch.empty(0, dtype=torch.uint8, device="cuda")), **mask)
+    if len(q_lens) == 1:
+        absent = [np.zeros(kv_lens[0], bool)]
+        for col in (0, 3, kv_lens[0] // page):
+            x.dev["table"][0, col] = -1
+            absent[0][col * page:col * page + page] = True
+        x.check(*run(), absent=absent, **mask)
+
+
 @pytest.mark.parametrize("q_len,mask", [(1, {}), (50, {}), (200, {}), (200, dict(sink=4, window=64)), (1, dict(sink=20, window=64))])
 @pytest.mark.parametrize("fmt,dtype", [("fp8", "bf16"), ("fp4", "bf16"), ("fp8", "f32")])
 def test_entries_that_name_no_page(q_len, mask, fmt, dtype):
