@@ -8,12 +8,16 @@
 //
 // Queries and caches of the states' own type: fp32 (the angle's fraction of a turn in fp64).  Keys of a quantised cache: fp64 throughout, fp64 sines and cosines too, and one rounding, to the code.  A
 // code's border is met by one key in 2^19 or so if the key itself is off by 2^-24, and then what a cache holds depends on the order of operations of whoever fills it.
+//
+// Bound: HBM where tokens are many (65539 of 28/4 heads into 8 bits 218 us, 5.2 TB/s), otherwise the chain of loads from cu_q to the page, sines and stores (8 tokens 5.5 us, 1028 of 32/8 heads 9.6).
 #include "kv_codes.h"
 
 #include <type_traits>
 
 namespace ilre {
 namespace {
+
+typedef __attribute__((ext_vector_type(4))) unsigned words4;
 
 constexpr int kThreads = 256;
 // Where the other channel of a pair is: with the same lane (half-split pairing over all 128 channels), anywhere (half-split over fewer), next to it.
@@ -32,6 +36,12 @@ struct Eight {  // channels, as they lie in memory
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) ((uint4 *)p)[i] = v[i];
+    }
+    // What is written is more than the L2s hold: it takes no place there.
+    __device__ __forceinline__ void store_past(unsigned char *p) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_nontemporal_store(__builtin_bit_cast(words4, v[i]), (words4 *)p + i);
     }
     __device__ __forceinline__ void choose(bool mine, const Eight &o)
     {
@@ -328,7 +338,12 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
         if (h < nq) {
             unsigned char *to = a.q_out + (int64_t)token * a.out_token + h * a.out_head;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) x.x[s].store(to + from[s] * ES);
+            for (int s = 0; s < 2; ++s) {
+                if (WPT == 1)
+                    x.x[s].store_past(to + from[s] * ES);
+                else
+                    x.x[s].store(to + from[s] * ES);
+            }
         }
     }
     if (step >= steps || cell < 0) return;
@@ -439,7 +454,8 @@ template <int DT, int FMT, int PAIR>
 hipError_t launch(const FillArgs &a, hipStream_t s)
 {
     // A token's heads go to several wavefronts while there are not tokens for all of them: eight up to 512 tokens (32/8 heads, 8 bits; a step of 8 heads each: 8 tokens 6.4 -> 5.4 us, 512 8.5 -> 7.9,
-    // but 1028 12.2 -> 15.8), four up to a few thousand; many tokens have one each, so that sines and weights are worked out once.
+    // but 1028 12.2 -> 15.8), four up to a few thousand; many tokens have one each, so that sines and weights are worked out once.  Their queries, and what is read back of
+    // many, are written past the L2s (65539 tokens of 28/4 heads stored in 8 bits and read back 271 -> 256 us, a million keys read back 607 -> 568).
     if (a.T <= 512)
         hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 8>), dim3((unsigned)a.T), dim3(512), 0, s, a);
     else if (a.T < 4096)
@@ -466,7 +482,8 @@ hipError_t launch_format(const FillArgs &a, int format, int pairing, hipStream_t
 
 // ------------------------------------------------------------------------------------------------ reading a cache back
 
-// Rows (token, head) with eight lanes each, which have the channels that they have above; ITEMS rows a lane, whose loads are under way together.  One pass, HBM.
+// Rows (token, head) with eight lanes each, which have the channels that they have above; ITEMS rows a lane, whose loads are under way together.  One pass, HBM: a million keys of 8 kv heads
+// out of 8 bits 568 us, 5.5 TB/s.
 template <int DT, int FMT, int ITEMS>
 __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int rows_first)
 {
@@ -553,7 +570,10 @@ __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a, int ro
             }
             r.x.put(f);
         }
-        r.x.store(to);
+        if (ITEMS > 1)
+            r.x.store_past(to);
+        else
+            r.x.store(to);
     };
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -581,7 +601,7 @@ hipError_t launch_read_items(const ReadArgs &a, hipStream_t s)
     const int rows_first = a.k_out ? a.k_token < a.k_head : a.v_token < a.v_head;
     const int64_t each = kThreads / 8;
     // Four rows a lane where there are many, one where what counts is how soon the first arrive (8 kv heads: 4100 tokens 10.4 -> 8.0 us with one, 16000 25.0 -> 24.4, 131072 158 -> 162, a
-    // million's keys 606 -> 854).
+    // million's keys 568, with one row 854).
     if (items <= 1 << 18)
         hipLaunchKernelGGL((read_kernel<DT, FMT, 1>), dim3((unsigned)((items + each - 1) / each)), dim3(kThreads), 0, s, a, rows_first);
     else
