@@ -158,7 +158,7 @@ __device__ __forceinline__ int page_of(const AttnArgs &a, const Block &b, int to
 // One wavefront's share of a tile, from its first token `tok` on: ROWS rows of ROWB bytes to LDS address `to`, 16-byte chunk c of a row at place
 // c ^ swizzle(row).  Rows that no row of the block sees (past hi, between sink and lo, on no page) are written as zeros: what lies there may
 // be anything, and 0 * NaN is no 0.  Always the same number of copies, so that they can be waited for by count.
-template <int ROWS, int ROWB, bool VALUES, bool PAGED>
+template <int ROWS, int ROWB, bool VALUES, bool PAGED, bool ONCE = false>
 __device__ __forceinline__ void copy_rows(const AttnArgs &a, const Block &b, const Source &src, int tok, int page, unsigned to, const int (&voff)[ROWS * ROWB / 1024],
                                           int lane)
 {
@@ -179,7 +179,12 @@ __device__ __forceinline__ void copy_rows(const AttnArgs &a, const Block &b, con
     const bool gap = __builtin_amdgcn_readfirstlane(tok < b.lo && tok + ROWS > b.sink);
     if (!gap) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) lds_dma16(rsrc, __builtin_amdgcn_readfirstlane(to + j * 1024), voff[j]);
+        for (int j = 0; j < N; ++j) {
+            if constexpr (ONCE)
+                lds_dma16_past(rsrc, __builtin_amdgcn_readfirstlane(to + j * 1024), voff[j]);
+            else
+                lds_dma16(rsrc, __builtin_amdgcn_readfirstlane(to + j * 1024), voff[j]);
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -1012,7 +1017,7 @@ __device__ __forceinline__ void join_waves(const AttnArgs &a, const Block &blk, 
 // tile buffers of its own and no barrier on the way; what they have is added up at the end.  One buffer each for keys and values (the next keys are asked for
 // when these have become logits) and two workgroups a compute unit: a workgroup's start is 3 us of dependent loads, and the other one reads meanwhile.
 // Two buffers each and one workgroup, 48 requests with 1 to 16384 tokens 96 -> 86 us, one token of 4097 15.4 -> 13.0 us, of a million 695 either way.
-template <int DT, int WAVES, bool PAGED, bool TREE = false>
+template <int DT, int WAVES, bool PAGED, bool TREE = false, bool ONCE = false>
 __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_tokens(const AttnArgs a)
 {
     using E = Elem<DT>;
@@ -1056,12 +1061,12 @@ __global__ __launch_bounds__(WAVES * 64, DT == ILRE_BF16 ? 2 : 1) void attend_to
         return p;
     };
     auto copy_keys = [&](int i, const Pages &p) {
-        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, token_of(i), p.id[0], lds0, kvoff, lane);
-        copy_rows<16, ROWB, false, PAGED>(a, blk, ks, token_of(i) + 16, p.id[1], lds0 + 16 * ROWB, kvoff, lane);
+        copy_rows<16, ROWB, false, PAGED, ONCE>(a, blk, ks, token_of(i), p.id[0], lds0, kvoff, lane);
+        copy_rows<16, ROWB, false, PAGED, ONCE>(a, blk, ks, token_of(i) + 16, p.id[1], lds0 + 16 * ROWB, kvoff, lane);
     };
     auto copy_values = [&](int i, const Pages &p) {
-        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, token_of(i), p.id[0], lds0 + SLOT, vvoff, lane);
-        copy_rows<16, ROWB, true, PAGED>(a, blk, vs, token_of(i) + 16, p.id[1], lds0 + SLOT + 16 * ROWB, vvoff, lane);
+        copy_rows<16, ROWB, true, PAGED, ONCE>(a, blk, vs, token_of(i), p.id[0], lds0 + SLOT, vvoff, lane);
+        copy_rows<16, ROWB, true, PAGED, ONCE>(a, blk, vs, token_of(i) + 16, p.id[1], lds0 + SLOT + 16 * ROWB, vvoff, lane);
     };
 
     Pages now, next;
@@ -1764,7 +1769,9 @@ hipError_t launch_tokens(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
         return launch(read_once<DT, FMT>(p, a) ? attend_codes<FMT, WAVES, TREE, true> : attend_codes<FMT, WAVES, TREE, FMT == ILRE_KV_FP8>, p, WAVES * 64,
                       WAVES * (32 * kHeadDim * 4 + 32 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1);
     else
-        return launch(attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64, WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
+        // Under a tree, tiles that are many take no place in L2 (8 drafted tokens over a million 687 -> 621 us, four drafts over 32768 each 106 -> 95; where a workgroup has a few tiles 20.9 -> 21.3).
+        return launch(TREE && p.many_tiles ? attend_tokens<DT, WAVES, PAGED, TREE, TREE> : attend_tokens<DT, WAVES, PAGED, TREE>, p, WAVES * 64,
+                      WAVES * (2 * 32 * Elem<DT>::ROWB + 32 * sizeof(float2)), a, s);
 }
 
 template <int DT, int FMT, bool TREE>

@@ -61,6 +61,7 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
     const int64_t most = std::max<int64_t>(tiles(max_kv), 1);
     const int64_t blocks = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq));
     const int64_t work = std::max<int64_t>(blocks * (Hkv / p.heads) * tiles(total_kv / n_seq), 1);
+    p.many_tiles = work >= 16 * kNumCU;
     const int64_t places = (p.rows == 32) == (dtype == ILRE_BF16) ? 2 * kNumCU : kNumCU;  // what LDS has room for
     const int64_t least = p.rows == 32 ? (most <= 3 ? 3 : work <= kNumCU ? 1 : 2) : dtype == ILRE_F32 ? 2 : (int64_t)T * Hq <= 2048 ? 4 : 12;
     int64_t per = std::max<int64_t>((work + places - 1) / places, least);

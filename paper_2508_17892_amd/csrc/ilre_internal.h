@@ -24,6 +24,12 @@ __device__ __forceinline__ void lds_dma16(i32x4 rsrc, unsigned lds_addr, int vof
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voffset), "s"(rsrc)
                  : "memory", "m0");
 }
+// The same of lines that nobody reads again, which take no place in L2.
+__device__ __forceinline__ void lds_dma16_past(i32x4 rsrc, unsigned lds_addr, int voffset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds_addr), "v"(voffset), "s"(rsrc)
+                 : "memory", "m0");
+}
 // The same from an address a lane.
 __device__ __forceinline__ void lds_dma16(uint64_t src, unsigned lds_addr)
 {
@@ -302,6 +308,7 @@ struct AttnPlan {
     int dtype, rows, tile, nblocks, nsplit, split_tiles;
     bool one_block;  // of rows a sequence, as promised
     int heads;       // kv heads a workgroup
+    bool many_tiles; // eight and more for each of two workgroups a compute unit
     size_t bytes;  // of workspace
 };
 

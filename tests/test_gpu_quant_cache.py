@@ -325,6 +325,23 @@ def test_drafted_tokens_that_nobody_sees_hold_anything(fmt, q_lens, kv_lens, Hq,
     _check_tree(x, words, out, lse)
 
 
+@pytest.mark.parametrize("fmt,dtype", [("plain", "bf16"), ("plain", "f32"), ("fp8", "bf16"), ("fp4", "bf16")])
+def test_drafts_over_contexts_promised_long(fmt, dtype):
+    """(Cut up, and read, as if the contexts were far longer than they are.)"""
+    _announce(f"tree, long contexts promised, {fmt} {dtype}")
+    q_lens, kv_lens = [7, 8, 0, 5], [300, 1031, 9, 5]
+    args = (q_lens, kv_lens, 32, 8, 64, dtype, "token")
+    x = Paged(*args, seed=8) if fmt == "plain" else Quant(fmt, *args, seed=8)
+    words = _tree(q_lens, 8, blank={3})
+    run = lambda **kw: il.ilre_tree_attention(x.dev["q"], x.cache(), _dev(words), max_q=8, max_kv=400000, total_kv=800000, **kw)  # noqa: E731
+    out, lse = run()
+    torch.cuda.synchronize()
+    _check_tree(x, words, out, lse)
+    again, lse2 = run()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    _check_tree(x, words, *run(workspace=torch.empty(0, dtype=torch.uint8, device="cuda")))
+
+
 def test_more_drafted_tokens_than_bits():
     """A sequence longer than max_q promised: what has no bit is not seen."""
     _announce("tree, too few words")
