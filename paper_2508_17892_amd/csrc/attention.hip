@@ -21,7 +21,9 @@ namespace ilre {
 //   - Up to 16 rows over a quantised cache (tiles of 128 tokens): a workgroup a compute unit reads nearly as fast as HBM gives (32 requests of 1500 tokens, 8 kv heads 24.9 us whole, 25.5 in two),
 //     so that lists stay whole where the longest has no more tiles than a compute unit's share of all and what a merge costs, four, or five at most (128 requests of 1000 tokens: whole 56 us, in two
 //     63; one of 640: whole 9.4, single tiles 10.5; four of 1000: single tiles 10.7, whole 13.6). What is cut makes two ranges a compute unit (48 requests of 1 to 16384 tokens, 4 kv heads:
-//     ranges of 12 tiles 47.0 us, 10 53.0, 7 50.3; 65536 tokens, 8 kv heads: 8 33.7, 6 36.3; 262144: 32 102.7, 22 106.8).
+//     ranges of 12 tiles 47.0 us, 10 53.0, 7 50.3; 65536 tokens, 8 kv heads: 8 33.7, 6 36.3; 262144: 32 102.7, 22 106.8). No range is longer than what would stay whole: many lists make two ranges a
+//     compute unit before the longest is cut, and one workgroup would walk it (32/8 heads, 8 bits: 128 requests of 1000 tokens but one of 1000003, in one range 11.0 ms, so 0.46; but one of 131072 1450
+//     and 144 us; 28/4 heads, 512 of 30 to 30000 tokens 754 us either way, with half of that 503, which the former calls take for 494 and 166).
 AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int Hq, int Hkv, int max_q, int max_kv, int64_t total_kv, int sink, int window, size_t workspace,
                         bool beside)
 {
@@ -69,13 +71,15 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
         per = work / (2 * kNumCU) >= 12 ? per : std::max<int64_t>((work + kNumCU - 1) / kNumCU, work <= kNumCU ? 1 : 2);
         if (most <= (work < kNumCU ? 3 : work / kNumCU + 4)) per = most;
     } else if (p.rows == 16) {
-        const int64_t lists = blocks * (Hkv / p.heads), mean = tiles(total_kv / n_seq);
-        auto units = [&](int64_t x) { return most == mean ? lists * ((most + x - 1) / x) : lists * (2 * mean + x) / (2 * x); };  // lists of unlike lengths end with half a range each
-        per = std::max<int64_t>(work <= kNumCU ? 1 : 2, work / (2 * kNumCU));
-        if (most <= std::max<int64_t>(5, work / kNumCU + 4))
-            per = most;
-        else
-            while (per < most && units(per) > 2 * kNumCU) ++per;
+        const int64_t lists = blocks * (Hkv / p.heads), mean = tiles(total_kv / n_seq), whole = std::max<int64_t>(5, work / kNumCU + 4);
+        per = most <= whole ? most : std::max<int64_t>(work <= kNumCU ? 1 : 2, work / (2 * kNumCU));
+        if (per < most) {
+            // the least that makes two ranges a compute unit at most: of lists of one length 2 kNumCU / lists each, of unlike ones lists (2 mean + per) / (2 per) together, as they end with half a range each
+            int64_t enough = most;
+            if (most == mean && lists <= 2 * kNumCU) enough = (most + 2 * kNumCU / lists - 1) / (2 * kNumCU / lists);
+            if (most != mean && lists < 4 * kNumCU + 2) enough = 2 * mean * lists / (4 * kNumCU + 2 - lists) + 1;
+            per = std::min({std::max(per, enough), most, whole});
+        }
     }
     int64_t n = (most + per - 1) / per;
     const int64_t row_bytes = (int64_t)T * Hq * (kHeadDim + 1) * (int64_t)sizeof(float);
