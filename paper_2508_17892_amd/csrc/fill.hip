@@ -456,9 +456,10 @@ hipError_t launch(const FillArgs &a, hipStream_t s)
     // A token's heads go to several wavefronts while there are not tokens for all of them: eight up to 512 tokens (32/8 heads, 8 bits; a step of 8 heads each: 8 tokens 6.4 -> 5.4 us, 512 8.5 -> 7.9,
     // but 1028 12.2 -> 15.8), four up to a few thousand; many tokens have one each, so that sines and weights are worked out once.  Their queries, and what is read back of
     // many, are written past the L2s (65539 tokens of 28/4 heads stored in 8 bits and read back 271 -> 256 us, a million keys read back 607 -> 568).
-    if (a.T <= 512)
+    const int wavefronts = fill_wavefronts(a.T);
+    if (wavefronts == 8)
         hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 8>), dim3((unsigned)a.T), dim3(512), 0, s, a);
-    else if (a.T < 4096)
+    else if (wavefronts == 4)
         hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 4>), dim3((unsigned)a.T), dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL((fill_kernel<DT, FMT, PAIR, 1>), dim3((unsigned)((a.T + 3) / 4)), dim3(kThreads), 0, s, a);
@@ -602,7 +603,7 @@ hipError_t launch_read_items(const ReadArgs &a, hipStream_t s)
     const int64_t each = kThreads / 8;
     // Four rows a lane where there are many, one where what counts is how soon the first arrive (8 kv heads: 4100 tokens 10.4 -> 8.0 us with one, 16000 25.0 -> 24.4, 131072 158 -> 162, a
     // million's keys 568, with one row 854).
-    if (items <= 1 << 18)
+    if (read_rows(items) == 1)
         hipLaunchKernelGGL((read_kernel<DT, FMT, 1>), dim3((unsigned)((items + each - 1) / each)), dim3(kThreads), 0, s, a, rows_first);
     else
         hipLaunchKernelGGL((read_kernel<DT, FMT, 4>), dim3((unsigned)((items + 4 * each - 1) / (4 * each))), dim3(kThreads), 0, s, a, rows_first);

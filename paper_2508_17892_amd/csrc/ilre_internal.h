@@ -261,6 +261,8 @@ struct FillArgs {
     uint8_t axes[ILRE_HEAD_DIM / 2];
 };
 
+// How many wavefronts share a token's heads.
+inline int fill_wavefronts(int T) { return T <= 512 ? 8 : T < 4096 ? 4 : 1; }
 hipError_t launch_fill(const FillArgs &a, int dtype, int format, int pairing, hipStream_t s);
 
 struct ReadArgs {
@@ -275,6 +277,8 @@ struct ReadArgs {
     int n_seq, num_pages, page_shift;
 };
 
+// How many rows (token, head) a lane has.
+inline int read_rows(int64_t rows) { return rows <= 1 << 18 ? 1 : 4; }
 hipError_t launch_read(const ReadArgs &a, int dtype, int format, hipStream_t s);
 
 // ---------------------------------------------------------------- attention over a paged cache or packed keys and values

@@ -1,10 +1,12 @@
 """GPU parity of quantised caches, head norms and reading back where calls are large or uneven: batches with one long context, chunks of a few thousand tokens, many heads, long reads."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2508_17892_amd as il
-from test_gpu_attention import _announce
-from test_gpu_quant_cache import Quant
+from oracle import quant_cache as oq
+from test_gpu_attention import DT, Paged, _announce, _f64
+from test_gpu_quant_cache import AXES3, BASE, Quant, _near, _states, _turned, _weights
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +28,156 @@ def test_one_long_context_among_many_short_ones(fmt, dtype, layout, long_at):
     again, lse2 = x.attend()
     assert torch.equal(out, again) and torch.equal(lse, lse2)
     x.check(*x.attend(workspace=torch.empty(0, dtype=torch.uint8, device="cuda")))
+
+
+# ------------------------------------------------------------------------------------------------ filling a cache: every kernel, several steps of query heads
+
+# q_lens, kv_lens, Hq, Hkv, rows of no sequence (in front, behind)
+FILL_SHAPES = {
+    "few": ([1, 2, 0, 1], [1, 900, 5, 64], 64, 8, (0, 0)),             # eight wavefronts a token, one goes from queries to keys
+    "512": ([300, 212], [500, 300], 12, 3, (0, 0)),
+    "513": ([513], [513], 28, 4, (0, 0)),                              # four wavefronts
+    "chunks": ([600, 0, 423], [700, 3, 423], 28, 4, (2, 3)),
+    "chunk": ([1028], [1500], 32, 8, (0, 0)),
+    "wide": ([1028], [1028], 64, 8, (0, 1)),
+    "4095": ([4000, 95], [4000, 100], 9, 1, (0, 0)),
+    "4096": ([4096], [4100], 9, 1, (0, 0)),                            # one
+    "many": ([2500, 1700], [2500, 1800], 28, 4, (1, 2)),
+    "many, 64/8": ([4100], [4100], 64, 8, (0, 0)),
+}
+PAIRINGS = (("half", 128), ("half", 64), ("interleaved", 96))
+FILL_CALLS = [(shape, dtype, fmt, *PAIRINGS[i]) for dtype in ("bf16", "f32") for fmt in ("plain", "fp8", "fp4") for i in range(3) for shape in ("few", "chunks", "many")]
+FILL_CALLS += [(shape, "bf16", fmt, *PAIRINGS[i]) for i, fmt in enumerate(("fp8", "fp4", "plain")) for shape in ("512", "513", "chunk", "wide", "4095", "4096")]
+FILL_CALLS += [("many, 64/8", "bf16", "fp8", "half", 128), ("wide", "f32", "fp4", "half", 128)]
+
+
+def _blank(fmt, kv_lens, Hq, Hkv, page, dtype, layout):
+    """A quantised cache of such lengths with nothing in it: the tables alone are made, and pages of ones."""
+    x = Paged([0] * len(kv_lens), [0] * len(kv_lens), Hq, Hkv, page, dtype, layout)
+    need = [-(-n // page) for n in kv_lens]
+    total = sum(need) + 2
+    order = torch.randperm(total, generator=torch.Generator().manual_seed(total)).int()
+    x.table = torch.full((len(kv_lens), max(need)), -7, dtype=torch.int32)
+    for s, m in enumerate(need):
+        x.table[s, :m] = order[sum(need[:s]):sum(need[:s]) + m]
+    x.dev.update(table=x.table.cuda(), kv_len=torch.tensor(kv_lens, dtype=torch.int32).cuda())
+
+    def pages(width):
+        t = torch.ones((total, page, Hkv, width) if layout == "token" else (total, Hkv, page, width), dtype=torch.uint8, device="cuda")
+        return t.permute(0, 2, 1, 3) if layout == "token" else t
+
+    x.kp, x.vp, x.ks, x.vs = (pages(w) for w in ((128,) * 2 if fmt == "fp8" else (64,) * 2) + (4, 4))
+    if fmt == "fp8":
+        x.kp, x.vp = x.kp.view(torch.float8_e4m3fn), x.vp.view(torch.float8_e4m3fn)
+    x.cache = lambda: il.QuantKV(x.kp, x.vp, x.ks, x.vs, x.dev["table"], x.dev["kv_len"], x.dev["cu"])
+    return x
+
+
+@pytest.mark.parametrize("shape,dtype,fmt,pairing,rotary", FILL_CALLS)
+def test_fill_of_every_size(shape, dtype, fmt, pairing, rotary):
+    _announce(f"fill, {shape} {dtype} {fmt} {pairing} {rotary}")
+    q_lens, kv_lens, Hq, Hkv, (front, behind) = FILL_SHAPES[shape]
+    n, page, axes = sum(q_lens), 16, 3 if fmt != "fp4" else 1
+    T = front + n + behind
+    args = (kv_lens, Hq, Hkv, page, dtype, "token" if pairing == "half" else "head")
+    x = Paged([0] * len(kv_lens), *args, fill=0.5) if fmt == "plain" else _blank(fmt, *args)
+    x.dev["cu"] = torch.tensor([front] + list(front + np.cumsum(q_lens)), dtype=torch.int32).cuda()
+    fused = _states(T, Hq, Hkv, dtype, T + rotary)
+    q, k, v = fused[:, :Hq], fused[:, Hq:Hq + Hkv], fused[:, Hq + Hkv:]
+    qw, kw = _weights(dtype, rotary, 0)
+    f = il.ilre_rope_frequencies(rotary, BASE)
+    places = np.concatenate([np.full(front, 3)] + [np.arange(m - a, m) for a, m in zip(q_lens, kv_lens)] + [np.full(behind, 5)])
+    pos = places[None] if axes == 1 else np.stack((places, places // 7 - 20, places % 31 + 5))
+    table = (0,) * (rotary // 2) if axes == 1 else AXES3[rotary // 2]
+    dev, got = fused.cuda(), torch.full((T, Hq, 128), 9.0, dtype=DT[dtype], device="cuda")
+    before = {name: getattr(x, name).clone() for name in ("kp", "vp") + (("ks", "vs") if fmt != "plain" else ())}
+    il.ilre_norm_rope_append(dev[:, :Hq], dev[:, Hq:Hq + Hkv], dev[:, Hq + Hkv:], x.cache(), f, None if axes == 1 else torch.from_numpy(pos).int().cuda(),
+                             norms=il.HeadNorms(qw.cuda(), kw.cuda(), eps=1e-6), axes=None if axes == 1 else table, q_out=got,
+                             pairing=il.ILRE_ROPE_HALF if pairing == "half" else il.ILRE_ROPE_INTERLEAVED)
+    torch.cuda.synchronize()
+    mine = slice(front, front + n)
+    assert (got[:front] == 9).all() and (got[front + n:] == 9).all()
+    pos = pos[:, mine]
+    sizes = [np.abs(oq.norm(_f64(t[mine]), _f64(w), 1e-6)).max(-1, keepdims=True) * 2 for t, w in ((q, qw), (k, kw))]
+    _near(got[mine], _turned(q[mine], qw, pos, table, f, pairing, 0), sizes[0], dtype)
+    want_k, want_v = _turned(k[mine], kw, pos, table, f, pairing, 0), _f64(v[mine])
+    seq, places = np.repeat(np.arange(len(q_lens)), q_lens), places[mine]
+    page_at, cell = x.table[seq, places // page].long().cuda(), torch.from_numpy(places % page).cuda()
+    if fmt == "plain":
+        _near(x.kp[page_at, :, cell], want_k, sizes[1], dtype)
+        assert torch.equal(x.vp[page_at, :, cell].cpu(), v[mine])
+    else:
+        for pages, scales, want in ((x.kp, x.ks, want_k), (x.vp, x.vs, want_v)):
+            codes, sc = oq.store(want, fmt)
+            assert np.array_equal(scales[page_at, :, cell].cpu().numpy(), sc)
+            stored = pages.view(torch.uint8)[page_at, :, cell].cpu().numpy()
+            assert np.array_equal(stored, codes), (int((stored != codes).sum()), codes.size)
+    for name, old in before.items():  # nothing else was touched
+        a, b = (t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t for t in (old, getattr(x, name)))
+        a[page_at, :, cell] = b[page_at, :, cell]
+        assert torch.equal(a, b), name
+
+
+TURNS = [(1, 64), (512, 9), (600, 28), (4095, 3), (4200, 28)]
+
+
+@pytest.mark.parametrize("T,H", TURNS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_rope_of_every_size(T, H, dtype):
+    _announce(f"norm_rope {T} {H} {dtype}")
+    x = _states(T, H, 1, dtype, T)[:, :H]
+    w = _weights(dtype, T, 1)[0]
+    pos = np.stack((np.arange(T) + 1000, np.arange(T) // 24, np.arange(T) % 24 - 7))
+    for pairing, rotary in PAIRINGS:
+        f, axes = il.ilre_rope_frequencies(rotary, BASE), AXES3[rotary // 2]
+        size = np.abs(oq.norm(_f64(x), _f64(w), 1e-6, 1.0)).max(-1, keepdims=True) * 2
+        kw = dict(norms=il.HeadNorms(w.cuda(), eps=1e-6, offset=1.0), axes=axes, pairing=il.ILRE_ROPE_HALF if pairing == "half" else il.ILRE_ROPE_INTERLEAVED)
+        got = il.ilre_norm_rope(x.cuda(), f, torch.from_numpy(pos).int().cuda(), **kw)
+        _near(got, _turned(x, w, pos, axes, f, pairing, 1.0), size, dtype)
+        y = x.cuda()
+        il.ilre_norm_rope(y, f, torch.from_numpy(pos).int().cuda(), out=y, **kw)
+        assert torch.equal(y, got)
+
+
+# ------------------------------------------------------------------------------------------------ reading back: several rows a lane
+
+READ_ROWS = {
+    "few long": ([700, 0, 64, 1, 300, 0], [20000, 0, 9000, 3, 3990, 0], 8),
+    "many short": ([i % 9 for i in range(1500)], [(7 * i) % 46 for i in range(1500)], 8),
+    "one head": ([900, 33], [200000, 62300], 1),
+}
+READS = [("few long", fmt, dtype) for fmt in ("plain", "fp8", "fp4") for dtype in ("bf16", "f32")] + [("many short", "fp8", "bf16"), ("one head", "fp4", "bf16")]
+
+
+@pytest.mark.parametrize("rows,fmt,dtype", READS)
+def test_long_reads(rows, fmt, dtype):
+    _announce(f"long read, {rows} {fmt} {dtype}")
+    lens, rows, H = READ_ROWS[rows]
+    S, page = len(lens), 16
+    args = ([0] * S, lens, H, H, page, dtype, "head" if fmt == "fp8" else "token")
+    x = Paged(*args, seed=3) if fmt == "plain" else Quant(fmt, *args, seed=3)
+    x.dev["table"][0, 0] = -1  # the first sequence's first tokens are on no page
+    out_type = DT[dtype]
+    k, v = ([t.to(out_type) for t in s] for s in (x.k, x.v))
+    for t in (k, v):
+        t[0][:page] = 0
+    # every sequence's tokens, and behind them a row of zeros for those that are not there
+    begin = np.concatenate(([0], np.cumsum(np.array(lens) + 1)))[:-1]
+    k, v = (torch.cat([torch.cat((t[s], torch.zeros(1, H, 128, dtype=out_type))) for s in range(S)]) for t in (k, v))
+    T, front, behind = sum(rows), 2, 3
+    seq = np.repeat(np.arange(S), rows)
+    rng = np.random.default_rng(0)
+    lengths = np.array(lens)[seq]
+    last = lengths - np.array(rows)[seq] + np.arange(T) - np.concatenate(([0], np.cumsum(rows)))[seq]
+    for tokens in (rng.integers(-3, lengths + 5), None):
+        at = last if tokens is None else tokens
+        where = torch.from_numpy(begin[seq] + np.where((at >= 0) & (at < lengths), at, lengths))
+        x.dev["cu"] = torch.tensor([front] + list(front + np.cumsum(rows)), dtype=torch.int32).cuda()
+        given = None if tokens is None else torch.from_numpy(np.concatenate((np.zeros(front), tokens, np.zeros(behind)))).int().cuda()
+        for layout in ("token", "head"):
+            out = [torch.full((T + front + behind, H, 128) if layout == "token" else (H, T + front + behind, 128), 9.0, dtype=out_type, device="cuda") for _ in range(2)]
+            view = out if layout == "token" else [t.transpose(0, 1) for t in out]
+            il.ilre_cache_read(x.cache(), T + front + behind, given, k_out=view[0], v_out=view[1])
+            torch.cuda.synchronize()
+            for got, states in zip(view, (k, v)):
+                assert torch.equal(got[front:front + T].cpu(), states[where]) and (got[:front] == 9).all() and (got[front + T:] == 9).all()

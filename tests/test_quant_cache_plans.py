@@ -66,6 +66,29 @@ def test_the_gpu_tests_have_a_long_context_that_is_cut(plans):
     assert all(rows == 16 and ranges > 4 for rows, _, ranges, _ in got), got
 
 
+def test_the_gpu_tests_reach_every_kernel_of_fill_and_read(plans):
+    """A fill kernel is one for the states' type, the cache's, where the other channel of a pair is, and how many wavefronts share a token; a read kernel for the types and how many rows a lane has."""
+    import test_gpu_quant_cache_long as long
+
+    def kernels(tokens, rows):
+        got = subprocess.run([os.path.join(ROOT, "_build", "sanitize", "attn_plan_driver"), "fill"], input="".join(f"{t} {r}\n" for t, r in zip(tokens, rows)),
+                             capture_output=True, text=True, timeout=60, check=True).stdout
+        return [tuple(map(int, line.split())) for line in got.split("\n")[:-1]]
+
+    types = [(dtype, fmt) for dtype in ("bf16", "f32") for fmt in ("plain", "fp8", "fp4")]
+    where = lambda pairing, rotary: "next" if pairing == "interleaved" else "lane" if rotary == 128 else "elsewhere"  # noqa: E731
+    calls = [(dtype, fmt, where(pairing, rotary), sum(long.FILL_SHAPES[shape][0])) for shape, dtype, fmt, pairing, rotary in long.FILL_CALLS]
+    reached = {(*c[:3], n) for c, (n, _) in zip(calls, kernels([c[3] for c in calls], [1] * len(calls)))}
+    assert not {(*t, w, n) for t in types for w in ("lane", "elsewhere", "next") for n in (8, 4, 1)} - reached
+    assert [n for n, _ in kernels([512, 513, 4095, 4096], [1] * 4)] == [8, 4, 4, 1] and {512, 513, 4095, 4096} <= {c[3] for c in calls}
+    heads = {(long.FILL_SHAPES[shape][2], long.FILL_SHAPES[shape][3]) for shape, *_ in long.FILL_CALLS}
+    assert {(28, 4), (32, 8), (64, 8)} <= heads  # several steps of eight query heads, a last one that is not full, and more than a token's wavefronts
+    calls = [(dtype, fmt, sum(long.READ_ROWS[r][1]) * long.READ_ROWS[r][2]) for r, fmt, dtype in long.READS]
+    reached = {(dtype, fmt) for (dtype, fmt, _), (_, n) in zip(calls, kernels([1] * len(calls), [c[2] for c in calls])) if n == 4}
+    assert reached == set(types)
+    assert kernels([1] * 3, [777 * 2, 1 << 18, (1 << 18) + 1]) == [(8, 1), (8, 1), (8, 4)]  # (the other reads of the tests: one row a lane)
+
+
 def test_a_plan_takes_no_time(plans):
     """(A search tile by tile took 27 us for a million tokens, 55 ms for two thousand million.)"""
     calls = [(1, 0, 1, 128, 128, 32, 8, 1, longest, longest + 127 * 1000, 0, 0, 0) for longest in (1000003, 100000000, 2000000000)] * 20
