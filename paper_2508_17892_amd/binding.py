@@ -681,11 +681,10 @@ def ilre_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[tor
     T, Hq, d, dt, q_out, st = _append_arguments(q, k, v, cache, q_out)
     if T == 0:
         return q_out
-    o = _opts(dt, 0, 0.0, ILRE_SCORE_SUM, None)
+    pos = None if positions is None else _int32_vector("positions", positions, T)
+    o = _call_opts_ref(dt, 0.0, 0, 0, _stream_of(q, k, v, q_out, positions, cache.k_pages))
     _check(load().ilre_rope_append(None if q is None else q.data_ptr(), None if q is None else q_out.data_ptr(), k.data_ptr(),
-                                   None if v is None else v.data_ptr(), T, Hq, d,
-                                   None if positions is None else _int32_vector("positions", positions, T), ctypes.byref(freqs), int(pairing),
-                                   cache._ref, st, ctypes.byref(o)))
+                                   None if v is None else v.data_ptr(), T, Hq, d, pos, ctypes.byref(freqs), int(pairing), cache._ref, st, o))
     return q_out
 
 
@@ -824,7 +823,7 @@ def ilre_paged_attention(q: torch.Tensor, cache: PagedKV, *, max_q: int, max_kv:
         raise ValueError("workspace is a contiguous device tensor")
     at = _attn_ref(1 if causal else 0, int(sink), int(window), int(max_q), int(max_kv), int(total_kv))
     st = _strides_ref(q0, q1, o0, o1)
-    o = _call_opts_ref(dt, float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _current_stream())
+    o = _call_opts_ref(dt, float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(q, out, lse, workspace, cache.k_pages))
     _check(load().ilre_paged_attention(q.data_ptr(), out.data_ptr(), lse.data_ptr(), T, Hq, d, at, cache._ref, st, o))
     return out, lse
 
