@@ -748,16 +748,21 @@ def ilre_norm_rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optiona
     return q_out
 
 
-def ilre_cache_read(cache: PagedKV, T: int, tokens: Optional[torch.Tensor] = None, *, dtype: torch.dtype = torch.bfloat16, values: bool = True,
+def ilre_cache_read(cache: PagedKV, T: int, tokens: Optional[torch.Tensor] = None, *, dtype: Optional[torch.dtype] = None, values: bool = True,
                     k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Keys and values out of a paged cache, T rows cut up by cache.cu_q: the tokens `tokens` (int32 [T]), or the last tokens of each sequence.  Returns (k_out, v_out) [T,
-    Hkv, d]; the caller's own tensors (k_out alone: keys only) may be views of the recall's key cache, k_cache.transpose(0, 1)."""
+    Hkv, d]; the caller's own tensors (k_out alone: keys only) may be views of the recall's key cache, k_cache.transpose(0, 1).  dtype: of the rows, bfloat16 (the default) or float32 out of a
+    quantised cache; a cache of the states' own type, and the caller's tensors, have theirs."""
     if k_out is None and v_out is None:
-        dt = dtype if cache.dtype is None else cache.k_pages.dtype
+        dt = (dtype or torch.bfloat16) if cache.dtype is None else cache.k_pages.dtype
+        if dtype not in (dt, None):
+            raise TypeError(f"the cache holds {dt}, not {dtype}")
         k_out = torch.empty((T, cache.Hkv, 128), dtype=dt, device=cache.k_pages.device)
         v_out = torch.empty_like(k_out) if values and cache.v_pages is not None else None
     k0 = k1 = v0 = v1 = 0
     ref = k_out if k_out is not None else v_out
+    if dtype not in (ref.dtype, None):
+        raise TypeError(f"k_out and v_out are {ref.dtype}, not {dtype}")
     dt = _dtype_code(ref)
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         if t is None:
