@@ -52,16 +52,28 @@ def norm(x, weight, eps, offset=0.0):
     return x / np.sqrt((x ** 2).mean(-1, keepdims=True) + eps) * w
 
 
+def angle(positions, inv_freq):
+    """(cosine, sine) in fp64 of the products positions * inv_freq as they are, not rounded to fp64: at position 2^30 that would be 2^-24 of an angle's turn.  Each product in two parts, exact in a float of
+    64 bits: positions of 31 bits times the upper 32 and the lower 21 of a frequency."""
+    assert np.finfo(np.longdouble).nmant >= 63
+    p, f = np.asarray(positions, np.longdouble), np.asarray(inv_freq, np.float64)
+    assert (np.abs(p) <= 2 ** 31).all()
+    c = f * (2.0 ** 21 + 1)
+    upper = c - (c - f)
+    a, b = p * upper.astype(np.longdouble), p * (f - upper).astype(np.longdouble)
+    return tuple(x.astype(np.float64) for x in (np.cos(a) * np.cos(b) - np.sin(a) * np.sin(b), np.sin(a) * np.cos(b) + np.cos(a) * np.sin(b)))
+
+
 def rope_axes(x, positions, axes, inv_freq, magnitude=1.0, pairing="half"):
     """x [T, H, d] turned, pair j by positions[axes[j]] (positions [number of axes, T])."""
     y = np.array(x, dtype=np.float64)
     r = 2 * len(inv_freq)
-    a = (np.asarray(positions, np.float64)[list(axes)].T * np.asarray(inv_freq))[:, None, :]
+    cos, sin = (t[:, None, :] for t in angle(np.asarray(positions)[list(axes)].T, inv_freq))
     first = slice(0, r // 2) if pairing == "half" else slice(0, r, 2)
     second = slice(r // 2, r) if pairing == "half" else slice(1, r, 2)
     u, w = np.array(y[..., first]), np.array(y[..., second])
-    y[..., first] = magnitude * (u * np.cos(a) - w * np.sin(a))
-    y[..., second] = magnitude * (w * np.cos(a) + u * np.sin(a))
+    y[..., first] = magnitude * (u * cos - w * sin)
+    y[..., second] = magnitude * (w * cos + u * sin)
     return y
 
 

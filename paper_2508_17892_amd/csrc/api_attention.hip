@@ -88,7 +88,12 @@ void fill_turns(ilre::FillArgs &a, const ilre_rope_freqs *f, const int32_t *posi
         a.positions = positions;
         a.rotary = f->rotary;
         a.magnitude = f->magnitude;
-        for (int j = 0; j < f->rotary / 2; ++j) a.turns[j] = f->inv_freq[j] / (2.0 * M_PI);
+        // A turn of fp64 alone would put a key at position 2^20 2^-33 of a turn off, at 2^31 2^-23: with the rest a turn has a hundred bits.
+        constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;  // 1 / (2 pi)
+        for (int j = 0; j < f->rotary / 2; ++j) {
+            a.turns[j] = f->inv_freq[j] * kTurn;
+            a.turns_rest[j] = fma(f->inv_freq[j], kTurn, -a.turns[j]) + f->inv_freq[j] * kTurnRest;
+        }
         for (int j = 0; axes && j < f->rotary / 2; ++j) a.axes[j] = axes[j];
     }
     if (n) {

@@ -6,7 +6,8 @@
 // and 64 + 8u .. 64 + 8u + 7, so that a head's loads and stores are whole, and the 32 channels that share a scale lie with four neighbouring lanes.  A channel is
 // r (x A + p B): p the other channel of its pair, A and B its cosine and signed sine times the weights of the two, r the norm.
 //
-// Queries and caches of the states' own type: fp32 (the angle's fraction of a turn in fp64).  Keys of a quantised cache: fp64 throughout, fp64 sines and cosines too, and one rounding, to the code.  A
+// Queries and caches of the states' own type: fp32 (the angle's fraction of a turn in fp64).  Keys of a quantised cache: fp64 throughout, fp64 sines and cosines too (of angles whose whole turns are
+// taken off before any rounding, so that far positions are as good as near ones), and one rounding, to the code.  A
 // code's border is met by one key in 2^19 or so if the key itself is off by 2^-24, and then what a cache holds depends on the order of operations of whoever fills it.
 //
 // Bound: HBM where tokens are many (65539 of 28/4 heads into 8 bits 218 us, 5.2 TB/s), otherwise the chain of loads from cu_q to the page, sines and stores (8 tokens 5.5 us, 1028 of 32/8 heads 9.6).
@@ -113,7 +114,7 @@ __device__ __forceinline__ T sum_of_eight(T x)
     return x + from_lane<kXor4>(x);
 }
 
-// Sine and cosine of `part` turns, |part| <= 1/2: to the nearest quarter turn, then the series of both up to x^15 and x^16, whose rests are below 2^-54 for |x| <= pi / 4.
+// Sine and cosine of `part` turns, |part| <= 1/2 (or 2^-20 more): to the nearest quarter turn, then the series of both up to x^15 and x^16, whose rests are below 2^-54 for |x| <= pi / 4.
 __device__ __forceinline__ void sine_and_cosine(double part, double &s, double &c)
 {
     const double quarter = rint(4.0 * part), x = fma(quarter, -0.25, part) * 6.283185307179586476925, y = x * x;
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
     };
     const bool queries = step < steps_q;
     fetch_weights(queries ? a.q_norm : a.k_norm, queries ? a.q_weight : a.k_weight);
-    const double turns = lane < half ? a.turns[lane] : 0.0;
+    const double turns = lane < half ? a.turns[lane] : 0.0, turns_rest = lane < half ? a.turns_rest[lane] : 0.0;
     const int position = a.positions && lane < half ? a.positions[(int64_t)a.axes[lane] * a.T + token] : 0;
 
     // the token's place in its sequence, and where that is in the cache
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(WPT > 4 ? WPT * 64 : kThreads) void fill_kernel(con
     }
     if (a.positions) place = position;
     if (lane < half) {
-        const double n = place * turns, part = n - rint(n);
+        const double part = fma(place, turns, -rint(place * turns)) + place * turns_rest;
         if (FMT == kPlain) {
             const float upper = (float)part, lower = (float)(part - upper) * 6.283185307f, m = (float)a.magnitude;
             float s, c;

@@ -257,7 +257,7 @@ struct FillArgs {
     const int32_t *table, *kv_len, *cu_q;
     int64_t table_stride, kv_limit;
     int n_seq, num_pages, page_shift;
-    double turns[ILRE_HEAD_DIM / 2];  // of pair j, a position
+    double turns[ILRE_HEAD_DIM / 2], turns_rest[ILRE_HEAD_DIM / 2];  // of pair j, a position; what fp64 left out of them
     uint8_t axes[ILRE_HEAD_DIM / 2];
 };
 

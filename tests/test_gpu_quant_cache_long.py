@@ -181,3 +181,70 @@ def test_long_reads(rows, fmt, dtype):
             torch.cuda.synchronize()
             for got, states in zip(view, (k, v)):
                 assert torch.equal(got[front:front + T].cpu(), states[where]) and (got[:front] == 9).all() and (got[front + T:] == 9).all()
+
+
+# ------------------------------------------------------------------------------------------------ far positions
+
+FAR = (999983, 1000003, 65000011, 2 ** 30 + 7, 2 ** 31 - 1, -(2 ** 31))
+
+
+def next_to_a_border(position, inv_freq, rng, n=1 << 16):
+    """fp32 (x1, x2) whose first channel, turned to the position, lies so near to 17, halfway between two codes, that an angle rounded to fp64 on the way (as turns, product and rest each rounded) puts
+    it on the other side; None where the search finds none."""
+    (cos, sin), turns = oq.angle(position, inv_freq), inv_freq / (2 * np.pi)
+    part = position * turns - np.rint(position * turns)
+    off_cos, off_sin = np.cos(2 * np.pi * part), np.sin(2 * np.pi * part)
+    if abs(cos) < 0.3:
+        return None
+    x2 = rng.uniform(16, 32, n).astype(np.float32).astype(np.float64)
+    x1 = ((17 + x2 * sin) / cos).astype(np.float32).astype(np.float64)
+    real, other = x1 * cos - x2 * sin - 17, x1 * off_cos - x2 * off_sin - 17
+    # (fp64 itself: a few times 2^-53 of products of up to 170)
+    hits = np.flatnonzero((real * other < 0) & (np.minimum(np.abs(real), np.abs(other)) > 2.0 ** -42))
+    return (x1[hits[0]], x2[hits[0]]) if len(hits) else None
+
+
+def far_states(pairing, rotary, inv_freq, seed):
+    """Keys [positions, 1, 128] of which channels lie next to borders of codes under a scale of one, and how many do."""
+    rng = np.random.default_rng(seed)
+    x, found = np.zeros((len(FAR), 1, 128)), 0
+    for t, p in enumerate(FAR):
+        for j in range(min(rotary // 2, 30)):
+            got = next_to_a_border(p, inv_freq[j], rng)
+            a, b = (j, j + rotary // 2) if pairing == "half" else (2 * j, 2 * j + 1)
+            if got and (pairing == "half" or j < 16):
+                x[t, 0, a], x[t, 0, b] = got
+                found += 1
+        # the block's largest magnitude: not turned, or turned from where it comes out as the first of its pair
+        if rotary < 128:
+            x[t, 0, 20 + rotary // 4] = 300
+        else:
+            cos, sin = oq.angle(p, inv_freq[31])
+            x[t, 0, 31], x[t, 0, 31 + 64] = np.float32(300 * cos), np.float32(-300 * sin)
+    return torch.from_numpy(x).float(), found
+
+
+@pytest.mark.parametrize("pairing,rotary", [("half", 128), ("half", 16), ("interleaved", 16)])
+def test_keys_at_far_positions_fall_on_their_side_of_a_border(pairing, rotary):
+    """What a cache holds is a function of the states alone, at a million tokens and at the last position there is."""
+    _announce(f"fill, far positions {pairing} {rotary}")
+    f = il.ilre_rope_frequencies(rotary, 500000.0)
+    inv_freq = np.array(f.inv_freq)[:rotary // 2]
+    k, found = far_states(pairing, rotary, inv_freq, rotary)
+    assert found >= 6
+    n = len(FAR)
+    for repeat in (1, 700 // n, 4100 // n + 1):  # each kind of kernel
+        T = n * repeat
+        x = _blank("fp8", [T], 4, 1, 16, "f32", "head")
+        x.dev["cu"] = torch.tensor([0, T], dtype=torch.int32).cuda()
+        states, pos = k.repeat(repeat, 1, 1).cuda(), torch.tensor(FAR * repeat, dtype=torch.int64).int().cuda()
+        il.ilre_norm_rope_append(None, states, None, x.cache(), f, pos, pairing=il.ILRE_ROPE_HALF if pairing == "half" else il.ILRE_ROPE_INTERLEAVED)
+        want = oq.rope_axes(_f64(k), np.array(FAR)[None], [0] * (rotary // 2), inv_freq, 1.0, pairing)
+        codes, scales = oq.store(want, "fp8")
+        assert (scales[:, 0, 0] == 127).all()
+        t = np.arange(T)
+        at, cell = x.table[0, t // 16].long().cuda(), torch.from_numpy(t % 16).cuda()
+        got = x.kp.view(torch.uint8)[at, :, cell].cpu().numpy()
+        bad = got != np.tile(codes, (repeat, 1, 1))
+        assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:5].tolist())
+        assert np.array_equal(x.ks[at, :, cell].cpu().numpy(), np.tile(scales, (repeat, 1, 1)))
