@@ -360,7 +360,8 @@ int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t
 /* Attention of the new tokens of n_seq sequences over a paged cache that holds them already: one token each, a chunk of a prompt, or any mixture.
    out[i,h,:] = sum_t softmax_t(q[i,h,:] . K[g(h),t,:] * scale) V[g(h),t,:] over the tokens that ilre_attn lets row i see; consecutive query heads share a kv
    head as in Eq. 4.  Rows that see nothing give zeros and lse = -inf.  Logits, softmax and sums are fp32, weights are rounded to opts->dtype for the
-   product with V (their sum is taken before that).  Over a quantised cache keys and values are the numbers that codes and scales stand for, exactly.  Values and keys that some row of the call sees have to be finite, and its logits below 2^30 in magnitude: fp32
+   product with V (their sum is taken before that).  Over a quantised cache keys and values are the numbers that codes and scales stand for, exactly,
+   and a block of byte 255 is NaN: a row that sees such a key is NaN, its lse too, one that sees such a value in that block's channels.  Values and keys that some row of the call sees have to be finite, and its logits below 2^30 in magnitude: fp32
    holds a logit and its row's reference to 2^-24 of themselves, and beyond that the exponential of what is left overflows.  What no row sees may hold anything.
    q, out     dev  [T, Hq, d] (strides->q_*, out_*); out must not overlap q
    lse        dev  [T, Hq] float, the natural logarithm of each row's sum of exponentials; may be NULL

@@ -28,6 +28,7 @@ __device__ __forceinline__ unsigned scale_byte(float top)
     return e == 255 ? 255u : (unsigned)(b < 1 ? 1 : b);
 }
 
+// (Byte 255 gives an infinity, the exponent that the conversion instructions take for a scale of NaN: whatever the code, zero included, NaN comes out.)
 __device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte << 23); }
 
 // 2^-(b - 127) for b = 1 .. 254 (the last one as a subnormal number).

@@ -248,3 +248,25 @@ def test_keys_at_far_positions_fall_on_their_side_of_a_border(pairing, rotary):
         bad = got != np.tile(codes, (repeat, 1, 1))
         assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:5].tolist())
         assert np.array_equal(x.ks[at, :, cell].cpu().numpy(), np.tile(scales, (repeat, 1, 1)))
+
+
+@pytest.mark.parametrize("n,kv,Hq,Hkv,dtype", [(1, 300, 8, 2, "bf16"), (1, 9000, 8, 2, "f32"), (7, 300, 8, 2, "bf16"), (200, 600, 8, 2, "bf16"), (200, 600, 8, 2, "f32"), (200, 600, 64, 8, "bf16")])
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_blocks_that_stand_for_nan(fmt, n, kv, Hq, Hkv, dtype):
+    """A block marked by the fill (byte 255, codes of zero) that rows see: nothing finite comes of it."""
+    _announce(f"byte 255 that is seen, {fmt} {n} of {kv} {Hq}/{Hkv} {dtype}")
+    G, t = Hq // Hkv, kv // 3  # a token that all rows see
+    for name in ("k", "v"):
+        x = Quant(fmt, [n], [kv], Hq, Hkv, 16, dtype, seed=1)
+        at = (int(x.table[0, t // 16]), 1, t % 16)
+        codes, scales = x.host[name]
+        codes[at][slice(32, 64) if fmt == "fp8" else slice(16, 32)] = 0
+        scales[at][1] = 255
+        x.upload()
+        out, lse = x.attend()
+        torch.cuda.synchronize()
+        want, want_lse = torch.zeros(n, Hq, 128, dtype=torch.bool), torch.zeros(n, Hq, dtype=torch.bool)
+        want[:, G:2 * G, slice(None) if name == "k" else slice(32, 64)] = True
+        want_lse[:, G:2 * G] = name == "k"
+        assert torch.equal(torch.isnan(out).cpu(), want) and torch.equal(torch.isnan(lse).cpu(), want_lse)
+        assert torch.isfinite(out[~want.cuda()]).all() and torch.isfinite(lse[~want_lse.cuda()]).all()
