@@ -1780,7 +1780,9 @@ hipError_t launch_codes16(const AttnPlan &p, const AttnArgs &a, hipStream_t s)
     auto go = [&](auto kernel, int heads) { return launch(kernel, p, 256, 4 * (32 * 256 + 16 * sizeof(float2)), a, s, FMT == ILRE_KV_FP4 ? kNumXCD : 1, heads); };
     if constexpr (DT == ILRE_BF16 && !TREE) {
         if (p.heads == 4) return go(attend_codes16<DT, FMT, 4, TREE, FMT == ILRE_KV_FP8, 4>, 4);
-        if (FMT == ILRE_KV_FP8 && p.heads == 2) return go(attend_codes16<DT, ILRE_KV_FP8, 4, TREE, true, 2>, 2);
+        if constexpr (FMT == ILRE_KV_FP8) {
+            if (p.heads == 2) return go(attend_codes16<DT, FMT, 4, TREE, true, 2>, 2);
+        }
     }
     return read_once<DT, FMT>(p, a) ? go(attend_codes16<DT, FMT, 4, TREE, true, 1>, 1) : go(attend_codes16<DT, FMT, 4, TREE, DT == ILRE_BF16 && FMT == ILRE_KV_FP8, 1>, 1);
 }
