@@ -1351,8 +1351,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
 //
 // Bound: HBM.  One token over a million (32/8 heads) 322 us in 8 bits, 6.5 TB/s, and 186 in 4, 6.0; heads side by side 350 and 227; over 4097, 8 bits, 6.8 us and 3.6 for the merge.
 //
-// Keys and values are exact in bf16, so that fp32 states take the bf16 matrix instructions too: queries and weights go in as three parts, each the rest rounded to nearest, which hold 24 bits
-// (the fp32 matrix instructions are a sixteenth as fast).
+// Keys and values are exact in bf16, so that fp32 states take the bf16 matrix instructions too: queries and weights go in as three parts, each the upper 16 bits of what is left, which hold 24 bits
+// (the fp32 matrix instructions are a sixteenth as fast; the nearest bf16 of a number beyond 2^128 - 2^119 would be an infinity).
 __device__ __forceinline__ void split_parts(const float (&x)[8], u32x4 (&part)[3])
 {
     float rest[8];
@@ -1362,10 +1362,10 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], u32x4 (&part)[3
     for (int n = 0; n < 3; ++n)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const unsigned u = pack_bf16(rest[2 * k], rest[2 * k + 1]);
-            part[n][k] = u;
-            rest[2 * k] -= __uint_as_float(u << 16);
-            rest[2 * k + 1] -= __uint_as_float(u & 0xFFFF0000u);
+            const unsigned lo = __float_as_uint(rest[2 * k]), hi = __float_as_uint(rest[2 * k + 1]);
+            part[n][k] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
+            rest[2 * k] -= __uint_as_float(lo & 0xFFFF0000u);
+            rest[2 * k + 1] -= __uint_as_float(hi & 0xFFFF0000u);
         }
 }
 

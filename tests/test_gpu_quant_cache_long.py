@@ -270,3 +270,24 @@ def test_blocks_that_stand_for_nan(fmt, n, kv, Hq, Hkv, dtype):
         want_lse[:, G:2 * G] = name == "k"
         assert torch.equal(torch.isnan(out).cpu(), want) and torch.equal(torch.isnan(lse).cpu(), want_lse)
         assert torch.isfinite(out[~want.cuda()]).all() and torch.isfinite(lse[~want_lse.cuda()]).all()
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("q_len", [1, 9])
+def test_queries_up_to_the_largest_float(fmt, q_len):
+    """fp32 queries beyond what bf16, of which three parts make one, rounds to a number; their logits are small."""
+    _announce(f"largest queries {fmt} {q_len}")
+    x = Quant(fmt, [q_len], [200], 8, 2, 16, "f32", seed=3)
+    codes, scales = oq.store(_f64(x.k[0]) * 2.0 ** -10, fmt)  # (products that fp32 holds)
+    t = torch.arange(200)
+    for part, new in zip(x.host["k"], (codes, scales)):
+        part[x.table[0, t // 16].long(), :, t % 16] = torch.from_numpy(new)
+    x.k[0] = torch.from_numpy(oq.read(codes, scales, fmt))
+    x.upload()
+    top = torch.finfo(torch.float32).max
+    x.q[:, :, 5], x.q[:, ::2, 70] = top, -top
+    x.q[:, 1, 5] = top * (1 - 2.0 ** -8)
+    x.dev["q"] = x.q.cuda()
+    out, lse = x.attend(scale=2.0 ** -118)
+    torch.cuda.synchronize()
+    x.check(out, lse, scale=2.0 ** -118)
