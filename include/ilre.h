@@ -255,7 +255,7 @@ typedef struct {
    Where the library writes one, the scale is the smallest power of two (2^-126 at least) with which the block's largest magnitude is no larger than the largest code's, so
    that nothing is cut off, and codes are rounded to nearest, ties to even, from values that have not been rounded before: keys in fp64 after norm and rotation, values as they
    come.  What a cache holds is thereby a function of the states alone.  A block with an infinity or a NaN gets byte 255, which stands for NaN, and codes of zero.
-   (A magnitude that its code rounds to 2^128, above 3.3e38, reads as an infinity.)
+   (A magnitude that its code rounds to 2^128, above 3.3e38, reads as an infinity; keys below 2^-126 are rounded to multiples of 2^-149 first.)
    The description is an ilre_paged_kv with more behind it: its struct_size says sizeof(ilre_quant_kv), k_pages and v_pages are the codes, strides count channels and are multiples
    of 128 (a lone channel's address is pages + offset * bits / 8, its scale's k_scales + offset / ILRE_KV_BLOCK: the scales have the layout of the codes).  Every call that takes
    an ilre_paged_kv takes &quant->kv; opts->dtype is then the element type of the states alone. */
@@ -353,7 +353,7 @@ int ilre_cache_read(void *k_out, void *v_out, int32_t T, int32_t d, const int32_
                     const ilre_opts *opts);
 
 /* Bytes of workspace the two attention calls can make use of (host computation only): partial results of sequences that are cut into several ranges of
-   tokens.  With less the calls cut less; without any they run all the same, slowly where few rows meet a long cache.  out_bytes: host. */
+   tokens, whatever the cache's format and layout.  With less the calls cut less; without any they run all the same, slowly where few rows meet a long cache.  out_bytes: host. */
 int ilre_attention_workspace_bytes(int32_t T, int32_t n_seq, int32_t Hq, int32_t Hkv, int32_t d, int32_t max_q, int32_t max_kv,
                                    int64_t total_kv, int32_t dtype, size_t *out_bytes);
 

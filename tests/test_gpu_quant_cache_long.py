@@ -291,3 +291,26 @@ def test_queries_up_to_the_largest_float(fmt, q_len):
     out, lse = x.attend(scale=2.0 ** -118)
     torch.cuda.synchronize()
     x.check(out, lse, scale=2.0 ** -118)
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("power", [-140, -132, -126, -118])
+def test_keys_around_the_least_scale(fmt, power):
+    """Keys below 2^-126 are rounded to multiples of 2^-149 on their way to a code: what lies further than that from a border falls on its side of it."""
+    _announce(f"fill, keys of 2^{power} {fmt}")
+    T = 64
+    k = (torch.randn(T, 2, 128, generator=torch.Generator().manual_seed(-power), dtype=torch.double) * 2.0 ** power).float()
+    x = _blank(fmt, [T], 4, 2, 16, "f32", "head")
+    x.dev["cu"] = torch.tensor([0, T], dtype=torch.int32).cuda()
+    f = il.ilre_rope_frequencies(128, BASE)
+    il.ilre_norm_rope_append(None, k.cuda(), k.cuda(), x.cache(), f)
+    want = oq.rope_axes(_f64(k), np.arange(T)[None], [0] * 64, np.array(f.inv_freq)[:64])
+    t = np.arange(T)
+    at, cell = x.table[0, t // 16].long().cuda(), torch.from_numpy(t % 16).cuda()
+    for pages, scales, y, off in ((x.kp, x.ks, want, 2.0 ** -149), (x.vp, x.vs, _f64(k), 0.0)):
+        got, sc = pages.view(torch.uint8)[at, :, cell].cpu().numpy(), scales[at, :, cell].cpu().numpy()
+        value = oq.read(got, sc, fmt)
+        assert np.array_equal(sc, oq.store(y, fmt)[1])
+        low, high = (oq.read(*oq.store(np.where(np.abs(y) > 2 * off, np.sign(y) * (np.abs(y) + d), y), fmt), fmt) for d in (-off, off))
+        sure = low == high
+        assert np.array_equal(value[sure], low[sure]) and sure.mean() > 0.99
