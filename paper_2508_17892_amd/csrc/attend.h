@@ -1349,7 +1349,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_codes(const AttnArgs a)
 // logits, i = 0..3, b = 0, 1; channels 16 db + 4 (l / 16) + i of sums.  Of keys it has a quarter of the codes, one block of a scale, of tokens l % 16 and 16 + l % 16.  With fewer
 // registers and half the LDS three or four workgroups fit a compute unit.  HEADS: kv heads a workgroup, whose wavefronts then share out the tokens of WAVES / HEADS x 32 between those of a head.
 //
-// Bound: HBM.  One token over a million (32/8 heads) 322 us in 8 bits, 6.5 TB/s, and 186 in 4, 6.0; heads side by side 350 and 227; over 4097, 8 bits, 6.8 us and 3.6 for the merge.
+// Bound: HBM.  One token over a million (32/8 heads) 323 us in 8 bits, 6.5 TB/s, and 187 in 4, 5.8 (with the merge, 6); heads side by side 349 and 228; over 4097, 8 bits, 6.8 us and 3.6 for the merge.
 //
 // Keys and values are exact in bf16, so that fp32 states take the bf16 matrix instructions too: queries and weights go in as three parts, each the upper 16 bits of what is left, which hold 24 bits
 // (the fp32 matrix instructions are a sixteenth as fast; the nearest bf16 of a number beyond 2^128 - 2^119 would be an infinity).

@@ -14,7 +14,7 @@ namespace ilre {
 //     new ones 18.4 us with 4, 25.2 with 12, 64 29.7 and 35.7, 200 51.9 and 40.3), 2 of 32 in fp32 (prompts of 77 to 900 tokens, 8/2 heads: 2 55.7 us, 4 58.6,
 //     6 74).
 //   - fp32 states over a quantised cache: 16 rows a workgroup however many there are, as only that kernel splits them into parts for the bf16 matrix instructions (32/8 heads, 8 bits: one token over 131072
-//     234 us with the fp32 instructions, 59 so; 8 over 30000 69 and 28, 100 over 9000 247 and 77, 1024 over 33000 5150 and 1800).
+//     234 us with the fp32 instructions, 53 so; 8 over 30000 69 and 28, 100 over 9000 247 and 75, 1024 over 33000 5150 and 1740).
 //   - Trees, and more than 16 rows over a quantised cache: a range leaves 32 rows behind for the merge, a quarter to half of what a tile of 128 tokens is. A range a compute unit, two from twelve tiles each
 //     on, and whole where that is a merge's worth longer at most (8 drafted tokens, 32/8 heads: contexts of 4105, 9009, 7 and 300 26.1 -> 20.8 us, eight of 3000 28.3 -> 26.9, one of 30000 33.9 -> 31.7,
 //     sixteen of 900 22.0 -> 19.8; in 8 bits 24.3 -> 18.8, 22.1 -> 20.4, 23.3 -> 21.7, 20.2 -> 16.8).
@@ -46,7 +46,7 @@ AttnPlan make_attn_plan(int dtype, int format, bool tree, int T, int n_seq, int 
     if (format != kPlain && (rows <= 16 || dtype == ILRE_F32)) {
         cut(16, 128);
         // Heads that lie side by side: a workgroup takes two or four of them, as 128 bytes here and there are read more slowly than what follows each other (one token, 8 kv heads, 8 bits: 131072
-        // tokens 67 us with one, 61 with two, 60 with four, 524288 231, 203 and 190; 4 bits 524288 142, 137 and 128, 131072 44, 44 and 44).  It cuts sequences into more ranges: not where a
+        // tokens 67 us with one, 61 with two, 60 with four, 524288 231, 203 and 190; 4 bits 524288 142, 137 and 128, 131072 44, 44 and 44).  Only there: not for 17 to 32 rows, trees and fp32 states, where nothing was measured.  It cuts sequences into more ranges: not where a
         // workgroup's share is short (8 bits, 16384 tokens 17.3, 18.0 and 20.9) or few lists are cut into very many ranges (131072 tokens of 4 kv heads 35.9, 37.5 and 38.3).
         const int64_t lists = std::min<int64_t>(p.nblocks, std::max<int64_t>((int64_t)T * G / p.rows, n_seq)) * Hkv, share = lists * tiles(total_kv / n_seq) / (2 * kNumCU);
         if (beside && dtype == ILRE_BF16 && !tree) p.heads = share >= 32 && Hkv % 4 == 0 && lists >= 8 ? 4 : format == ILRE_KV_FP8 && share >= 8 && Hkv % 2 == 0 && lists >= 8 ? 2 : 1;
