@@ -10,7 +10,7 @@
 // taken off before any rounding, so that far positions are as good as near ones), and one rounding, to the code.  A
 // code's border is met by one key in 2^19 or so if the key itself is off by 2^-24, and then what a cache holds depends on the order of operations of whoever fills it.
 //
-// Bound: HBM where tokens are many (65539 of 28/4 heads into 8 bits 218 us, 5.2 TB/s), otherwise the chain of loads from cu_q to the page, sines and stores (8 tokens 5.5 us, 1028 of 32/8 heads 9.6).
+// Bound: HBM where tokens are many (65539 of 28/4 heads into 8 bits 220 us, 5.2 TB/s), otherwise the chain of loads from cu_q to the page, sines and stores (8 tokens 5.7 us, 1028 of 32/8 heads 9.5).
 #include "kv_codes.h"
 
 #include <type_traits>
